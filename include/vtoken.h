@@ -95,8 +95,9 @@ enum {
     VTOKEN_FLAG_GATHER_OVERFLOW = 32u,/* gather_logical / build_slot_mapping: more live tokens than the output holds */
     VTOKEN_FLAG_BAD_VICTIM = 64u,     /* vtoken_evict_tokens: a victim outside its request's registered tokens: skipped */
     VTOKEN_FLAG_APPEND_STOPPED = 128u,/* vtoken_sync_new_tokens: table capacity or block list exhausted: request grew less */
-    VTOKEN_FLAG_CHECK_FAILED = 256u   /* checked build only: an index into scratch, a table or a pool fell outside its
+    VTOKEN_FLAG_CHECK_FAILED = 256u,  /* checked build only: an index into scratch, a table or a pool fell outside its
                                          range; the access was skipped */
+    VTOKEN_FLAG_BAD_POSITION = 512u   /* vtoken_write_tokens: a position outside [0, max_position): token skipped */
 };
 
 /* Launch shape of the bulk-copy kernel (tuning and tests; the defaults are the measured best).
@@ -558,6 +559,113 @@ int vtoken_gather_logical_noalloc(const void *k_pool, const void *v_pool, int32_
  * Uses the context's planner scratch (do not overlap with a plan in flight).  Capturable. */
 int vtoken_check_tables(vtoken_ctx *ctx, const vtoken_plan_in *in, const uint8_t *protect, uint32_t *out_bits,
                         void *cuda_stream);
+
+/* ---- Writing and reading the cache: the attention step next to the relocation -----------------------
+ * The calls below serve the step that surrounds a repack: the projections of the step's tokens go into
+ * the slots that vtoken_sync_new_tokens gave them, and the step's queries attend to the active tokens
+ * through the cached slot-translation arrays (vtoken_slot_cache_update).  They work on one layer of the
+ * context's pools per call, only enqueue kernels on the stream and are capturable.
+ *
+ * Types.  VTOKEN_KV_BF16 / VTOKEN_KV_FP16 rows are [num_kv_heads][head_dim] 16-bit values.  VTOKEN_KV_FP4
+ * rows hold 4-bit values (1 sign, 2 exponent, 1 mantissa bit: 0, .5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) with one 8-bit scale (4 exponent, 3 mantissa bits, at most 448) per 16 consecutive values of
+ * a head: first [num_kv_heads][head_dim / 2] bytes of codes, element 2i in the low half of byte i, then
+ * [num_kv_heads][head_dim / 16] bytes of scales, padded with bytes that are neither read nor written to a
+ * multiple of 16.  A value is code * scale * 2^exponent.  Its two factors have 2 and 4 significant bits,
+ * so every 4-bit row is held exactly by the 16-bit types and attention over it rounds nothing that the
+ * 16-bit cache would not.  To every other call of this library such rows are opaque bytes: create the
+ * context with num_kv_heads 1, head_dim = vtoken_kv_row_bytes, elem_bytes 1. */
+enum { VTOKEN_KV_BF16 = 0, VTOKEN_KV_FP16 = 1, VTOKEN_KV_FP4 = 2 };
+
+typedef struct {
+    int32_t num_q_heads, num_kv_heads; /* num_q_heads a multiple of num_kv_heads; query head h reads key head
+                                          h / (num_q_heads / num_kv_heads) */
+    int32_t head_dim;                  /* 64 or 128 */
+    int32_t kv_type;                   /* VTOKEN_KV_*: the rows of the pools */
+    int32_t act_type;                  /* VTOKEN_KV_BF16 or VTOKEN_KV_FP16: queries, keys, values, outputs; equal to
+                                          kv_type unless that is VTOKEN_KV_FP4 */
+    int32_t k_exponent, v_exponent;    /* -60 .. 60, VTOKEN_KV_FP4 only: power of two that every value of the K (V)
+                                          rows carries besides its scale, for pools whose values leave the range
+                                          of code * scale (about 2^-10 .. 2688) */
+} vtoken_heads;
+
+/* Bytes of one pool row; it must equal the context's num_kv_heads * head_dim * elem_bytes in the calls below
+ * (VTOKEN_EINVAL otherwise).  Negative: VTOKEN_EINVAL, the geometry is not supported. */
+int64_t vtoken_kv_row_bytes(const vtoken_heads *heads);
+
+typedef struct {                   /* all pointers DEVICE, 16-byte aligned unless an int array */
+    const int32_t *num_tokens;     /* device scalar, clamped to [0, max_tokens]; NULL: max_tokens */
+    int32_t max_tokens;            /* rows of the arrays below */
+    const void *q, *k, *v;         /* [max_tokens][heads][head_dim] act_type; q may be NULL (no queries) */
+    int64_t q_stride, k_stride, v_stride;   /* elements between tokens, multiples of 8; 0: dense.  The three may be slices
+                                          of one projection output */
+    const int32_t *positions;      /* [max_tokens] logical token ids */
+    const int32_t *slots;          /* [max_tokens] slot of each token; negative: not cached */
+    const void *q_weight, *k_weight; /* [head_dim] act_type, or NULL: no normalisation of the queries (keys) */
+    float eps;                     /* > 0 where a weight is given */
+    const float *cos_sin;          /* [max_position][rot_dim]: rot_dim / 2 cosines, then rot_dim / 2 sines */
+    int32_t max_position;          /* rows of cos_sin; positions are checked against it */
+    int32_t rot_dim;               /* rotated leading dimensions of a head: multiple of 16, 0 = no rotation (cos_sin
+                                      may be NULL, positions are not read) */
+    int32_t interleaved;           /* rotated pairs: 0 (i, i + rot_dim / 2); 1 (2i, 2i + 1) */
+    void *q_out;                   /* [max_tokens][num_q_heads][head_dim]; may be q itself (with q's stride) */
+    int64_t q_out_stride;          /* elements, multiple of 8; 0: dense */
+} vtoken_write_in;
+
+/* One pass over the projections of a step's tokens.  Per head x of q and k, in 32 bits: with a weight w,
+ * x_i <- x_i * w_i / sqrt(mean(x^2) + eps); then the pairs (a, b) of the first rot_dim dimensions become
+ * (a cos - b sin, b cos + a sin) at the token's position; rounded once to act_type.  Queries go to q_out;
+ * keys and (untouched) values go to the K and V rows of the token's slot in `layer`.  Into VTOKEN_KV_FP4
+ * pools a key row is computed in 64 bits, rounded to act_type and then, like the value row, held per group
+ * of 16 as scale = nearest 8-bit scale of max|x| / 6 and codes = nearest 4-bit values of x / scale (ties
+ * to even; a zero scale gives zero codes; a group with a NaN or an infinity gets the scale NaN and reads
+ * back as NaN).  A token whose slot lies outside the pool writes no row (VTOKEN_FLAG_BAD_SLOT), one whose
+ * position lies outside cos_sin is skipped altogether (VTOKEN_FLAG_BAD_POSITION); slots must be distinct. */
+int vtoken_write_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_write_in *in,
+                        void *cuda_stream);
+
+/* The K and V rows of the given slots of `layer` as act_type values: out_k / out_v [max_tokens][num_kv_heads]
+ * [head_dim], 16-byte aligned; either may be NULL.  A negative slot reads as zeros, one outside the pool too
+ * (VTOKEN_FLAG_BAD_SLOT).  num_tokens as above. */
+int vtoken_read_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const int32_t *num_tokens,
+                       int32_t max_tokens, const int32_t *slots, void *out_k, void *out_v, void *cuda_stream);
+
+typedef struct {                   /* all pointers DEVICE */
+    const int32_t *num_requests;   /* device scalar R <= max_requests of the context */
+    const int32_t *q_offsets;      /* [R+1] first query row of each request, non-decreasing */
+    const int32_t *positions;      /* [max_query_tokens] logical id of each query token */
+    const void *q;                 /* [max_query_tokens][num_q_heads][head_dim] act_type, 16-byte aligned */
+    int64_t q_stride;              /* elements between tokens, multiple of 8; 0: dense */
+    int32_t max_query_tokens;      /* rows of q; q_offsets beyond it are clipped (VTOKEN_FLAG_CAPACITY) */
+    int32_t max_query_len;         /* a hint: longest q_offsets[r+1] - q_offsets[r], >= 1.  It chooses between the
+                                      kernel for few and the one for many query rows per request; both are
+                                      right for every length */
+    const int32_t *tt_offsets;     /* [R+1] the slot cache of request r starts at tt_offsets[r] */
+    const int32_t *cache_slots;    /* slots of its active tokens, in ascending order of their ids */
+    const int32_t *cache_ids;      /* their logical ids, strictly ascending; NULL: 0, 1, 2, ... (nothing was evicted) */
+    const int32_t *cache_len;      /* [R] active tokens */
+    float sm_scale;                /* factor of the scores, finite */
+    int32_t window;                /* 0: none; else a query at p sees ids > p - window ... */
+    int32_t sinks;                 /* ... and ids < sinks (attention sinks).  Always: ids <= p */
+    void *out;                     /* [max_query_tokens][num_q_heads][head_dim] act_type, 16-byte aligned */
+    int64_t out_stride;            /* elements, multiple of 8; 0: dense */
+    float *lse;                    /* [max_query_tokens][num_q_heads] or NULL: natural logarithm of the sum of the
+                                      exponentials of the scaled scores */
+    void *workspace;               /* 16-byte aligned, zeroed by the caller once, when it is allocated; each call leaves
+                                      it ready for the next.  Calls that may overlap need workspaces of their own */
+    int64_t workspace_bytes;       /* >= vtoken_attention_workspace_bytes (VTOKEN_ECAPACITY otherwise) */
+} vtoken_attention_in;
+
+/* Bytes of workspace for calls of up to max_query_tokens rows on this context; negative: VTOKEN_EINVAL. */
+int64_t vtoken_attention_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens);
+
+/* out = softmax(sm_scale * q K^T) V over the cached tokens that the query sees, for the query rows of every
+ * request; scores, softmax and sums in 32 bits.  A row that sees no token is zero, its lse minus infinity.
+ * Tokens that no query of the row's request sees are not read; what a masked token holds (NaN, infinities) does
+ * not reach a row that does not see it.  A slot outside the pool makes its token invisible
+ * (VTOKEN_FLAG_BAD_SLOT).  Every row is summed in an order that depends on the sizes and the tables alone. */
+int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in,
+                     void *cuda_stream);
 
 /* Diagnostics. */
 const char *vtoken_strerror(int code);

@@ -7,6 +7,12 @@ names, argument marshalling only).  There is no CPU fallback: using the binding 
 built library raises ImportError.
 """
 from .binding import (  # noqa: F401
+    Heads,
+    vtoken_attention,
+    vtoken_attention_workspace_bytes,
+    vtoken_kv_row_bytes,
+    vtoken_read_tokens,
+    vtoken_write_tokens,
     VtokenError,
     vtoken_apply_moves,
     vtoken_block_liveness,

@@ -16,7 +16,8 @@ CHECKED_LIB_PATH = os.path.join(_PKG, "libvtoken_checked.so")     # same ABI, ev
 OK, EINVAL, ECAPACITY, ECUDA, ENOMEM, ESTATE = 0, -1, -2, -3, -4, -5
 NOT_SELECTED, REPACKED, NO_GAIN, DEFERRED_NO_FREE = 0, 1, 2, 3
 FLAG_BAD_SLOT, FLAG_BAD_BLOCK, FLAG_BAD_FREE, FLAG_CAPACITY, FLAG_TIMEOUT, FLAG_GATHER_OVERFLOW = 1, 2, 4, 8, 16, 32
-FLAG_BAD_VICTIM, FLAG_APPEND_STOPPED, FLAG_CHECK_FAILED = 64, 128, 256
+FLAG_BAD_VICTIM, FLAG_APPEND_STOPPED, FLAG_CHECK_FAILED, FLAG_BAD_POSITION = 64, 128, 256, 512
+KV_BF16, KV_FP16, KV_FP4 = 0, 1, 2
 
 SYMBOLS = ["vtoken_create", "vtoken_destroy", "vtoken_plan", "vtoken_repack", "vtoken_gather_logical",
            "vtoken_read_counts", "vtoken_repack_host", "vtoken_strerror", "vtoken_last_cuda_error",
@@ -26,7 +27,8 @@ SYMBOLS = ["vtoken_create", "vtoken_destroy", "vtoken_plan", "vtoken_repack", "v
            "vtoken_waves_workspace_bytes", "vtoken_repack_waves", "vtoken_slot_cache_mark",
            "vtoken_slot_cache_update", "vtoken_repack_host_partial", "vtoken_check_tables",
            "vtoken_evict_tokens_counted", "vtoken_sync_new_tokens_counted", "vtoken_checked_build",
-           "vtoken_debug_probe"]
+           "vtoken_debug_probe", "vtoken_kv_row_bytes", "vtoken_write_tokens", "vtoken_read_tokens",
+           "vtoken_attention_workspace_bytes", "vtoken_attention"]
 
 
 class VtokenError(RuntimeError):
@@ -107,6 +109,32 @@ class HostTables(ctypes.Structure):
                 ("req_status", ctypes.c_void_p), ("counts", ctypes.c_void_p), ("released_blocks", ctypes.c_void_p)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("kv_type", ctypes.c_int32), ("act_type", ctypes.c_int32), ("k_exponent", ctypes.c_int32),
+                ("v_exponent", ctypes.c_int32)]
+
+
+class WriteIn(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_void_p), ("max_tokens", ctypes.c_int32), ("q", ctypes.c_void_p),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("positions", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("cos_sin", ctypes.c_void_p), ("max_position", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("q_out", ctypes.c_void_p),
+                ("q_out_stride", ctypes.c_int64)]
+
+
+class AttentionIn(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_void_p), ("q_offsets", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("max_query_tokens", ctypes.c_int32),
+                ("max_query_len", ctypes.c_int32), ("tt_offsets", ctypes.c_void_p), ("cache_slots", ctypes.c_void_p),
+                ("cache_ids", ctypes.c_void_p), ("cache_len", ctypes.c_void_p), ("sm_scale", ctypes.c_float),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("out", ctypes.c_void_p),
+                ("out_stride", ctypes.c_int64), ("lse", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64)]
+
+
 _lib = None
 _libs = {}
 _flavour = "production"
@@ -184,6 +212,16 @@ def load():
         lib.vtoken_slot_cache_update.argtypes = [ctypes.c_void_p] * 13
         lib.vtoken_checked_build.argtypes = []
         lib.vtoken_debug_probe.argtypes = [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p]
+        lib.vtoken_kv_row_bytes.argtypes = [ctypes.POINTER(Heads)]
+        lib.vtoken_kv_row_bytes.restype = ctypes.c_int64
+        lib.vtoken_write_tokens.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32,
+                                            ctypes.POINTER(WriteIn), ctypes.c_void_p]
+        lib.vtoken_read_tokens.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32, ctypes.c_void_p,
+                                           ctypes.c_int32] + [ctypes.c_void_p] * 4
+        lib.vtoken_attention_workspace_bytes.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32]
+        lib.vtoken_attention_workspace_bytes.restype = ctypes.c_int64
+        lib.vtoken_attention.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32,
+                                         ctypes.POINTER(AttentionIn), ctypes.c_void_p]
         _libs[path] = lib
         _lib = lib
     return _lib
@@ -483,3 +521,52 @@ def vtoken_repack_waves(ctx, *, num_requests, bt_offsets, bt_blocks, tt_offsets,
                                       int(partial.get("detach_rule", 0))))
     _check(load().vtoken_repack_waves(ctx, ctypes.byref(pin), po, num_waves, ctypes.byref(wout), _stream(stream)),
            "vtoken_repack_waves", ctx)
+
+
+# ---- the attention step around the relocation ------------------------------------------------
+def vtoken_kv_row_bytes(heads) -> int:
+    """Bytes of a pool row of this geometry; VtokenError EINVAL when it is not supported."""
+    n = load().vtoken_kv_row_bytes(ctypes.byref(heads))
+    if n < 0:
+        raise VtokenError(int(n), "vtoken_kv_row_bytes")
+    return n
+
+
+def vtoken_write_tokens(ctx, *, heads, layer, max_tokens, k, v, slots, positions=None, num_tokens=None, q=None,
+                        q_out=None, q_weight=None, k_weight=None, eps=0.0, cos_sin=None, max_position=0, rot_dim=0,
+                        interleaved=False, q_stride=0, k_stride=0, v_stride=0, q_out_stride=0, stream=None) -> None:
+    """Queries and keys normalised per head and rotated, keys and values written to their slots."""
+    a = WriteIn(_ptr(num_tokens), max_tokens, _ptr(q), _ptr(k), _ptr(v), q_stride, k_stride, v_stride,
+                _ptr(positions), _ptr(slots), _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos_sin), max_position,
+                rot_dim, interleaved, _ptr(q_out), q_out_stride)
+    rc = load().vtoken_write_tokens(ctx, heads, layer, a, _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_write_tokens", ctx)
+
+
+def vtoken_read_tokens(ctx, *, heads, layer, max_tokens, slots, out_k=None, out_v=None, num_tokens=None,
+                       stream=None) -> None:
+    """K and V rows of the given slots as 16-bit values."""
+    rc = load().vtoken_read_tokens(ctx, heads, layer, _ptr(num_tokens), max_tokens, _ptr(slots), _ptr(out_k),
+                                   _ptr(out_v), _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_read_tokens", ctx)
+
+
+def vtoken_attention_workspace_bytes(ctx, heads, max_query_tokens) -> int:
+    n = load().vtoken_attention_workspace_bytes(ctx, ctypes.byref(heads), max_query_tokens)
+    if n < 0:
+        raise VtokenError(int(n), "vtoken_attention_workspace_bytes")
+    return n
+
+
+def vtoken_attention(ctx, *, heads, layer, num_requests, q_offsets, positions, q, max_query_tokens, max_query_len,
+                     tt_offsets, cache_slots, cache_len, out, sm_scale, workspace, workspace_bytes, cache_ids=None,
+                     lse=None, window=0, sinks=0, q_stride=0, out_stride=0, stream=None) -> None:
+    """Queries of every request against the active tokens of its slot cache."""
+    a = AttentionIn(_ptr(num_requests), _ptr(q_offsets), _ptr(positions), _ptr(q), q_stride, max_query_tokens,
+                    max_query_len, _ptr(tt_offsets), _ptr(cache_slots), _ptr(cache_ids), _ptr(cache_len), sm_scale,
+                    window, sinks, _ptr(out), out_stride, _ptr(lse), _ptr(workspace), workspace_bytes)
+    rc = load().vtoken_attention(ctx, heads, layer, a, _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_attention", ctx)

@@ -23,7 +23,8 @@ LIB = os.path.join(PKG, "libvtoken.so")
 CHECKED_LIB = os.path.join(PKG, "libvtoken_checked.so")
 
 LIB_SOURCES = ["api.cu", "plan.cu", "plan_small.cu", "copy.cu", "gather.cu", "gather_static.cu", "runtime.cu", "plan_partial.cu",
-               "waves.cu", "slot_cache.cu", "check.cu"]
+               "waves.cu", "slot_cache.cu", "check.cu", "tokens.cu", "attention.cu"]
+HEADERS = ["common.cuh", "heads.cuh", "attention.cuh"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC",
@@ -40,8 +41,7 @@ def _nvcc() -> str:
 def _stale(lib: str, sources) -> bool:
     if not os.path.exists(lib):
         return True
-    deps = [os.path.join(CSRC, s) for s in sources] + [os.path.join(CSRC, "common.cuh"),
-                                                       os.path.join(INCLUDE, "vtoken.h")]
+    deps = [os.path.join(CSRC, s) for s in [*sources, *HEADERS]] + [os.path.join(INCLUDE, "vtoken.h")]
     return os.path.getmtime(lib) < max(os.path.getmtime(d) for d in deps if os.path.exists(d))
 
 

@@ -1,0 +1,207 @@
+// What the attention kernels share: arguments, the request's share of the slot cache, matrix instructions,
+// rows of the pools in registers, and the exact recomputation of a row that a masked NaN reached.
+#pragma once
+#include "heads.cuh"
+
+struct VtkAttnArgs {
+    const int32_t *num_requests;
+    vtk_arr<const int32_t> q_offsets, positions, tt_offsets, cache_slots, cache_ids, cache_len;
+    const uint16_t *q;
+    uint16_t *out;
+    float *lse;
+    const uint8_t *k_rows, *v_rows;      // this layer's slabs
+    int64_t q_stride, out_stride, row_bytes, slots_per_layer, max_tokens;
+    int32_t max_requests, max_query_tokens, hq, hkv, group;
+    int32_t window, sinks;
+    float scale_log2;                    // sm_scale * log2(e) * 2^k_exponent
+    float v_mul;                         // 2^v_exponent
+    uint32_t *flags;
+    uint32_t *counters;                  // workspace: arrivals of split rows, zero between calls
+    float *part;                         // workspace: partial rows
+    int32_t target;                      // items (per key head) that a call is cut into when it is long enough
+    int32_t min_chunk;                   // tokens of the smallest item
+};
+
+// What a request's queries read of its slot cache: entries [0, n_sink) and [lo, lo + n - n_sink), numbered
+// 0 .. n - 1 in that order ("virtual" indexes).
+struct VtkRequest {
+    int q0, qn;                          // query rows
+    int64_t base;                        // first cache entry
+    int lo, n_sink, n;
+    __device__ __forceinline__ int64_t entry(int v) const { return base + (v < n_sink ? v : lo + (v - n_sink)); }
+    __device__ __forceinline__ int index(int v) const { return v < n_sink ? v : lo + (v - n_sink); }
+};
+
+__device__ __forceinline__ int vtk_clamp_offset(int x, int cap) { return x < 0 ? 0 : (x > cap ? cap : x); }
+
+// entries of the ascending ids [base, base + len) that are <= p
+__device__ inline int vtk_ids_up_to(const VtkAttnArgs &a, int64_t base, int len, int p)
+{
+    if (p < 0) return 0;
+    if (a.cache_ids.null()) return p + 1 < len ? p + 1 : len;
+    if (len == 0 || a.cache_ids[base + len - 1] <= p) return len;
+    int lo = 0, hi = len - 1;            // ids[hi] > p
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (a.cache_ids[base + mid] <= p) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+// Ids are strictly ascending from 0 or above, so ids[i] >= i: entry i >= sinks cannot be a sink, and of the
+// entries with ids <= pmax at most (pmax - pmin) + window have an id > pmin - window.
+__device__ inline VtkRequest vtk_request_span(const VtkAttnArgs &a, int64_t base, int len, int pmin, int pmax)
+{
+    VtkRequest q;
+    q.q0 = q.qn = 0;
+    q.base = base;
+    const int hi = vtk_ids_up_to(a, base, len, pmax);
+    int64_t lo = 0;
+    if (a.window > 0) lo = (int64_t)hi - ((int64_t)pmax - pmin) - a.window;
+    q.lo = lo > 0 ? (int)lo : 0;
+    q.n_sink = a.sinks < q.lo ? a.sinks : q.lo;
+    q.n = q.n_sink + (hi - q.lo);
+    return q;
+}
+
+// rows and cache range of request r, clipped to what exists
+__device__ inline void vtk_request_rows(const VtkAttnArgs &a, int r, int &q0, int &qn, int64_t &base, int &len, bool &clipped)
+{
+    const int a0 = a.q_offsets[r], a1 = a.q_offsets[r + 1];
+    const int64_t t0 = a.tt_offsets[r], t1 = a.tt_offsets[r + 1];
+    const int want = a.cache_len[r];
+    q0 = vtk_clamp_offset(a0, a.max_query_tokens);
+    const int q1 = vtk_clamp_offset(a1, a.max_query_tokens);
+    qn = q1 > q0 ? q1 - q0 : 0;
+    base = t0 < 0 ? 0 : (t0 > a.max_tokens ? a.max_tokens : t0);
+    const int64_t end = t1 < base ? base : (t1 > a.max_tokens ? a.max_tokens : t1);
+    len = want < 0 ? 0 : (want > end - base ? (int)(end - base) : want);
+    clipped = a0 != q0 || a1 != q1 || q1 < q0 || t0 != base || t1 != end || want != len;
+}
+
+__device__ __forceinline__ bool vtk_sees(int id, int p, int window, int sinks)
+{
+    return id <= p && (window == 0 || id > (int64_t)p - window || id < sinks);
+}
+
+// ---- matrix instructions: 16 x 8 += 16 x 16 by 16 x 8, 32-bit accumulators ----------------------
+template <typename M>
+__device__ __forceinline__ void vtk_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void vtk_mma<VtkBf16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void vtk_mma<VtkFp16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ float vtk_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint4 vtk_ldg16(const void *p)
+{
+    uint4 w;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p));
+    return w;
+}
+
+// ---- one head of one pool row, `N` consecutive values from `d` on, as 32-bit values -------------
+// (the value without 2^exponent)
+template <int D, bool FP4, typename Act, int N>
+__device__ __forceinline__ void vtk_row_values(const uint8_t *row, int hkv, int head, int d, float (&x)[N])
+{
+    if (!FP4) {
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(row + ((int64_t)head * D + d) * 2);
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+            const float2 v = Act::unpack(p[j]);
+            x[2 * j] = v.x;
+            x[2 * j + 1] = v.y;
+        }
+    } else {
+        static_assert(N == 2 || N == 4, "one or two bytes of codes");
+        const uint32_t two = *reinterpret_cast<const uint16_t *>(row + head * (D / 2) + (d / 4) * 2);
+        const uint32_t codes = N == 4 ? two : two >> (4 * (d & 2));
+        const uint32_t s2 = vtk_scales_to_half2(row[hkv * (D / 2) + head * (D / 16) + d / 16]);
+        const float s = __half2float(__ushort_as_half((uint16_t)(s2 & 0xffffu)));
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+            const float2 v = VtkFp16::unpack(vtk_codes_to_half2(codes >> (8 * j)));
+            x[2 * j] = v.x * s;
+            x[2 * j + 1] = v.y * s;
+        }
+    }
+}
+
+// One query row by one warp, token by token: the definition.  The matrix kernels multiply a masked token's
+// value by a zero weight, so a NaN or an infinity there would reach rows that do not see the token; a row
+// whose result is not finite is computed again here, where only the tokens it sees are touched.  Values come
+// out as the lane's D / 32 consecutive dimensions.
+template <int D, bool FP4, typename Act>
+__device__ __noinline__ void vtk_row_again(const VtkAttnArgs &a, int64_t q_row, int head, int pos, int64_t base, int len,
+                                           float (&o)[D / 32], float &m, float &l)
+{
+    constexpr int N = D / 32;
+    const int lane = vtk_lane(), kv = head / a.group;
+    float q[N];
+    const uint32_t *qp = reinterpret_cast<const uint32_t *>(a.q + q_row * a.q_stride + (int64_t)head * D + lane * N);
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+        const float2 v = Act::unpack(qp[j]);
+        q[2 * j] = v.x;
+        q[2 * j + 1] = v.y;
+    }
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = 0.f;
+    for (int i = 0; i < len; ++i) {
+        const int id = a.cache_ids.null() ? i : a.cache_ids[base + i];
+        const int64_t slot = a.cache_slots[base + i];
+        if (slot < 0 || slot >= a.slots_per_layer || !vtk_sees(id, pos, a.window, a.sinks)) continue;
+        float k[N], v[N];
+        vtk_row_values<D, FP4, Act, N>(a.k_rows + slot * a.row_bytes, a.hkv, kv, lane * N, k);
+        vtk_row_values<D, FP4, Act, N>(a.v_rows + slot * a.row_bytes, a.hkv, kv, lane * N, v);
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) s += q[j] * k[j];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        s *= a.scale_log2;
+        const float m2 = fmaxf(m, s), keep = m == m2 ? 1.f : (m == -INFINITY ? 0.f : exp2f(m - m2));
+        const float p = s == -INFINITY ? 0.f : exp2f(s - m2);
+        l = l * keep + p;
+#pragma unroll
+        for (int j = 0; j < N; ++j) o[j] = o[j] * keep + p * v[j];
+        m = m2;
+    }
+}
+
+// the row's output and lse: the lane's N consecutive dimensions
+template <int D, typename Act>
+__device__ __forceinline__ void vtk_store_row(const VtkAttnArgs &a, int64_t q_row, int head, float (&o)[D / 32], float m, float l)
+{
+    constexpr int N = D / 32;
+    const int lane = vtk_lane();
+    const float r = l == 0.f ? 0.f : a.v_mul / l;
+    uint32_t *p = reinterpret_cast<uint32_t *>(a.out + q_row * a.out_stride + (int64_t)head * D + lane * N);
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) w[j] = Act::pack(o[2 * j] * r, o[2 * j + 1] * r);
+    if (N == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[N / 2 - 1]);
+    else p[0] = w[0];
+    if (a.lse != nullptr && lane == 0) a.lse[q_row * a.hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// host: launchers of attention.cu and of attention_prompt.cu
+int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st);
+int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs *a);

@@ -25,6 +25,7 @@ constexpr int AT_WARPS = 4, AT_NT = AT_WARPS * 32;
 // CTAs per SM: what 168 (8 query rows) and 255 registers a thread leave room for
 template <int NR> constexpr int AT_CTAS = NR == 8 ? 3 : 2;
 // requests whose spans a CTA keeps in shared memory (below the 48 KB of static arrays)
+constexpr int AT_ROW_LIMIT = 32;          // query rows (tokens times group) of a request up to which it is worked on here
 template <int NR> constexpr int AT_KNOWN = NR == 8 ? 512 : 256;
 
 // ---- 16 tokens of one head in registers --------------------------------------------------------
@@ -116,6 +117,7 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
     bool c;
     vtk_request_rows(a, r, k.q0, k.qn, k.base, k.len, c);
     clipped |= c;
+    if (k.qn * (int64_t)a.group > a.row_limit) k.qn = 0;
     k.lo = k.n_sink = 0;
     k.n = k.len;
     if (k.qn > 0 && k.qn <= 8) {         // few queries: only what one of them can see
@@ -552,8 +554,8 @@ int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *
         a->target = (int32_t)target;
         a->min_chunk = 64;
     }
-    const int64_t counters = (splits * 4 + 15) / 16 * 16;
-    if (a && a->counters) a->part = (float *)((uint8_t *)a->counters + counters);
+    const int64_t counters = (splits * 4 + 15) / 16 * 16 + 16;           // and the prompt kernel's two tickets in front
+    if (a && a->counters) a->part = (float *)((uint8_t *)(a->counters - 4) + counters);
     return counters + splits * 16 * (heads->head_dim + 2) * 4;
 }
 
@@ -616,9 +618,12 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     a.scale_log2 = in->sm_scale * 1.4426950408889634f * two_to(heads->k_exponent);
     a.v_mul = two_to(heads->v_exponent);
     a.flags = &ctx->rt_counts->error_flags;
-    a.counters = (uint32_t *)in->workspace;
+    a.counters = (uint32_t *)in->workspace + 4;
     a.part = nullptr;
-    return vtk_launch_attention_rows(ctx, heads, a, in->max_query_len, (cudaStream_t)cuda_stream);
+    const bool prompts = (int64_t)in->max_query_len * a.group > AT_ROW_LIMIT;
+    a.row_limit = prompts ? AT_ROW_LIMIT : INT32_MAX;
+    const int rc = vtk_launch_attention_rows(ctx, heads, a, prompts ? 1 : in->max_query_len, (cudaStream_t)cuda_stream);
+    return rc == VTOKEN_OK && prompts ? vtk_launch_attention_prompt(ctx, heads, a, (uint32_t *)in->workspace, (cudaStream_t)cuda_stream) : rc;
 }
 
 }  // extern "C"

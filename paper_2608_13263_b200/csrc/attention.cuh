@@ -20,6 +20,7 @@ struct VtkAttnArgs {
     float *part;                         // workspace: partial rows
     int32_t target;                      // items (per key head) that a call is cut into when it is long enough
     int32_t min_chunk;                   // tokens of the smallest item
+    int32_t row_limit;                   // requests of more query rows (tokens times group) belong to attention_prompt.cu
 };
 
 // What a request's queries read of its slot cache: entries [0, n_sink) and [lo, lo + n - n_sink), numbered
@@ -204,4 +205,5 @@ __device__ __forceinline__ void vtk_store_row(const VtkAttnArgs &a, int64_t q_ro
 
 // host: launchers of attention.cu and of attention_prompt.cu
 int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st);
+int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st);
 int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs *a);

@@ -1,0 +1,702 @@
+// Attention of many query rows per request (prompts and chunks of prompts) over the slot cache, on the fifth
+// generation tensor cores.
+//
+// Bound by the tensor cores and, about equally, by the exponentials: 4 * D flops and one exponential per pair, and
+// 128 x 128 pairs of D 128 take the tensor pipe (8192 flops a cycle) as long as the SM's 16 exponentials a cycle.
+// One CTA per SM takes items (request, two tiles of 128 query rows, key head); the rows of a tile are the query
+// tokens of the request times the heads of the group, so a K or V tile is read once for all of them, and the two
+// row tiles share it again.  Roles, 16 warps:
+//   0 .. 3, 4 .. 7   softmax of row tile 0 and 1, one thread a row: scores from tensor memory, running maximum (moved
+//                    only when a score passes it by 2^8), exponentials, P as 16 bits back into the scores' columns
+//   8 .. 11          producers: rows of Q, K and V gathered by slot into 128-byte-swizzled tiles, 16 bytes a thread by
+//                    cp.async, or 4-bit rows expanded to half precision in registers on the way
+//   12               one thread issues every tcgen05.mma: S = Q K^T (both operands from shared memory, K-major),
+//                    O += P V (P from tensor memory, V as it lies: token rows, the MN-major operand)
+//   13               looks up the next item while this one runs
+// While the softmax of one row tile runs, the products of the other keep the tensor pipe busy.
+// Tensor memory: 2 x 128 columns of scores (P overwrites the first half of its own), 2 x D columns of output.
+// Every wait is bounded (wait_limit_ms): where one runs out, the roles leave their loops, the tensor memory is freed
+// and VTOKEN_FLAG_TIMEOUT is set.
+#include "attention.cuh"
+
+namespace {
+
+constexpr int AP_NT = 512, AP_STAGES = 4, AP_TILE = 128, AP_META = 4;
+
+struct Item {                            // what one CTA works on
+    int none;
+    int kv, q0, first, rows, len;        // key head; first query row of the request; first row and rows of the pair of tiles
+    int pmin[2], pmax[2];                // positions of the two row tiles
+    int tiles;                           // tiles of 128 tokens
+    VtkRequest span;
+};
+
+struct Meta {                            // what the softmax needs of a tile's tokens
+    int ids[AP_TILE];
+    uint32_t every[2][4];                // bit: the token is seen by every row of the tile
+};
+
+template <int D>
+struct Shared {
+    uint8_t q[2][D / 64][AP_TILE * 128];
+    uint8_t kv[AP_STAGES][D / 64][AP_TILE * 128];
+    Meta meta[AP_META];
+    int slots[2][AP_TILE];               // the producers' tile: slot, -1 = zeros
+    float row_scale[2][AP_TILE];
+    Item item[2];
+    int prefix[AP_NT + 1];
+    int warp_sum[AP_NT / 32];
+    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], s_full[2], p_full[2], o_full[2], q_full, drain;
+    uint32_t tmem;
+    int abort;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t global_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// false when the phase did not complete within the limit, or another role has given up
+__device__ __noinline__ bool mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
+{
+    const uint64_t t0 = global_ns();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try(bar, parity)) return true;
+        if (*abort) return false;
+        if (global_ns() - t0 > limit_ns) { *abort = 1; return false; }
+    }
+}
+__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, uint64_t limit_ns, int *abort)
+{
+    return mbar_try(bar, parity) || mbar_try(bar, parity) || mbar_wait_long(bar, parity, limit_ns, abort);
+}
+
+// ---- tcgen05 -------------------------------------------------------------------------------------
+__device__ __forceinline__ void tc_commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+#define R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
+#define W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+// 32 consecutive columns of the warp's 32 lanes: thread = lane, register = column
+__device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+                 "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24) : "r"(addr));
+}
+__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
+                 "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(addr), W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24) : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), W8(r, 0), W8(r, 8) : "memory");
+}
+
+// Shared-memory operand: 128-byte swizzle; 8-row (K-major) or 8-token (MN-major) groups 1024 bytes apart, 64-wide
+// panels a whole tile apart (used by the MN-major operand only).
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)(AP_TILE * 128 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// byte offset of 16-byte piece c (of D / 8) of row `row` in a tile of D / 64 panels
+__device__ __forceinline__ uint32_t swizzled(int row, int c)
+{
+    return (uint32_t)((c >> 3) * (AP_TILE * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// barrier of the 128 producers that tells all of them whether all said yes
+__device__ __forceinline__ bool producers_agree(bool yes)
+{
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+                 : "=r"(r) : "r"((uint32_t)yes) : "memory");
+    return r != 0;
+}
+
+// entries of the ascending ids [base, base + len) that are <= p, found by a warp: 32 probes a round
+__device__ inline int ids_up_to_warp(const VtkAttnArgs &a, int64_t base, int len, int64_t p)
+{
+    if (p < 0) return 0;
+    if (a.cache_ids.null()) return p + 1 < len ? (int)(p + 1) : len;
+    int lo = 0, hi = len;                // ids below lo are <= p, ids from hi on are > p
+    while (lo < hi) {
+        const int step = (hi - lo + 31) / 32, probe = lo + vtk_lane() * step;
+        const bool le = probe < hi && a.cache_ids[base + probe] <= p;
+        const int n = __popc(__ballot_sync(0xffffffffu, le));
+        const int next_hi = lo + n * step;
+        if (n > 0) lo = lo + (n - 1) * step + 1;
+        if (next_hi < hi) hi = next_hi < lo ? lo : next_hi;
+    }
+    return lo;
+}
+
+// The scheduler's work: ticket -> item.  Items of a request run from its last rows (the longest under a causal
+// mask) to its first; all key heads of a pair of tiles follow one another.
+template <int D>
+__device__ void next_item(const VtkAttnArgs &a, Shared<D> &sh, Item &out, int R, int seg, uint32_t *tickets, int row_limit)
+{
+    const int lane = vtk_lane();
+    int idx = 0;
+    if (lane == 0) idx = (int)atomicAdd(tickets, 1u);
+    idx = __shfl_sync(0xffffffffu, idx, 0);
+    Item it;
+    it.none = 1;
+    if (idx / a.hkv < sh.prefix[AP_NT]) {
+        it.none = 0;
+        it.kv = idx % a.hkv;
+        const int pair = idx / a.hkv;
+        int lo = 0, hi = AP_NT;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (sh.prefix[mid] <= pair) lo = mid; else hi = mid;
+        }
+        int left = pair - sh.prefix[lo], r = lo * seg, qn, pairs;
+        int64_t base;
+        bool clipped;
+        for (;; ++r) {
+            vtk_request_rows(a, r, it.q0, qn, base, it.len, clipped);
+            pairs = qn * a.group > row_limit ? (qn * a.group + 2 * AP_TILE - 1) / (2 * AP_TILE) : 0;
+            if (left < pairs) break;
+            left -= pairs;
+        }
+        it.first = (pairs - 1 - left) * 2 * AP_TILE;
+        it.rows = qn * a.group - it.first < 2 * AP_TILE ? qn * a.group - it.first : 2 * AP_TILE;
+        int pmin = INT32_MAX, pmax = -1;
+        for (int x = 0; x < 2; ++x) {
+            int lo_p = INT32_MAX, hi_p = -1;
+            const int r0 = it.first + x * AP_TILE, r1 = it.first + (it.rows < (x + 1) * AP_TILE ? it.rows : (x + 1) * AP_TILE);
+            if (r0 < r1)
+                for (int t = r0 / a.group + lane; t <= (r1 - 1) / a.group; t += 32) {
+                    const int p = a.positions[it.q0 + t];
+                    lo_p = p < lo_p ? p : lo_p;
+                    hi_p = p > hi_p ? p : hi_p;
+                }
+            it.pmin[x] = __reduce_min_sync(0xffffffffu, lo_p);
+            it.pmax[x] = __reduce_max_sync(0xffffffffu, hi_p);
+            pmin = it.pmin[x] < pmin ? it.pmin[x] : pmin;
+            pmax = it.pmax[x] > pmax ? it.pmax[x] : pmax;
+        }
+        it.span.q0 = it.q0;
+        it.span.qn = qn;
+        it.span.base = base;
+        const int end = ids_up_to_warp(a, base, it.len, pmax);
+        it.span.lo = a.window > 0 ? ids_up_to_warp(a, base, it.len, (int64_t)pmin - a.window) : 0;
+        if (it.span.lo > end) it.span.lo = end;
+        it.span.n_sink = a.sinks > 0 ? ids_up_to_warp(a, base, it.span.lo, (int64_t)a.sinks - 1) : 0;
+        it.span.n = it.span.n_sink + end - it.span.lo;
+        it.tiles = (it.span.n + AP_TILE - 1) / AP_TILE;
+    }
+    if (lane == 0) out = it;
+}
+
+// 4-bit codes of 8 values (one word) times their group's scale, as halves
+__device__ __forceinline__ uint4 expand8(uint32_t w, uint32_t s)
+{
+    return make_uint4(vtk_hmul2(vtk_codes_to_half2(w), s), vtk_hmul2(vtk_codes_to_half2(w >> 8), s),
+                      vtk_hmul2(vtk_codes_to_half2(w >> 16), s), vtk_hmul2(vtk_codes_to_half2(w >> 24), s));
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint4 w)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+}
+
+template <int D, bool FP4, typename Act>
+__global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid_constant__ VtkAttnArgs a, uint32_t *tickets, int row_limit,
+                                                                    uint64_t limit_ns, float scale, int negate)
+{
+    using Mma = typename std::conditional<FP4, VtkFp16, Act>::type;
+    constexpr int PANEL = AP_TILE * 128, PIECES = D / 8;
+    extern __shared__ uint8_t raw[];
+    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+    vtk_release_successor();
+    vtk_wait_for_predecessor();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    // ---- once per CTA: barriers, tensor memory, pairs of tiles per request ----
+    if (tid == 0) {
+        for (int i = 0; i < AP_STAGES; ++i) { mbar_init(&sh.kv_full[i], 128); mbar_init(&sh.kv_empty[i], 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(&sh.s_full[x], 1); mbar_init(&sh.p_full[x], 128); mbar_init(&sh.o_full[x], 1); }
+        mbar_init(&sh.q_full, 128);
+        mbar_init(&sh.drain, 1);
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    int R = *a.num_requests;
+    bool clipped = R < 0 || R > a.max_requests;
+    R = R < 0 ? 0 : (R > a.max_requests ? a.max_requests : R);
+    const int seg = (R + AP_NT - 1) / AP_NT;
+    int pairs = 0;
+    for (int r = tid * seg; r < (tid + 1) * seg && r < R; ++r) {
+        int q0, qn, len;
+        int64_t base;
+        bool c;
+        vtk_request_rows(a, r, q0, qn, base, len, c);
+        clipped |= c;
+        if (qn * a.group > row_limit) pairs += (qn * a.group + 2 * AP_TILE - 1) / (2 * AP_TILE);
+    }
+    if (clipped && blockIdx.x == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
+    const int incl = vtk_warp_incl_scan(pairs);
+    if (lane == 31) sh.warp_sum[warp] = incl;
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    int before = 0;
+    for (int w = 0; w < warp; ++w) before += sh.warp_sum[w];
+    sh.prefix[tid + 1] = before + incl;
+    if (tid == 0) sh.prefix[0] = 0;
+    __syncthreads();
+    const uint32_t tmem = sh.tmem;
+    if (warp == 13) next_item<D>(a, sh, sh.item[0], R, seg, tickets, row_limit);
+
+    // running counts of the rings and barriers
+    uint32_t kv_count = 0;               // K and V tiles loaded (producers) or used (mma)
+    uint32_t s_count[2] = {0, 0}, item_count = 0, tile_count = 0, q_count = 0, o_count[2] = {0, 0};
+    constexpr uint32_t IDESC = (1u << 4) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 7) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 10) |
+                               ((uint32_t)(AP_TILE >> 4) << 24);
+    const uint32_t idesc_s = IDESC | ((uint32_t)(AP_TILE >> 3) << 17) | ((uint32_t)negate << 13);
+    constexpr uint32_t idesc_o = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);
+
+    for (;; ++item_count) {
+        __syncthreads();
+        const Item &it = sh.item[item_count & 1];
+        if (it.none || *(volatile int *)&sh.abort) break;
+        const int T = it.tiles;
+        const bool two = it.rows > AP_TILE;
+
+        if (warp < 8) {
+            // ================= softmax: thread = row =================
+            const int x = warp >> 2, row = tid & 127;
+            const uint32_t lanes = (uint32_t)(warp & 3) << 21;                   // 32 lanes a warp
+            const uint32_t t_s = tmem + lanes + x * AP_TILE, t_o = tmem + lanes + 2 * AP_TILE + x * D;
+            const bool have = x * AP_TILE + row < it.rows;
+            const int at = it.first + x * AP_TILE + row;
+            const int64_t tok = it.q0 + (have ? at / a.group : 0);
+            const int head = it.kv * a.group + (have ? at % a.group : 0);
+            const int pos = have ? a.positions[tok] : -1;
+            float m = -INFINITY, l = 0.f, c = scale;
+            bool ok = true;
+            if (x == 0 || two) {
+                if (FP4 && T > 0) {                                              // row scales come with the queries
+                    ok = __all_sync(0xffffffffu, mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort));
+                    c = scale * sh.row_scale[x][row];
+                }
+                for (int j = 0; j < T && ok; ++j) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort));
+                    if (!ok) break;
+                    tc_after_sync();
+                    const Meta &mt = sh.meta[(tile_count + j) % AP_META];
+                    uint32_t s[32];
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        tc_ld32(t_s + 32 * q, s);
+                        tc_wait_ld();
+                        const uint32_t every = mt.every[x][q];
+                        if (every == 0xffffffffu) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (vtk_sees(mt.ids[32 * q + i], pos, a.window, a.sinks)) top = fmaxf(top, __uint_as_float(s[i]));
+                        }
+                    }
+                    const bool up = (top - m) * c > 8.f || (m == -INFINITY && top > -INFINITY);
+                    if (__any_sync(0xffffffffu, up)) {
+                        const float next = fmaxf(m, top);
+                        const float f = m == -INFINITY ? 0.f : vtk_exp2((m - next) * c);
+                        m = next;
+                        l *= f;
+                        if (j > 0) {                                             // the products up to j - 1 are complete: S j came after them
+#pragma unroll
+                            for (int q = 0; q < D / 32; ++q) {
+                                tc_ld32(t_o + 32 * q, s);
+                                tc_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * f);
+                                tc_st32(t_o + 32 * q, s);
+                            }
+                            tc_wait_st();
+                        }
+                    }
+                    const float mc = m == -INFINITY ? 0.f : m * c;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        tc_ld32(t_s + 32 * q, s);
+                        tc_wait_ld();
+                        const uint32_t every = mt.every[x][q];
+                        if (every != 0xffffffffu) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!vtk_sees(mt.ids[32 * q + i], pos, a.window, a.sinks)) s[i] = 0xff800000u;
+                        }
+                        uint32_t p[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float p0 = vtk_exp2(fmaf(__uint_as_float(s[2 * i]), c, -mc)), p1 = vtk_exp2(fmaf(__uint_as_float(s[2 * i + 1]), c, -mc));
+                            sum += p0 + p1;
+                            p[i] = Mma::pack(p0, p1);
+                        }
+                        tc_st16(t_s + 16 * q, p);
+                    }
+                    l += sum;
+                    tc_wait_st();
+                    tc_before_sync();
+                    mbar_arrive(&sh.p_full[x]);
+                }
+                if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort));
+                if (ok) {
+                    if (T > 0) tc_after_sync();
+                    const float r = l == 0.f ? 0.f : a.v_mul / l;
+                    bool bad = !(fabsf(l) < INFINITY);
+                    uint16_t *dst = a.out + tok * a.out_stride + (int64_t)head * D;
+#pragma unroll
+                    for (int q = 0; q < D / 32; ++q) {
+                        uint32_t o[32];
+                        if (T > 0) {
+                            tc_ld32(t_o + 32 * q, o);
+                            tc_wait_ld();
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float y = T > 0 && l != 0.f ? __uint_as_float(o[i]) * r : 0.f;
+                            bad |= T > 0 && !(fabsf(__uint_as_float(o[i])) < INFINITY);
+                            o[i] = __float_as_uint(y);
+                        }
+                        if (have) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint4 w;
+                                w.x = Act::pack(__uint_as_float(o[8 * i]), __uint_as_float(o[8 * i + 1]));
+                                w.y = Act::pack(__uint_as_float(o[8 * i + 2]), __uint_as_float(o[8 * i + 3]));
+                                w.z = Act::pack(__uint_as_float(o[8 * i + 4]), __uint_as_float(o[8 * i + 5]));
+                                w.w = Act::pack(__uint_as_float(o[8 * i + 6]), __uint_as_float(o[8 * i + 7]));
+                                *reinterpret_cast<uint4 *>(dst + 32 * q + 8 * i) = w;
+                            }
+                        }
+                    }
+                    if (have && a.lse != nullptr)
+                        a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * 0.69314718055994531f;
+                    // rows that a masked NaN may have reached: token by token
+                    unsigned again = __ballot_sync(0xffffffffu, have && bad);
+                    while (again) {
+                        const int src = __ffs(again) - 1;
+                        again &= again - 1;
+                        const int64_t q_row = __shfl_sync(0xffffffffu, (int)tok, src);
+                        const int h2 = __shfl_sync(0xffffffffu, head, src), p2 = __shfl_sync(0xffffffffu, pos, src);
+                        float acc[D / 32], m2, l2;
+                        vtk_row_again<D, FP4, Act>(a, q_row, h2, p2, it.span.base, it.len, acc, m2, l2);
+                        vtk_store_row<D, Act>(a, q_row, h2, acc, m2, l2);
+                    }
+                    tc_before_sync();
+                }
+            }
+        } else if (warp < 12) {
+            // ================= producers =================
+            if (T > 0) {
+                const int pt = tid - 256;
+                // queries, rows of both tiles
+                if (!FP4) {
+                    const int rows = two ? 2 * AP_TILE : AP_TILE;
+                    for (int i = pt; i < rows * PIECES; i += 128) {
+                        const int row = i / PIECES, piece = i % PIECES, at = it.first + row;
+                        const bool there = row < it.rows;
+                        const uint16_t *src = a.q;
+                        if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D + 8 * piece;
+                        cp_async16(smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
+                    }
+                    cp_commit();
+                } else {
+                    for (int x = 0; x < (two ? 2 : 1); ++x) {
+                        const int row = x * AP_TILE + pt, at = it.first + row;
+                        const bool there = row < it.rows;
+                        const uint16_t *src = a.q;
+                        if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
+                        float up = 1.f, down = 1.f;
+                        if (Act::kind == VTOKEN_KV_BF16) {           // bf16 queries in half precision: see attention.cu
+                            float top = 0.f, v[8];
+                            for (int i = 0; i < PIECES; ++i) {
+                                vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0), v);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+                            }
+                            int e2 = (int)(__float_as_uint(top) >> 23) - 127;
+                            e2 = 14 - (e2 > 100 ? 100 : (e2 < -100 ? -100 : e2));
+                            up = __uint_as_float((uint32_t)(127 + e2) << 23);
+                            down = __uint_as_float((uint32_t)(127 - e2) << 23);
+                        }
+                        sh.row_scale[x][pt] = down;
+                        for (int i = 0; i < PIECES; ++i) {
+                            uint4 w = there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+                            if (Act::kind == VTOKEN_KV_BF16) {
+                                float v[8];
+                                vtk_unpack8<VtkBf16>(w, v);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[e] *= up;
+                                w = vtk_pack8<VtkFp16>(v);
+                            }
+                            st_shared16(smem_u32(sh.q[x]) + swizzled(pt, i), w);
+                        }
+                    }
+                    async_proxy_fence();
+                    mbar_arrive(&sh.q_full);
+                }
+                const int pmin = two && it.pmin[1] < it.pmin[0] ? it.pmin[1] : it.pmin[0];
+                const int pmax = two && it.pmax[1] > it.pmax[0] ? it.pmax[1] : it.pmax[0];
+                int64_t slot = -1;
+                int id = INT32_MAX;
+                auto fetch = [&](int j) {                          // this thread's token of tile j
+                    const int v = j * AP_TILE + pt;
+                    slot = -1;
+                    id = INT32_MAX;
+                    if (v < it.span.n) {
+                        slot = a.cache_slots[it.span.entry(v)];
+                        id = a.cache_ids.null() ? it.span.index(v) : a.cache_ids[it.span.entry(v)];
+                    }
+                };
+                fetch(0);
+                int owed = -1, q_owed = !FP4;                      // 16-bit: a stage (the queries) whose copies are in flight
+                auto deliver = [&](int stage) { async_proxy_fence(); mbar_arrive(&sh.kv_full[stage]); };
+                for (int j = 0; j < T; ++j) {
+                    if (slot >= a.slots_per_layer) {
+                        atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
+                        slot = -1;
+                    }
+                    if (slot < 0) id = INT32_MAX;
+                    Meta &mt = sh.meta[(tile_count + j) % AP_META];
+                    const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
+                    bool ok = mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                    // (K two tiles ago is consumed, so both softmaxes are past the tile whose meta this overwrites)
+                    const bool any = id <= pmax && (a.window == 0 || id > (int64_t)pmin - a.window || id < a.sinks);
+                    mt.ids[pt] = id;
+                    sh.slots[j & 1][pt] = any ? (int)slot : -1;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const bool every = id <= it.pmin[x] && (a.window == 0 || id > (int64_t)it.pmax[x] - a.window || id < a.sinks);
+                        const unsigned bits = __ballot_sync(0xffffffffu, every);
+                        if (lane == 0) mt.every[x][warp - 8] = bits;
+                    }
+                    ok = producers_agree(ok);
+                    if (!ok) break;
+                    if (j + 1 < T) fetch(j + 1);
+#pragma unroll 1
+                    for (int which = 0; which < 2; ++which) {
+                        const uint32_t stage = which ? stage_v : stage_k;
+                        if (which) {
+                            ok = mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                            ok = producers_agree(ok);
+                            if (!ok) break;
+                        }
+                        const uint8_t *rows = which ? a.v_rows : a.k_rows;
+                        const uint32_t dst = smem_u32(sh.kv[stage]);
+                        if (!FP4) {
+                            const int piece = pt % PIECES;
+#pragma unroll 4
+                            for (int row = pt / PIECES; row < AP_TILE; row += 128 / PIECES) {
+                                const int64_t s = sh.slots[j & 1][row];
+                                const uint8_t *src = rows + (s < 0 ? 0 : s) * a.row_bytes + ((int64_t)it.kv * D + 8 * piece) * 2;
+                                cp_async16(dst + swizzled(row, piece), src, s >= 0);
+                            }
+                            cp_commit();
+                            cp_wait<1>();
+                            if (q_owed) { async_proxy_fence(); mbar_arrive(&sh.q_full); q_owed = 0; }
+                            if (owed >= 0) deliver(owed);
+                            owed = (int)stage;
+                        } else {
+                            // four threads a token: a quarter of its codes and scales each
+                            constexpr int QW = D / 32;                   // words of 8 codes a thread
+                            const int part = pt & 3;
+#pragma unroll 2
+                            for (int row = pt >> 2; row < AP_TILE; row += 32) {
+                                const int64_t s = sh.slots[j & 1][row];
+                                uint32_t w[QW], sc = 0;
+#pragma unroll
+                                for (int i = 0; i < QW; ++i) w[i] = 0;
+                                if (s >= 0) {
+                                    const uint8_t *src = rows + s * a.row_bytes;
+                                    const uint8_t *codes = src + it.kv * (D / 2) + part * (D / 8);
+                                    const uint8_t *scales = src + a.hkv * (D / 2) + it.kv * (D / 16) + part * (D / 64);
+                                    if (D == 128) {
+                                        const uint4 q4 = vtk_ldg16(codes);
+                                        w[0] = q4.x; w[1] = q4.y; w[QW - 2] = q4.z; w[QW - 1] = q4.w;
+                                        sc = __ldg(reinterpret_cast<const uint16_t *>(scales));
+                                    } else {
+                                        const uint2 q2 = __ldg(reinterpret_cast<const uint2 *>(codes));
+                                        w[0] = q2.x; w[1] = q2.y;
+                                        sc = __ldg(scales);
+                                    }
+                                }
+                                const uint32_t two_scales = vtk_scales_to_half2(sc);
+#pragma unroll
+                                for (int i = 0; i < QW; ++i)
+                                    st_shared16(dst + swizzled(row, part * QW + i), expand8(w[i], __byte_perm(two_scales, 0, i < 2 ? 0x1010 : 0x3232)));
+                            }
+                            deliver((int)stage);
+                        }
+                    }
+                    if (!ok) break;
+                }
+                if (!FP4) {
+                    cp_wait<0>();
+                    if (q_owed) { async_proxy_fence(); mbar_arrive(&sh.q_full); }
+                    if (owed >= 0) deliver(owed);
+                }
+            }
+        } else if (warp == 12) {
+            // ================= products: one thread =================
+            if (lane == 0 && T > 0) {
+                bool ok = mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort);
+                auto wait_tile = [&](uint32_t cc) {
+                    return mbar_wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1, limit_ns, &sh.abort);
+                };
+                auto scores = [&](int x, uint32_t cc) {
+                    const uint32_t qa = smem_u32(sh.q[x]), ka = smem_u32(sh.kv[cc % AP_STAGES]);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = (k / 4) * PANEL + (k % 4) * 32;
+                        tc_mma_ss(tmem + x * AP_TILE, operand(qa + off), operand(ka + off), idesc_s, k > 0);
+                    }
+                    tc_commit(&sh.s_full[x]);
+                };
+                auto outputs = [&](int x, uint32_t cc, bool first) {
+                    const uint32_t va = smem_u32(sh.kv[cc % AP_STAGES]);
+#pragma unroll
+                    for (int k = 0; k < AP_TILE / 16; ++k)
+                        tc_mma_ts(tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + 8 * k, operand(va + k * 16 * 128), idesc_o, !first || k > 0);
+                };
+                ok = ok && wait_tile(kv_count);
+                if (ok) {
+                    tc_after_sync();
+                    scores(0, kv_count);
+                    if (two) scores(1, kv_count);
+                    tc_commit(&sh.kv_empty[kv_count % AP_STAGES]);
+                }
+                for (int j = 0; j < T && ok; ++j) {
+                    const uint32_t ck = kv_count + 2 * j, cv = ck + 1;
+                    for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
+                        ok = mbar_wait(&sh.p_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort);
+                        if (ok && x == 0) ok = wait_tile(cv);
+                        if (!ok) break;
+                        tc_after_sync();
+                        outputs(x, cv, j == 0);
+                        const bool last_x = x == 1 || !two;
+                        if (last_x) tc_commit(&sh.kv_empty[cv % AP_STAGES]);
+                        if (j + 1 < T) {
+                            if (x == 0) ok = wait_tile(ck + 2);
+                            if (!ok) break;
+                            tc_after_sync();
+                            scores(x, ck + 2);
+                            if (last_x) tc_commit(&sh.kv_empty[(ck + 2) % AP_STAGES]);
+                        } else {
+                            tc_commit(&sh.o_full[x]);
+                        }
+                    }
+                }
+                if (!ok) {                                           // what was issued ends before the tensor memory goes
+                    tc_commit(&sh.drain);
+                    const uint64_t t0 = global_ns();
+                    while (!mbar_try(&sh.drain, 0) && global_ns() - t0 < limit_ns) {}
+                }
+            }
+            __syncwarp();
+        } else if (warp == 13) {
+            next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
+        }
+        kv_count += 2 * T;
+        tile_count += T;
+        s_count[0] += T;                                             // the second tile's barriers move only when there is one
+        s_count[1] += two ? T : 0;
+        if (T > 0) { ++q_count; ++o_count[0]; o_count[1] += two; }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        if (sh.abort) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_TIMEOUT);
+        __threadfence();
+        if (atomicAdd(tickets + 1, 1u) == gridDim.x - 1) { tickets[0] = 0; tickets[1] = 0; }
+    }
+    if (warp == 12) {
+        tc_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+template <int D, bool FP4, typename Act>
+int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st)
+{
+    constexpr int smem = (int)sizeof(Shared<D>) + 1024;
+    static_assert(smem <= 232448, "shared memory of a CTA");
+    auto kernel = attention_prompt_kernel<D, FP4, Act>;
+    VTK_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    // the sign of the scores' factor goes into the product (a zero factor: one that no 32-bit score can be seen through)
+    const float scale = a.scale_log2 == 0.f ? 7.9e-31f : (a.scale_log2 < 0.f ? -a.scale_log2 : a.scale_log2);
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(ctx->num_sms), dim3(AP_NT), smem, st, a, tickets, a.row_limit,
+                                       (uint64_t)ctx->wait_limit_ns, scale, (int)(a.scale_log2 < 0.f)));
+    VTK_CUDA(ctx, cudaGetLastError());
+    return VTOKEN_OK;
+}
+
+template <int D>
+int launch_by_type(vtoken_ctx *ctx, const vtoken_heads *h, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st)
+{
+    if (h->kv_type == VTOKEN_KV_FP4)
+        return h->act_type == VTOKEN_KV_BF16 ? launch<D, true, VtkBf16>(ctx, a, tickets, st) : launch<D, true, VtkFp16>(ctx, a, tickets, st);
+    return h->act_type == VTOKEN_KV_BF16 ? launch<D, false, VtkBf16>(ctx, a, tickets, st) : launch<D, false, VtkFp16>(ctx, a, tickets, st);
+}
+
+}  // namespace
+
+int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st)
+{
+    return heads->head_dim == 128 ? launch_by_type<128>(ctx, heads, a, tickets, st) : launch_by_type<64>(ctx, heads, a, tickets, st);
+}

@@ -1,234 +1,412 @@
 // Attention of few query rows per request (a decode step) over the slot cache.
 //
-// Bound by HBM: every visible K and V row is read once, 4 * D flops per row, head and query.  The work is cut
-// along the cache: an item is (request, tile of query rows, key head, chunk of the cache); one CTA takes an item,
-// its warps the chunk's 16-token tiles in turn, with a running maximum and sum per query row and the output
-// accumulators in registers.  A request of one chunk is finished by its CTA; of a longer one every CTA leaves a
-// partial row and the last to arrive joins them in chunk order, so the order of the sums is that of the tables.
+// Bound by HBM: every visible K and V row is read once, 4 * D flops per row, head and query.
 //
-// The heads of a group (and the query tokens of a request) are the rows of one matrix product, so a K or V row is
-// read once for all of them.  Both products take their operand from the cache straight from global memory into the
-// registers where mma.m16n8k16 wants it, without a pass through shared memory: the order of the contracted
-// dimension is free as long as both operands agree, so
-//   S = Q K^T : a lane's 16-byte load of K (8 dimensions of one token) is the B fragment of two instructions;
-//   O^T = V^T P^T : a lane loads 16 bytes (8 dimensions) of four tokens, byte permutes pair the tokens up to the
-//   A fragment, and the accumulator layout of S (rows = queries, columns = tokens) is the B fragment of P^T as it is.
+// The cut.  A segment is (request, tile of query rows, key head); its cache is numbered in tiles of 16 tokens (32 of
+// the 4-bit cache), and
+// all tiles of all segments in one row.  Teams of warps take equal shares of that row -- so every SM reads the same
+// number of bytes whatever the lengths -- and every CTA (one per SM) works them out for itself from the tables.  A
+// team is one warp when there are segments enough, the CTA's warps when there are few.  Its warps take the tiles of a
+// segment in turn, each with a running maximum and sum per query row and the output accumulators in registers, and
+// join in shared memory at the segment's end.  A segment that lies inside one share is finished there; at most the
+// first and the last segment of a share are parts of longer ones: they leave a partial row, and the last team to
+// arrive joins the parts in the order of the tables, so the sums do not depend on who came when.
+//
+// The stream.  Each warp copies its tiles (K and V rows of one head, gathered by slot) with cp.async into a ring of
+// its own, several tiles ahead and across the ends of segments, so that about 100 KB per SM are in flight through
+// joins, query loads and masks.  Pieces of 16 bytes are permuted within a row so that the reads below are free of
+// bank conflicts.
+//
+// The products.  The heads of a group (and the query tokens of a request) are the rows of one matrix product, so a
+// K or V row is read once for all of them.  The order of the contracted dimension is free as long as both operands
+// agree, so mma.m16n8k16 gets its fragments with 16-byte loads:
+//   S = Q K^T : 8 dimensions of one token are the B fragment of two instructions;
+//   O^T = V^T P^T : 8 dimensions of four tokens, paired up to the A fragment by byte permutes; the accumulator layout
+//   of S (rows = queries, columns = tokens) is the B fragment of P^T as it is.
 // P is handed to the second product as the sum of two 16-bit values, so that its rounding does not add to that of
 // the 16-bit output; over the 4-bit cache the products run in half precision, whose 11 bits are enough next to a
 // bf16 output.  These legacy matrix instructions are enough here: 8 or 16 rows leave a 128-row tcgen05 tile mostly
-// empty, and at full HBM rate the products need well under a tenth of the tensor rate.
+// empty, and at full HBM rate the products need well under a third of the legacy tensor rate.
 #include "attention.cuh"
 
 namespace {
 
-constexpr int AT_WARPS = 4, AT_NT = AT_WARPS * 32;
-// CTAs per SM: what 168 (8 query rows) and 255 registers a thread leave room for
-template <int NR> constexpr int AT_CTAS = NR == 8 ? 3 : 2;
-// requests whose spans a CTA keeps in shared memory (below the 48 KB of static arrays)
-constexpr int AT_ROW_LIMIT = 32;          // query rows (tokens times group) of a request up to which it is worked on here
-template <int NR> constexpr int AT_KNOWN = NR == 8 ? 512 : 256;
+constexpr int AT_ROW_LIMIT = 32;         // query rows (tokens times group) of a request up to which it is worked on here
+constexpr int AT_KNOWN = 8;              // requests of a share that are looked up together at the start
+constexpr int AT_MIN_SHARE = 2;          // tiles of the smallest share, for each warp of its team
+constexpr int AT_PARTS = 3;              // shares that a segment of mean length is cut into at most, about
 
-// ---- 16 tokens of one head in registers --------------------------------------------------------
-// K: lane (g, t) holds of tokens g and 8 + g the dimensions `kdim(j) .. + 7`, j < D / 32.
-// V: lane (g, t) holds of tokens 2t, 2t + 1, 2t + 8, 2t + 9 the dimensions `vdim(x) .. + 7`, x < D / 64.
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+template <int BYTES>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool there)
+{
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// ---- a tile of tokens of one head in a warp's ring ---------------------------------------------
+// K fragments of 16 tokens: lane (g, t) takes of tokens g and 8 + g the dimensions kdim(t, j) .. + 7, j < D / 32.
+// V fragments: lane (g, t) takes of tokens 2t, 2t + 1, 2t + 8, 2t + 9 the dimensions vdim(g, x) .. + 7, x < D / 64.
 template <int D, typename Act>
 struct Rows16 {
     static constexpr bool FP4 = false;
     using Mma = Act;
-    uint4 k[2][D / 32], v[4][D / 64];
+    static constexpr int WARPS = 8, TILE = 16, PITCH = D * 2, HALF = TILE * PITCH, STAGE = 2 * HALF, PIECES = D / 8;
     static __device__ __forceinline__ int kdim(int t, int j) { return 32 * j + 8 * t; }
     static __device__ __forceinline__ int vdim(int g, int x) { return 64 * x + 8 * g; }
-    __device__ __forceinline__ void load_k(int u, bool there, const uint8_t *row, int, int head, int t)
+    // slot: lane i < TILE holds that of token i, negative = zeros
+    static __device__ __forceinline__ void issue(uint32_t dst, const uint8_t *k_rows, const uint8_t *v_rows, int64_t row_bytes, int, int head, int slot)
+    {
+        const int lane = vtk_lane(), c = lane % PIECES, sub = lane / PIECES;
+        constexpr int PER = 32 / PIECES;
+        const int64_t off0 = (int64_t)head * (D * 2) + 16 * c;
+#pragma unroll
+        for (int i = 0; i < TILE / PER; ++i) {
+            const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
+            const int64_t off = (s < 0 ? 0 : s) * row_bytes + off0;
+            cp_async<16>(dst + tok * PITCH + ((c ^ ((tok & 1) << 2)) << 4), k_rows + off, s >= 0);
+            cp_async<16>(dst + HALF + tok * PITCH + ((c ^ (((tok >> 1) & 3) << 1)) << 4), v_rows + off, s >= 0);
+        }
+    }
+    const uint8_t *at;
+    __device__ __forceinline__ void get_k(int b, int u, int g, int t, uint4 (&k)[D / 32]) const
     {
 #pragma unroll
         for (int j = 0; j < D / 32; ++j)
-            k[u][j] = there ? vtk_ldg16(row + ((int64_t)head * D + kdim(t, j)) * 2) : make_uint4(0, 0, 0, 0);
+            k[j] = *reinterpret_cast<const uint4 *>(at + (16 * b + 8 * u + g) * PITCH + (((4 * j + t) ^ ((g & 1) << 2)) << 4));
     }
-    __device__ __forceinline__ void load_v(int i, bool there, const uint8_t *row, int, int head, int g)
+    // of token 16 b + 2t + (i & 1) + 8 (i >> 1)
+    __device__ __forceinline__ void get_v(int b, int i, int g, int t, uint4 (&v)[D / 64]) const
     {
 #pragma unroll
         for (int x = 0; x < D / 64; ++x)
-            v[i][x] = there ? vtk_ldg16(row + ((int64_t)head * D + vdim(g, x)) * 2) : make_uint4(0, 0, 0, 0);
+            v[x] = *reinterpret_cast<const uint4 *>(at + HALF + (16 * b + 2 * t + (i & 1) + 8 * (i >> 1)) * PITCH + (((8 * x + g) ^ (t << 1)) << 4));
     }
-    __device__ __forceinline__ uint4 get_k(int u, int j) const { return k[u][j]; }
-    __device__ __forceinline__ uint4 get_v(int i, int x) const { return v[i][x]; }
 };
 
-template <int D>
+template <int D, int W>
 struct Rows4 {
     static constexpr bool FP4 = true;
     using Mma = VtkFp16;
-    uint32_t k[2][D / 32], v[4][D / 64], ks[2], vs[4];
+    static constexpr int WARPS = W, TILE = 32, PITCH = D / 2, HALF = TILE * PITCH, SCALES = D / 16, PIECES = D / 32;
+    static constexpr int STAGE = 2 * HALF + 2 * TILE * SCALES;
     static __device__ __forceinline__ int kdim(int t, int j) { return (D / 4) * t + 8 * j; }
     static __device__ __forceinline__ int vdim(int g, int x) { return (D / 8) * g + 8 * x; }
-    __device__ __forceinline__ void load_k(int u, bool there, const uint8_t *row, int hkv, int head, int t)
+    static __device__ __forceinline__ int vswizzle(int tok, int c) { return D == 128 ? c ^ ((tok >> 1) & 3) : c; }
+    static __device__ __forceinline__ void issue(uint32_t dst, const uint8_t *k_rows, const uint8_t *v_rows, int64_t row_bytes, int hkv, int head, int slot)
     {
-        const uint8_t *codes = row + head * (D / 2) + (D / 8) * t;
-        const uint8_t *scales = row + hkv * (D / 2) + head * (D / 16) + (D / 64) * t;
-        if (D == 128) {
-            const uint4 w = there ? vtk_ldg16(codes) : make_uint4(0, 0, 0, 0);
-            k[u][0] = w.x; k[u][1] = w.y; k[u][D / 32 - 2] = w.z; k[u][D / 32 - 1] = w.w;
-            ks[u] = there ? __ldg(reinterpret_cast<const uint16_t *>(scales)) : 0;
+        const int lane = vtk_lane(), c = lane % PIECES, sub = lane / PIECES;
+        constexpr int PER = 32 / PIECES;
+#pragma unroll
+        for (int i = 0; i < TILE / PER; ++i) {
+            const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
+            const int64_t off = (s < 0 ? 0 : s) * row_bytes + head * PITCH + 16 * c;
+            cp_async<16>(dst + tok * PITCH + 16 * c, k_rows + off, s >= 0);
+            cp_async<16>(dst + HALF + tok * PITCH + 16 * vswizzle(tok, c), v_rows + off, s >= 0);
+        }
+        const int64_t off = (slot < 0 ? 0 : slot) * row_bytes + hkv * PITCH + head * SCALES;
+        cp_async<SCALES>(dst + 2 * HALF + lane * SCALES, k_rows + off, slot >= 0);
+        cp_async<SCALES>(dst + 2 * HALF + (TILE + lane) * SCALES, v_rows + off, slot >= 0);
+    }
+    const uint8_t *at;
+    __device__ __forceinline__ void get_k(int b, int u, int g, int t, uint4 (&k)[D / 32]) const
+    {
+        const uint8_t *codes = at + (16 * b + 8 * u + g) * PITCH + t * (D / 8), *sc = at + 2 * HALF + (16 * b + 8 * u + g) * SCALES;
+        if (D == 128) {                  // words 0, 1 belong to the first of the lane's two groups, 2, 3 to the second
+            const uint4 w = *reinterpret_cast<const uint4 *>(codes);
+            const uint32_t two = vtk_scales_to_half2(*reinterpret_cast<const uint16_t *>(sc + 2 * t));
+            const uint32_t s0 = __byte_perm(two, 0, 0x1010), s1 = __byte_perm(two, 0, 0x3232);
+            k[0] = vtk_expand8(w.x, s0);
+            k[1] = vtk_expand8(w.y, s0);
+            k[D / 32 - 2] = vtk_expand8(w.z, s1);
+            k[D / 32 - 1] = vtk_expand8(w.w, s1);
         } else {
-            const uint2 w = there ? __ldg(reinterpret_cast<const uint2 *>(codes)) : make_uint2(0, 0);
-            k[u][0] = w.x; k[u][1] = w.y;
-            ks[u] = there ? __ldg(scales) : 0;
+            const uint2 w = *reinterpret_cast<const uint2 *>(codes);
+            const uint32_t s0 = __byte_perm(vtk_scales_to_half2(sc[t]), 0, 0x1010);
+            k[0] = vtk_expand8(w.x, s0);
+            k[1] = vtk_expand8(w.y, s0);
         }
     }
-    __device__ __forceinline__ void load_v(int i, bool there, const uint8_t *row, int hkv, int head, int g)
+    __device__ __forceinline__ void get_v(int b, int i, int g, int t, uint4 (&v)[D / 64]) const
     {
-        const uint8_t *codes = row + head * (D / 2) + (D / 16) * g;
-        const uint8_t *scales = row + hkv * (D / 2) + head * (D / 16);
+        const int tok = 16 * b + 2 * t + (i & 1) + 8 * (i >> 1);
+        const uint32_t s0 = __byte_perm(vtk_scales_to_half2(at[2 * HALF + (TILE + tok) * SCALES + (D == 128 ? g : g >> 1)]), 0, 0x1010);
+        const uint8_t *codes = at + HALF + tok * PITCH;
         if (D == 128) {
-            const uint2 w = there ? __ldg(reinterpret_cast<const uint2 *>(codes)) : make_uint2(0, 0);
-            v[i][0] = w.x; v[i][D / 64 - 1] = w.y;
-            vs[i] = there ? __ldg(scales + g) : 0;
+            const uint2 w = *reinterpret_cast<const uint2 *>(codes + 16 * vswizzle(tok, g >> 1) + 8 * (g & 1));
+            v[0] = vtk_expand8(w.x, s0);
+            v[D / 64 - 1] = vtk_expand8(w.y, s0);
         } else {
-            v[i][0] = there ? __ldg(reinterpret_cast<const uint32_t *>(codes)) : 0;
-            vs[i] = there ? __ldg(scales + g / 2) : 0;
+            v[0] = vtk_expand8(*reinterpret_cast<const uint32_t *>(codes + 4 * g), s0);
         }
-    }
-    static __device__ __forceinline__ uint4 expand(uint32_t w, uint32_t s)
-    {
-        return make_uint4(vtk_hmul2(vtk_codes_to_half2(w), s), vtk_hmul2(vtk_codes_to_half2(w >> 8), s),
-                          vtk_hmul2(vtk_codes_to_half2(w >> 16), s), vtk_hmul2(vtk_codes_to_half2(w >> 24), s));
-    }
-    __device__ __forceinline__ uint4 get_k(int u, int j) const
-    {
-        // D 128: words 0, 1 belong to the first of the lane's two groups, 2, 3 to the second
-        const uint32_t two = vtk_scales_to_half2(D == 128 ? (j < 2 ? (ks[u] & 0xffu) : (ks[u] >> 8)) : ks[u]);
-        return expand(k[u][j], __byte_perm(two, 0, 0x1010));
-    }
-    __device__ __forceinline__ uint4 get_v(int i, int x) const
-    {
-        return expand(v[i][x], __byte_perm(vtk_scales_to_half2(vs[i]), 0, 0x1010));
     }
 };
 
-// a request as a CTA's shared memory keeps it
+// ring stages of a warp: what is left of 227 KB next to the join buffer, eight at most
+template <int NR, typename Rows, int D> constexpr int at_stages()
+{
+    constexpr int NW = Rows::WARPS, room = (231000 - 128 - NW * NR * 8 - NW * NR * D * 4) / NW / (Rows::STAGE + Rows::TILE * 4);
+    return room > 8 ? 8 : room;
+}
+
+template <int D, int NR, typename Rows>
+struct Shared {
+    static constexpr int ST = at_stages<NR, Rows, D>(), NW = Rows::WARPS, NT = NW * 32;
+    alignas(128) uint8_t ring[NW][ST][Rows::STAGE];
+    alignas(16) union {
+        float o[NW][NR][D];        // join: 16-byte pieces of a row permuted by the row
+        struct { int prefix[NT + 1]; int warp_sum[NW], warp_segments[NW]; int segments; } plan;
+    };
+    float2 ml[NW][NR];
+    int ids[NW][ST][Rows::TILE];
+    int last[NW];
+};
+
+// one request as the cut sees it
 struct Known {
-    int q0, qn, lo, n_sink, n, len;
-    int64_t base;
+    int q0, qn, len, tiles, row_tiles;
+    int pmax, floor;                     // no query sees an id above pmax, nor one up to floor that is no sink
+    VtkRequest s;                        // (base, lo, n_sink, n)
 };
 
+template <int NR, int TILE>
 __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
 {
     Known k;
     bool c;
-    vtk_request_rows(a, r, k.q0, k.qn, k.base, k.len, c);
+    vtk_request_rows(a, r, k.q0, k.qn, k.s.base, k.len, c);
     clipped |= c;
     if (k.qn * (int64_t)a.group > a.row_limit) k.qn = 0;
-    k.lo = k.n_sink = 0;
-    k.n = k.len;
+    k.s.lo = k.s.n_sink = 0;
+    k.s.n = k.len;
+    k.pmax = INT32_MAX - 1;
+    k.floor = -1;
+    k.row_tiles = (k.qn * a.group + NR - 1) / NR;
     if (k.qn > 0 && k.qn <= 8) {         // few queries: only what one of them can see
+        const int last = vtk_last_id(a, k.s.base, k.len);
         int pmin = a.positions[k.q0], pmax = pmin;
         for (int i = 1; i < k.qn; ++i) {
             const int p = a.positions[k.q0 + i];
             pmin = p < pmin ? p : pmin;
             pmax = p > pmax ? p : pmax;
         }
-        const VtkRequest s = vtk_request_span(a, k.base, k.len, pmin, pmax);
-        k.lo = s.lo;
-        k.n_sink = s.n_sink;
-        k.n = s.n;
+        k.pmax = pmax;
+        k.floor = vtk_floor(pmin, a.window);
+        k.s = vtk_request_span(a, k.s.base, k.len, last, pmin, pmax);
     }
+    k.tiles = k.qn > 0 ? (k.s.n > 0 ? (k.s.n + TILE - 1) / TILE : 1) : 0;
     return k;
 }
 
-// NR: query rows of an item (8 or 16); SPLIT_P: P as a sum of two 16-bit values
+// A walk over the segments of a share; the request it is at is kept in the warp's shared memory.
+template <int NR, int TILE>
+struct Walk {
+    Known *k;
+    int r, rt, kv, t0, t1;               // segment and its tiles [t0, t1) inside the share
+    int64_t f, f1;                       // next tile of the row of all tiles, end of the share
+    __device__ __forceinline__ void clip() { t1 = k->tiles - t0 < f1 - f ? k->tiles : t0 + (int)(f1 - f); }
+    __device__ __forceinline__ bool done() const { return f >= f1; }
+    static __device__ __forceinline__ bool in_window(int r, int r_known) { return r >= r_known && r - r_known < AT_KNOWN; }
+    __device__ __forceinline__ void next(const VtkAttnArgs &a, const Known *known, int r_known)
+    {
+        f += t1 - t0;
+        t0 = t1 = 0;
+        if (done()) return;
+        if (++kv == a.hkv) {
+            kv = 0;
+            if (++rt == k->row_tiles) {
+                rt = 0;
+                bool c = false;
+                int tiles;
+                do {
+                    ++r;
+                    const Known n = in_window(r, r_known) ? known[r - r_known] : look_up<NR, TILE>(a, r, c);
+                    tiles = n.tiles;
+                    __syncwarp();
+                    if (vtk_lane() == 0) *k = n;
+                    __syncwarp();
+                } while (tiles == 0);
+            }
+        }
+        clip();
+    }
+};
+
+// NR: query rows of a segment (8 or 16); SPLIT_P: P as a sum of two 16-bit values
 template <int D, int NR, typename Rows, typename Act, bool SPLIT_P>
-__global__ void __launch_bounds__(AT_NT, AT_CTAS<NR>) attention_rows_kernel(const __grid_constant__ VtkAttnArgs a)
+__global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(const __grid_constant__ VtkAttnArgs a)
 {
     using Mma = typename Rows::Mma;
-    constexpr int RH = NR / 8, MT = D / 16, N = D / 32;
-    __shared__ __align__(16) float s_o[AT_WARPS][NR][D + 4];
-    __shared__ float2 s_ml[AT_WARPS][NR];
-    __shared__ Known s_known[AT_KNOWN<NR>];
-    __shared__ int s_items[AT_NT + 1], s_splits[AT_NT + 1];
-    __shared__ unsigned long long s_sum[AT_WARPS];
-    __shared__ int s_last;
+    using Sh = Shared<D, NR, Rows>;
+    constexpr int RH = NR / 8, MT = D / 16, N = D / 32, ST = Sh::ST, TILE = Rows::TILE, NW = Rows::WARPS, NT = NW * 32;
+    extern __shared__ __align__(128) uint8_t raw[];
+    Sh &sh = *reinterpret_cast<Sh *>(raw);
+    __shared__ Known s_known[AT_KNOWN], s_get[NW], s_use[NW];
     vtk_release_successor();
     vtk_wait_for_predecessor();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
 
-    // ---- the cut: every CTA works it out for itself (one or two loads per request and two scans) ----
+    // ---- the share: tiles before each thread's requests, by two or three rounds of loads per request and a scan ----
     int R = *a.num_requests;
     bool clipped = R < 0 || R > a.max_requests;
     R = R < 0 ? 0 : (R > a.max_requests ? a.max_requests : R);
-    const int seg = (R + AT_NT - 1) / AT_NT, r_lo = tid * seg, r_hi = r_lo + seg < R ? r_lo + seg : R;
-    unsigned long long total = 0;
-    for (int r = r_lo; r < r_hi; ++r) {
-        const Known k = look_up(a, r, clipped);
-        if (r < AT_KNOWN<NR>) s_known[r] = k;
-        total += (unsigned long long)k.n * ((k.qn * a.group + NR - 1) / NR);
+    const int seg = (R + NT - 1) / NT;
+    int mine = 0, my_segments = 0;
+    Known own;                                               // the thread's last request: its only one below 257 requests
+    for (int r = tid * seg; r < (tid + 1) * seg && r < R; ++r) {
+        own = look_up<NR, TILE>(a, r, clipped);
+        mine += own.tiles * own.row_tiles;
+        my_segments += own.tiles > 0 ? own.row_tiles : 0;
     }
     if (clipped && blockIdx.x == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    if (lane == 0) s_sum[warp] = total;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < AT_WARPS; ++w) total += s_sum[w];
-    int64_t want = (int64_t)((total + a.target - 1) / a.target);
-    want = want < a.min_chunk ? a.min_chunk : want;
-    const int chunk = (int)((want + AT_WARPS * 16 - 1) / (AT_WARPS * 16)) * (AT_WARPS * 16);
-    int items = 0, splits = 0;
-    for (int r = r_lo; r < r_hi; ++r) {
-        const Known k = r < AT_KNOWN<NR> ? s_known[r] : look_up(a, r, clipped);
-        const int rt = (k.qn * a.group + NR - 1) / NR, nc = k.n > chunk ? (k.n + chunk - 1) / chunk : 1;
-        items += rt * nc;
-        if (nc > 1) splits += rt * nc;
-    }
     {
-        const int i_items = vtk_warp_incl_scan(items), i_splits = vtk_warp_incl_scan(splits);
-        __shared__ int w_items[AT_WARPS], w_splits[AT_WARPS];
-        if (lane == 31) { w_items[warp] = i_items; w_splits[warp] = i_splits; }
+        const int incl = vtk_warp_incl_scan(mine);
+        my_segments = __reduce_add_sync(0xffffffffu, my_segments);
+        if (lane == 31) {
+            sh.plan.warp_sum[warp] = incl;
+            sh.plan.warp_segments[warp] = my_segments;
+        }
         __syncthreads();
-        int b_items = 0, b_splits = 0;
-        for (int w = 0; w < warp; ++w) { b_items += w_items[w]; b_splits += w_splits[w]; }
-        s_items[tid + 1] = b_items + i_items;
-        s_splits[tid + 1] = b_splits + i_splits;
-        if (tid == 0) s_items[0] = s_splits[0] = 0;
+        int before = 0, all_segments = 0;
+        for (int w = 0; w < warp; ++w) before += sh.plan.warp_sum[w];
+        for (int w = 0; w < NW; ++w) all_segments += sh.plan.warp_segments[w];
+        if (tid == 0) sh.plan.segments = all_segments;
+        sh.plan.prefix[tid + 1] = before + incl;
+        if (tid == 0) sh.plan.prefix[0] = 0;
         __syncthreads();
     }
-    const int64_t all = (int64_t)s_items[AT_NT] * a.hkv;
-
-    for (int64_t item = blockIdx.x; item < all; item += gridDim.x) {
-        // ---- which: the heads of a chunk follow one another, so neighbouring CTAs read neighbouring bytes ----
-        const int kv = (int)(item % a.hkv), idx = (int)(item / a.hkv);
-        int lo = 0, hi = AT_NT;                              // s_items[lo] <= idx < s_items[hi]
+    const int64_t W = (int64_t)sh.plan.prefix[NT] * a.hkv;
+    // ---- teams: the fewer segments there are, the more warps share one ----
+    const int64_t segments = (int64_t)sh.plan.segments * a.hkv, warps = (int64_t)gridDim.x * NW;
+    int team = NW;                                           // warps of a team
+    if (segments * AT_PARTS >= warps) team = 1;
+    else if (segments * AT_PARTS * (NW / 4) >= warps) team = NW / 4;
+    else if (segments * AT_PARTS * (NW / 2) >= warps) team = NW / 2;
+    const int teams = NW / team, my_team = warp / team, tw = warp % team;
+    // at least AT_MIN_SHARE tiles a warp: a segment that is cut finer costs more to join than it gains
+    const int64_t most = (W + AT_MIN_SHARE * team - 1) / (AT_MIN_SHARE * team), G = most < (int64_t)gridDim.x * teams ? most : (int64_t)gridDim.x * teams;
+    const bool packed = G == (int64_t)gridDim.x * teams;     // a CTA's shares side by side; few shares: on different SMs
+    const int share0 = packed ? blockIdx.x * teams : blockIdx.x, share = packed ? share0 + my_team : my_team * gridDim.x + blockIdx.x;
+    auto find = [&](int64_t f) {                             // thread segment that holds tile f
+        const int at = (int)(f / a.hkv);                     // (in tiles of one key head)
+        int lo = 0, hi = NT;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (s_items[mid] <= idx) lo = mid; else hi = mid;
+            if (sh.plan.prefix[mid] <= at) lo = mid; else hi = mid;
         }
-        int left = idx - s_items[lo], split0 = s_splits[lo], r = lo * seg, nc = 1;
-        Known rq;
-        for (;; ++r) {
-            rq = r < AT_KNOWN<NR> ? s_known[r] : look_up(a, r, clipped);
-            nc = rq.n > chunk ? (rq.n + chunk - 1) / chunk : 1;
-            const int its = nc * ((rq.qn * a.group + NR - 1) / NR);
-            if (left < its) break;
-            left -= its;
-            if (nc > 1) split0 += its;
+        return lo;
+    };
+    Walk<NR, TILE> use;
+    use.f = share < G ? W * share / G : 0;
+    use.f1 = share < G ? W * (share + 1) / G : 0;
+    use.k = &s_use[warp];
+    int64_t left = 0;
+    if (share < G) {
+        const int lo = find(use.f);
+        left = use.f - (int64_t)sh.plan.prefix[lo] * a.hkv;
+        use.r = lo * seg;
+    }
+    const int known0 = G > 0 ? find(share0 < G ? W * share0 / G : 0) : 0;
+    if (seg == 1 && tid >= known0 && tid < known0 + AT_KNOWN && tid < R) s_known[tid - known0] = own;
+    const int r_known = seg == 1 ? known0 : INT32_MAX;
+    __syncthreads();                                         // the plan's arrays become the join buffers
+    if (share >= G) return;
+    for (;; ++use.r) {
+        bool c = false;
+        const Known k = use.in_window(use.r, r_known) ? s_known[use.r - r_known] : look_up<NR, TILE>(a, use.r, c);
+        const int64_t all = (int64_t)k.tiles * k.row_tiles * a.hkv;
+        if (left < all) {
+            if (lane == 0) s_use[warp] = s_get[warp] = k;
+            __syncwarp();
+            break;
         }
-        const int rt = left / nc, c = left % nc;
-        split0 += rt * nc;                                   // first partial of this row tile
-        const int rows = rq.qn * a.group - rt * NR < NR ? rq.qn * a.group - rt * NR : NR;
+        left -= all;
+    }
+    use.rt = (int)(left / ((int64_t)use.k->tiles * a.hkv));
+    left -= (int64_t)use.rt * use.k->tiles * a.hkv;
+    use.kv = (int)(left / use.k->tiles);
+    use.t0 = (int)(left - (int64_t)use.kv * use.k->tiles);
+    use.clip();
+    auto team_sync = [&]() {
+        if (team == 1) __syncwarp();
+        else asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + my_team), "r"(team * 32) : "memory");
+    };
 
+    // ---- the stream: this warp's tiles, ST - 1 ahead of their use, whatever segment they are of ----
+    struct Next {                                            // a tile whose slots are on their way
+        int slot, id, kv, pmax, floor;
+        bool there;
+    };
+    Walk<NR, TILE> get = use;
+    get.k = &s_get[warp];
+    int tile = get.t0 + tw, issued = 0;
+    bool more = true;
+    auto meta = [&]() {                                      // the warp's next tile: slots and ids of its tokens
+        while (more && tile >= get.t1) {
+            get.next(a, s_known, r_known);
+            more = !get.done();
+            tile = get.t0 + tw;
+        }
+        Next n;
+        n.slot = -1;
+        n.id = INT32_MAX;
+        n.pmax = n.floor = -1;
+        n.kv = get.kv;
+        n.there = more;
+        const int v = tile * TILE + lane;
+        if (more && lane < TILE && v < get.k->s.n) {
+            n.slot = a.cache_slots[get.k->s.entry(v)];
+            n.id = a.cache_ids.null() ? get.k->s.index(v) : a.cache_ids[get.k->s.entry(v)];
+            n.pmax = get.k->pmax;
+            n.floor = get.k->floor;
+        }
+        tile += team;
+        return n;
+    };
+    auto issue = [&](Next n) {
+        if (n.there) {
+            if (n.slot >= 0 && (int64_t)n.slot >= a.slots_per_layer) {
+                atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
+                n.slot = -1;
+            }
+            if (!vtk_sees(n.id, n.pmax, n.floor, a.sinks)) n.slot = -1;
+            const int stage = issued % ST;
+            if (lane < TILE) sh.ids[warp][stage][lane] = n.slot < 0 ? INT32_MAX : n.id;
+            Rows::issue(smem_u32(sh.ring[warp][stage]), a.k_rows, a.v_rows, a.row_bytes, a.hkv, n.kv, n.slot);
+            ++issued;
+        }
+        cp_commit();
+    };
+    Next next;
+    {
+        Next first[ST - 1];
+#pragma unroll
+        for (int i = 0; i < ST - 1; ++i) first[i] = meta();
+        next = meta();
+#pragma unroll
+        for (int i = 0; i < ST - 1; ++i) issue(first[i]);
+    }
+
+    int used = 0;
+    for (; !use.done(); use.next(a, s_known, r_known)) {
+        const int kv = use.kv, rt = use.rt;
+        const int rows = use.k->qn * a.group - rt * NR < NR ? use.k->qn * a.group - rt * NR : NR;
         // ---- queries: lane (g, t) holds of rows g and 8 + g the dimensions its K fragments hold ----
         uint4 q[RH][D / 32];
-        int pos[RH];
+        int pos[RH], floor[RH];
         float scale[RH];
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
             const int row = g + 8 * h, at = rt * NR + row;
-            pos[h] = -1;
+            pos[h] = floor[h] = -1;
             scale[h] = a.scale_log2;
             const uint16_t *p = nullptr;
             if (row < rows) {
-                const int64_t tok = rq.q0 + at / a.group;
+                const int64_t tok = use.k->q0 + at / a.group;
                 pos[h] = a.positions[tok];
+                floor[h] = vtk_floor(pos[h], a.window);
                 p = a.q + tok * a.q_stride + (int64_t)(kv * a.group + at % a.group) * D;
             }
 #pragma unroll
@@ -267,6 +445,7 @@ __global__ void __launch_bounds__(AT_NT, AT_CTAS<NR>) attention_rows_kernel(cons
         }
         pmin = __reduce_min_sync(0xffffffffu, pmin);
         pmax = __reduce_max_sync(0xffffffffu, pmax);
+        const int floor_min = vtk_floor(pmin, a.window), floor_max = vtk_floor(pmax, a.window);
 
         float o[MT][RH][4], m[RH], l[RH];
 #pragma unroll
@@ -278,97 +457,56 @@ __global__ void __launch_bounds__(AT_NT, AT_CTAS<NR>) attention_rows_kernel(cons
 #pragma unroll
         for (int h = 0; h < RH; ++h) { m[h] = -INFINITY; l[h] = 0.f; }
 
-        // ---- the chunk: warp w takes tiles w, w + AT_WARPS, ... of 16 tokens ----
-        const int v_end = c * chunk + chunk < rq.n ? c * chunk + chunk : rq.n;
-        const int span = rq.n_sink;
-        auto meta = [&](int v, int &slot, int &id) {         // lanes 0 .. 15: entry v + lane
-            slot = -1;
-            id = INT32_MAX;
-            if (lane < 16 && v + lane < v_end) {
-                const int i = v + lane < span ? v + lane : rq.lo + (v + lane - span);
-                slot = a.cache_slots[rq.base + i];
-                id = a.cache_ids.null() ? i : a.cache_ids[rq.base + i];
-            }
-        };
-        int v = c * chunk + warp * 16, slot = -1, id = INT32_MAX, slot2, id2;
-        unsigned some = 0, full = 0;
-        Rows rows_now;
-        auto judge = [&]() {
-            if (slot >= 0 && (int64_t)slot >= a.slots_per_layer) {
-                atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
-                slot = -1;
-            }
-            const bool any = slot >= 0 && id <= pmax && (a.window == 0 || id > (int64_t)pmin - a.window || id < a.sinks);
-            const bool every = any && id <= pmin && (a.window == 0 || id > (int64_t)pmax - a.window || id < a.sinks);
-            some = __ballot_sync(0xffffffffu, any);
-            full = __ballot_sync(0xffffffffu, every);
-        };
-        auto load_k = [&]() {
+        for (int tl = use.t0 + tw; tl < use.t1; tl += team, ++used) {
+            cp_wait<ST - 2>();
+            __syncwarp();
+            issue(next);
+            next = meta();
+            const int stage = used % ST;
+            Rows rows_now;
+            rows_now.at = sh.ring[warp][stage];
+            const int *ids = sh.ids[warp][stage];
+            const int my_id = ids[lane & (TILE - 1)];
+            if (!__any_sync(0xffffffffu, vtk_sees(my_id, pmax, floor_min, a.sinks))) continue;
+            const bool full = __all_sync(0xffffffffu, vtk_sees(my_id, pmin, floor_max, a.sinks));
+            constexpr int SUB = TILE / 16;
+            float p[SUB][2][4], tile_max[RH];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int64_t s = __shfl_sync(0xffffffffu, slot, 8 * u + g);
-                rows_now.load_k(u, (some >> (8 * u + g)) & 1u, a.k_rows + s * a.row_bytes, a.hkv, kv, t);
-            }
-        };
-        auto load_v = [&]() {
+            for (int b = 0; b < SUB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int tok = 2 * t + (i & 1) + 8 * (i >> 1);
-                const int64_t s = __shfl_sync(0xffffffffu, slot, tok);
-                rows_now.load_v(i, (some >> tok) & 1u, a.v_rows + s * a.row_bytes, a.hkv, kv, g);
-            }
-        };
-        auto advance = [&]() {                               // to the warp's next tile that some row sees
-            while (v < v_end) {
-                slot = slot2;
-                id = id2;
-                meta(v + AT_WARPS * 16, slot2, id2);
-                judge();
-                if (some) return;
-                v += AT_WARPS * 16;
-            }
-            some = 0;
-        };
-        meta(v, slot2, id2);
-        advance();
-        if (some) { load_k(); load_v(); }
-        while (some) {
-            float s[2][4];
+                for (int u = 0; u < 2; ++u) {
+                    p[b][u][0] = p[b][u][1] = p[b][u][2] = p[b][u][3] = 0.f;
+                    uint4 k[D / 32];
+                    rows_now.get_k(b, u, g, t, k);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.f;
-#pragma unroll
-                for (int j = 0; j < D / 32; ++j) {
-                    const uint4 k = rows_now.get_k(u, j);
-                    vtk_mma<Mma>(s[u], q[0][j].x, RH == 2 ? q[RH - 1][j].x : 0u, q[0][j].y, RH == 2 ? q[RH - 1][j].y : 0u, k.x, k.y);
-                    vtk_mma<Mma>(s[u], q[0][j].z, RH == 2 ? q[RH - 1][j].z : 0u, q[0][j].w, RH == 2 ? q[RH - 1][j].w : 0u, k.z, k.w);
+                    for (int j = 0; j < D / 32; ++j) {
+                        vtk_mma<Mma>(p[b][u], q[0][j].x, RH == 2 ? q[RH - 1][j].x : 0u, q[0][j].y, RH == 2 ? q[RH - 1][j].y : 0u, k[j].x, k[j].y);
+                        vtk_mma<Mma>(p[b][u], q[0][j].z, RH == 2 ? q[RH - 1][j].z : 0u, q[0][j].w, RH == 2 ? q[RH - 1][j].w : 0u, k[j].z, k[j].w);
+                    }
                 }
-            }
-            // the tile's masks; then the next tile's K rows are on their way while this one is worked on
-            const unsigned some_now = some, full_now = full;
-            int ids[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ids[i] = __shfl_sync(0xffffffffu, id, 2 * t + (i & 1) + 8 * (i >> 1));
-            v += AT_WARPS * 16;
-            advance();
-            if (some) load_k();
-            float p[2][4], tile_max[RH];
 #pragma unroll
             for (int h = 0; h < RH; ++h) tile_max[h] = -INFINITY;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int b = 0; b < SUB; ++b)
 #pragma unroll
-                for (int e = 0; e < 2 * RH; ++e) {
-                    const int h = e >> 1, tok = 2 * t + (e & 1) + 8 * u;
-                    float x = s[u][e] * scale[h];
-                    if (full_now != 0xffffu) {
-                        const bool see = ((full_now >> tok) & 1u) ||
-                                         (((some_now >> tok) & 1u) && vtk_sees(ids[(e & 1) + 2 * u], pos[h], a.window, a.sinks));
-                        x = see ? x : -INFINITY;
-                    }
-                    p[u][e] = x;
-                    tile_max[h] = fmaxf(tile_max[h], x);
-                }
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 2 * RH; ++e) p[b][u][e] *= scale[e >> 1];
+            if (!full) {
+#pragma unroll
+                for (int b = 0; b < SUB; ++b)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 2 * RH; ++e)
+                            if (!vtk_sees(ids[16 * b + 2 * t + (e & 1) + 8 * u], pos[e >> 1], floor[e >> 1], a.sinks)) p[b][u][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int b = 0; b < SUB; ++b)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 2 * RH; ++e) tile_max[e >> 1] = fmaxf(tile_max[e >> 1], p[b][u][e]);
             // the running maximum moves only when a score passes it by 2^8: sums and P stay far inside 32 bits
             bool up = tile_max[0] > m[0] + 8.f;
             if (RH == 2) up |= tile_max[RH - 1] > m[RH - 1] + 8.f;
@@ -390,116 +528,125 @@ __global__ void __launch_bounds__(AT_NT, AT_CTAS<NR>) attention_rows_kernel(cons
                     }
                 }
             }
-            uint32_t b[RH][2], b_lo[RH][2];
 #pragma unroll
-            for (int h = 0; h < RH; ++h) {
-                const float base = m[h] == -INFINITY ? 0.f : m[h];
+            for (int b = 0; b < SUB; ++b) {
+                uint32_t w[RH][2], w_lo[RH][2];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float p0 = vtk_exp2(p[u][2 * h] - base), p1 = vtk_exp2(p[u][2 * h + 1] - base);
-                    l[h] += p0 + p1;
-                    b[h][u] = Mma::pack(p0, p1);
-                    if (SPLIT_P) {
-                        const float2 r = Mma::unpack(b[h][u]);
-                        b_lo[h][u] = Mma::pack(p0 - r.x, p1 - r.y);
+                for (int h = 0; h < RH; ++h) {
+                    const float base = m[h] == -INFINITY ? 0.f : m[h];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const float p0 = vtk_exp2(p[b][u][2 * h] - base), p1 = vtk_exp2(p[b][u][2 * h + 1] - base);
+                        l[h] += p0 + p1;
+                        w[h][u] = Mma::pack(p0, p1);
+                        if (SPLIT_P) {
+                            const float2 r = Mma::unpack(w[h][u]);
+                            w_lo[h][u] = Mma::pack(p0 - r.x, p1 - r.y);
+                        }
+                    }
+                }
+                uint4 v[4][D / 64];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) rows_now.get_v(b, i, g, t, v[i]);
+#pragma unroll
+                for (int x = 0; x < D / 64; ++x) {
+                    const uint32_t w0[4] = {v[0][x].x, v[0][x].y, v[0][x].z, v[0][x].w}, w1[4] = {v[1][x].x, v[1][x].y, v[1][x].z, v[1][x].w};
+                    const uint32_t w2[4] = {v[2][x].x, v[2][x].y, v[2][x].z, v[2][x].w}, w3[4] = {v[3][x].x, v[3][x].y, v[3][x].z, v[3][x].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t a0 = __byte_perm(w0[i], w1[i], 0x5410), a1 = __byte_perm(w0[i], w1[i], 0x7632);
+                        const uint32_t a2 = __byte_perm(w2[i], w3[i], 0x5410), a3 = __byte_perm(w2[i], w3[i], 0x7632);
+#pragma unroll
+                        for (int h = 0; h < RH; ++h) {
+                            vtk_mma<Mma>(o[4 * x + i][h], a0, a1, a2, a3, w[h][0], w[h][1]);
+                            if (SPLIT_P) vtk_mma<Mma>(o[4 * x + i][h], a0, a1, a2, a3, w_lo[h][0], w_lo[h][1]);
+                        }
                     }
                 }
             }
-#pragma unroll
-            for (int x = 0; x < D / 64; ++x) {
-                const uint4 v0 = rows_now.get_v(0, x), v1 = rows_now.get_v(1, x), v2 = rows_now.get_v(2, x), v3 = rows_now.get_v(3, x);
-                const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-                const uint32_t w2[4] = {v2.x, v2.y, v2.z, v2.w}, w3[4] = {v3.x, v3.y, v3.z, v3.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = __byte_perm(w0[i], w1[i], 0x5410), a1 = __byte_perm(w0[i], w1[i], 0x7632);
-                    const uint32_t a2 = __byte_perm(w2[i], w3[i], 0x5410), a3 = __byte_perm(w2[i], w3[i], 0x7632);
-#pragma unroll
-                    for (int h = 0; h < RH; ++h) {
-                        vtk_mma<Mma>(o[4 * x + i][h], a0, a1, a2, a3, b[h][0], b[h][1]);
-                        if (SPLIT_P) vtk_mma<Mma>(o[4 * x + i][h], a0, a1, a2, a3, b_lo[h][0], b_lo[h][1]);
-                    }
-                }
-            }
-            if (some) load_v();
         }
 
-        // ---- join the warps ----
+        // ---- join the team's warps ----
+        auto piece = [](int row, int c) { return ((c ^ (row & 7)) << 2); };      // 16-byte piece c of a row
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-            if (t == 0) s_ml[warp][g + 8 * h] = make_float2(m[h], l[h]);
+            if (t == 0) sh.ml[warp][g + 8 * h] = make_float2(m[h], l[h]);
 #pragma unroll
             for (int x = 0; x < D / 64; ++x)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {                // query row 2t + e: eight consecutive dimensions
-                    float *dst = &s_o[warp][8 * h + 2 * t + e][Rows::vdim(g, x)];
-                    *reinterpret_cast<float4 *>(dst) = make_float4(o[4 * x][h][e], o[4 * x][h][2 + e], o[4 * x + 1][h][e], o[4 * x + 1][h][2 + e]);
-                    *reinterpret_cast<float4 *>(dst + 4) = make_float4(o[4 * x + 2][h][e], o[4 * x + 2][h][2 + e], o[4 * x + 3][h][e], o[4 * x + 3][h][2 + e]);
+                    const int row = 8 * h + 2 * t + e, c = Rows::vdim(g, x) / 4;
+                    *reinterpret_cast<float4 *>(&sh.o[warp][row][piece(row, c)]) = make_float4(o[4 * x][h][e], o[4 * x][h][2 + e], o[4 * x + 1][h][e], o[4 * x + 1][h][2 + e]);
+                    *reinterpret_cast<float4 *>(&sh.o[warp][row][piece(row, c + 1)]) = make_float4(o[4 * x + 2][h][e], o[4 * x + 2][h][2 + e], o[4 * x + 3][h][e], o[4 * x + 3][h][2 + e]);
                 }
         }
-        __syncthreads();
-        float *part = nc > 1 ? a.part + ((int64_t)(split0 + c) * a.hkv + kv) * (NR * (D + 2)) : nullptr;
+        team_sync();
+        const int w0 = my_team * team;
+        const int64_t seg_lo = use.f - use.t0, seg_hi = seg_lo + use.k->tiles;
+        const bool whole = use.t0 == 0 && use.t1 == use.k->tiles;
+        // shares that hold parts of this segment, and where a share leaves its part
+        const int first = (int)(((seg_lo + 1) * G - 1) / W), parts = (int)((seg_hi * G - 1) / W) - first + 1;
+        auto part_at = [&](int i) { return a.part + (int64_t)(2 * i + (i == first)) * (NR * (D + 2)); };
         auto finish = [&](int row, float (&acc)[N], float mm, float ll) {
             const int at = rt * NR + row, head = kv * a.group + at % a.group;
-            const int64_t tok = rq.q0 + at / a.group;
+            const int64_t tok = use.k->q0 + at / a.group;
             bool bad = !(fabsf(ll) < INFINITY);
 #pragma unroll
             for (int j = 0; j < N; ++j) bad |= !(fabsf(acc[j]) < INFINITY);
-            if (rq.qn > 1 && __any_sync(0xffffffffu, bad))   // (one query token: what it does not see was not read)
-                vtk_row_again<D, Rows::FP4, Act>(a, tok, head, a.positions[tok], rq.base, rq.len, acc, mm, ll);
+            if (use.k->qn > 1 && __any_sync(0xffffffffu, bad))   // (one query token: what it does not see was not read)
+                vtk_row_again<D, Rows::FP4, Act>(a, tok, head, a.positions[tok], use.k->s.base, use.k->len, acc, mm, ll);
             vtk_store_row<D, Act>(a, tok, head, acc, mm, ll);
         };
-        for (int row = warp; row < rows; row += AT_WARPS) {
+        for (int row = tw; row < rows; row += team) {
             float mm = -INFINITY, ll = 0.f, acc[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) acc[j] = 0.f;
-#pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) mm = fmaxf(mm, s_ml[w][row].x);
-#pragma unroll
-            for (int w = 0; w < AT_WARPS; ++w) {
-                const float2 ml = s_ml[w][row];
+            for (int w = w0; w < w0 + team; ++w) mm = fmaxf(mm, sh.ml[w][row].x);
+#pragma unroll 4
+            for (int w = w0; w < w0 + team; ++w) {
+                const float2 ml = sh.ml[w][row];
                 const float f = ml.x == -INFINITY ? 0.f : (ml.x == mm ? 1.f : vtk_exp2(ml.x - mm));
                 ll += f * ml.y;
+                const float *src = &sh.o[w][row][piece(row, lane * N / 4) + (lane * N) % 4];
 #pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] += f * s_o[w][row][lane * N + j];
+                for (int j = 0; j < N; ++j) acc[j] += f * src[j];
             }
-            if (nc > 1) {
-                float *dst = part + row * D + lane * N;
+            if (!whole) {
+                float *dst = part_at(share) + row * D + lane * N;
                 if (N == 4) *reinterpret_cast<float4 *>(dst) = make_float4(acc[0], acc[1], acc[N - 2], acc[N - 1]);
                 else *reinterpret_cast<float2 *>(dst) = make_float2(acc[0], acc[1]);
-                if (lane == 0) *reinterpret_cast<float2 *>(part + NR * D + 2 * row) = make_float2(mm, ll);
+                if (lane == 0) *reinterpret_cast<float2 *>(part_at(share) + NR * D + 2 * row) = make_float2(mm, ll);
             } else {
                 finish(row, acc, mm, ll);
             }
         }
-        if (nc > 1) {
+        if (!whole) {
             __threadfence();
-            __syncthreads();
-            uint32_t *counter = a.counters + (int64_t)split0 * a.hkv + kv;
-            if (tid == 0) {
-                s_last = atomicAdd(counter, 1u) == (unsigned)(nc - 1);
-                if (s_last) *counter = 0;                    // ready for the next call
+            team_sync();
+            if (tw == 0 && lane == 0) {
+                const bool last = atomicAdd(&a.counters[first], 1u) == (unsigned)(parts - 1);
+                if (last) a.counters[first] = 0;             // ready for the next call
+                sh.last[my_team] = last;
             }
-            __syncthreads();
-            if (s_last) {
+            team_sync();
+            if (*(volatile int *)&sh.last[my_team]) {
                 __threadfence();
-                const float *first = a.part + ((int64_t)split0 * a.hkv + kv) * (NR * (D + 2));
-                const int64_t step = (int64_t)a.hkv * (NR * (D + 2));
-                for (int row = warp; row < rows; row += AT_WARPS) {
+                for (int row = tw; row < rows; row += team) {
                     float mm = -INFINITY, ll = 0.f, acc[N];
 #pragma unroll
                     for (int j = 0; j < N; ++j) acc[j] = 0.f;
-                    for (int i = lane; i < nc; i += 32) mm = fmaxf(mm, __ldcg(first + i * step + NR * D + 2 * row));
+                    for (int i = lane; i < parts; i += 32) mm = fmaxf(mm, __ldcg(part_at(first + i) + NR * D + 2 * row));
 #pragma unroll
                     for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-#pragma unroll 4
-                    for (int i = 0; i < nc; ++i) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(first + i * step + NR * D + 2 * row));
+#pragma unroll 8
+                    for (int i = 0; i < parts; ++i) {
+                        const float *src = part_at(first + i);
+                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(src + NR * D + 2 * row));
                         const float f = ml.x == -INFINITY ? 0.f : (ml.x == mm ? 1.f : vtk_exp2(ml.x - mm));
                         ll += f * ml.y;
-                        const float *src = first + i * step + row * D + lane * N;
+                        src += row * D + lane * N;
                         if (N == 4) {
                             const float4 x = __ldcg(reinterpret_cast<const float4 *>(src));
                             acc[0] += f * x.x; acc[1] += f * x.y; acc[N - 2] += f * x.z; acc[N - 1] += f * x.w;
@@ -512,14 +659,18 @@ __global__ void __launch_bounds__(AT_NT, AT_CTAS<NR>) attention_rows_kernel(cons
                 }
             }
         }
-        __syncthreads();                                     // shared memory is reused by the next item
+        team_sync();                                         // the join buffers are used by the next segment
     }
 }
 
 template <int D, int NR, typename Rows, typename Act, bool SPLIT_P>
 int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, cudaStream_t st)
 {
-    VTK_CUDA(ctx, vtk_launch_dependent(ctx, attention_rows_kernel<D, NR, Rows, Act, SPLIT_P>, dim3(ctx->num_sms * AT_CTAS<NR>), dim3(AT_NT), 0, st, a));
+    auto kernel = attention_rows_kernel<D, NR, Rows, Act, SPLIT_P>;
+    constexpr int smem = (int)sizeof(Shared<D, NR, Rows>);
+    static_assert(Shared<D, NR, Rows>::ST >= 2 && smem + sizeof(Known) * (AT_KNOWN + 2 * Rows::WARPS) <= 232448, "shared memory of a CTA");
+    VTK_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(ctx->num_sms), dim3(Rows::WARPS * 32), smem, st, a));
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
 }
@@ -528,7 +679,7 @@ template <int D, typename Act>
 int launch_by_type(vtoken_ctx *ctx, bool fp4, bool wide, const VtkAttnArgs &a, cudaStream_t st)
 {
     constexpr bool bf = Act::kind == VTOKEN_KV_BF16;
-    if (fp4) return wide ? launch<D, 16, Rows4<D>, Act, !bf>(ctx, a, st) : launch<D, 8, Rows4<D>, Act, !bf>(ctx, a, st);
+    if (fp4) return wide ? launch<D, 16, Rows4<D, 8>, Act, !bf>(ctx, a, st) : launch<D, 8, Rows4<D, 12>, Act, !bf>(ctx, a, st);
     return wide ? launch<D, 16, Rows16<D, Act>, Act, true>(ctx, a, st) : launch<D, 8, Rows16<D, Act>, Act, true>(ctx, a, st);
 }
 
@@ -542,21 +693,13 @@ float two_to(int e)
 
 }  // namespace
 
-// Items per key head, and the workspace that the cut can need: only requests of more than one chunk leave partial
-// rows, at most 2 * target of them per key head (n > chunk gives ceil(n / chunk) < 2 n / chunk, and the sum of n
-// over row tiles is at most target * chunk).
+// A share leaves at most two partial row tiles (8 rows a tile from up to 12 teams a CTA, or 16 from up to 8).
 int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs *a)
 {
-    const int64_t items = (int64_t)ctx->num_sms * AT_CTAS<8> * 4;
-    const int64_t target = (items + heads->num_kv_heads - 1) / heads->num_kv_heads;
-    const int64_t splits = 2 * target * heads->num_kv_heads;
-    if (a) {
-        a->target = (int32_t)target;
-        a->min_chunk = 64;
-    }
-    const int64_t counters = (splits * 4 + 15) / 16 * 16 + 16;           // and the prompt kernel's two tickets in front
-    if (a && a->counters) a->part = (float *)((uint8_t *)(a->counters - 4) + counters);
-    return counters + splits * 16 * (heads->head_dim + 2) * 4;
+    const int64_t shares = (int64_t)ctx->num_sms * 12;
+    const int64_t counters = (shares * 4 + 15) / 16 * 16 + 16;       // and the prompt kernel's two tickets in front
+    if (a) a->part = (float *)((uint8_t *)(a->counters - 4) + counters);
+    return counters + shares * 2 * (16 * 8 / 12 + 1) * (heads->head_dim + 2) * 4;
 }
 
 int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st)

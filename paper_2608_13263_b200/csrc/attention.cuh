@@ -18,8 +18,6 @@ struct VtkAttnArgs {
     uint32_t *flags;
     uint32_t *counters;                  // workspace: arrivals of split rows, zero between calls
     float *part;                         // workspace: partial rows
-    int32_t target;                      // items (per key head) that a call is cut into when it is long enough
-    int32_t min_chunk;                   // tokens of the smallest item
     int32_t row_limit;                   // requests of more query rows (tokens times group) belong to attention_prompt.cu
 };
 
@@ -35,12 +33,18 @@ struct VtkRequest {
 
 __device__ __forceinline__ int vtk_clamp_offset(int x, int cap) { return x < 0 ? 0 : (x > cap ? cap : x); }
 
-// entries of the ascending ids [base, base + len) that are <= p
-__device__ inline int vtk_ids_up_to(const VtkAttnArgs &a, int64_t base, int len, int p)
+// the last id of [base, base + len): -1 when there is none
+__device__ __forceinline__ int vtk_last_id(const VtkAttnArgs &a, int64_t base, int len)
 {
+    return len == 0 ? -1 : (a.cache_ids.null() ? len - 1 : a.cache_ids[base + len - 1]);
+}
+
+// entries of the ascending ids [base, base + len) that are <= p
+__device__ inline int vtk_ids_up_to(const VtkAttnArgs &a, int64_t base, int len, int last, int p)
+{
+    if (last <= p) return len;
     if (p < 0) return 0;
     if (a.cache_ids.null()) return p + 1 < len ? p + 1 : len;
-    if (len == 0 || a.cache_ids[base + len - 1] <= p) return len;
     int lo = 0, hi = len - 1;            // ids[hi] > p
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -51,12 +55,12 @@ __device__ inline int vtk_ids_up_to(const VtkAttnArgs &a, int64_t base, int len,
 
 // Ids are strictly ascending from 0 or above, so ids[i] >= i: entry i >= sinks cannot be a sink, and of the
 // entries with ids <= pmax at most (pmax - pmin) + window have an id > pmin - window.
-__device__ inline VtkRequest vtk_request_span(const VtkAttnArgs &a, int64_t base, int len, int pmin, int pmax)
+__device__ inline VtkRequest vtk_request_span(const VtkAttnArgs &a, int64_t base, int len, int last, int pmin, int pmax)
 {
     VtkRequest q;
     q.q0 = q.qn = 0;
     q.base = base;
-    const int hi = vtk_ids_up_to(a, base, len, pmax);
+    const int hi = vtk_ids_up_to(a, base, len, last, pmax);
     int64_t lo = 0;
     if (a.window > 0) lo = (int64_t)hi - ((int64_t)pmax - pmin) - a.window;
     q.lo = lo > 0 ? (int)lo : 0;
@@ -80,10 +84,9 @@ __device__ inline void vtk_request_rows(const VtkAttnArgs &a, int r, int &q0, in
     clipped = a0 != q0 || a1 != q1 || q1 < q0 || t0 != base || t1 != end || want != len;
 }
 
-__device__ __forceinline__ bool vtk_sees(int id, int p, int window, int sinks)
-{
-    return id <= p && (window == 0 || id > (int64_t)p - window || id < sinks);
-}
+// Ids are not negative.  A query at p sees the ids in (vtk_floor(p), p] and those below `sinks`.
+__device__ __forceinline__ int vtk_floor(int p, int window) { return window == 0 || p < window ? -1 : p - window; }
+__device__ __forceinline__ bool vtk_sees(int id, int p, int floor, int sinks) { return id <= p && (id > floor || id < sinks); }
 
 // ---- matrix instructions: 16 x 8 += 16 x 16 by 16 x 8, 32-bit accumulators ----------------------
 template <typename M>
@@ -91,13 +94,13 @@ __device__ __forceinline__ void vtk_mma(float (&c)[4], uint32_t a0, uint32_t a1,
 template <>
 __device__ __forceinline__ void vtk_mma<VtkBf16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 template <>
 __device__ __forceinline__ void vtk_mma<VtkFp16>(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
@@ -163,12 +166,13 @@ __device__ __noinline__ void vtk_row_again(const VtkAttnArgs &a, int64_t q_row, 
     }
     m = -INFINITY;
     l = 0.f;
+    const int floor = vtk_floor(pos, a.window);
 #pragma unroll
     for (int j = 0; j < N; ++j) o[j] = 0.f;
     for (int i = 0; i < len; ++i) {
         const int id = a.cache_ids.null() ? i : a.cache_ids[base + i];
         const int64_t slot = a.cache_slots[base + i];
-        if (slot < 0 || slot >= a.slots_per_layer || !vtk_sees(id, pos, a.window, a.sinks)) continue;
+        if (slot < 0 || slot >= a.slots_per_layer || !vtk_sees(id, pos, floor, a.sinks)) continue;
         float k[N], v[N];
         vtk_row_values<D, FP4, Act, N>(a.k_rows + slot * a.row_bytes, a.hkv, kv, lane * N, k);
         vtk_row_values<D, FP4, Act, N>(a.v_rows + slot * a.row_bytes, a.hkv, kv, lane * N, v);

@@ -235,12 +235,6 @@ __device__ void next_item(const VtkAttnArgs &a, Shared<D> &sh, Item &out, int R,
     if (lane == 0) out = it;
 }
 
-// 4-bit codes of 8 values (one word) times their group's scale, as halves
-__device__ __forceinline__ uint4 expand8(uint32_t w, uint32_t s)
-{
-    return make_uint4(vtk_hmul2(vtk_codes_to_half2(w), s), vtk_hmul2(vtk_codes_to_half2(w >> 8), s),
-                      vtk_hmul2(vtk_codes_to_half2(w >> 16), s), vtk_hmul2(vtk_codes_to_half2(w >> 24), s));
-}
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 w)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
@@ -322,7 +316,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             const int at = it.first + x * AP_TILE + row;
             const int64_t tok = it.q0 + (have ? at / a.group : 0);
             const int head = it.kv * a.group + (have ? at % a.group : 0);
-            const int pos = have ? a.positions[tok] : -1;
+            const int pos = have ? a.positions[tok] : -1, floor = vtk_floor(pos, a.window);
             float m = -INFINITY, l = 0.f, c = scale;
             bool ok = true;
             if (x == 0 || two) {
@@ -348,7 +342,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         } else {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (vtk_sees(mt.ids[32 * q + i], pos, a.window, a.sinks)) top = fmaxf(top, __uint_as_float(s[i]));
+                                if (vtk_sees(mt.ids[32 * q + i], pos, floor, a.sinks)) top = fmaxf(top, __uint_as_float(s[i]));
                         }
                     }
                     const bool up = (top - m) * c > 8.f || (m == -INFINITY && top > -INFINITY);
@@ -379,7 +373,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         if (every != 0xffffffffu) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                if (!vtk_sees(mt.ids[32 * q + i], pos, a.window, a.sinks)) s[i] = 0xff800000u;
+                                if (!vtk_sees(mt.ids[32 * q + i], pos, floor, a.sinks)) s[i] = 0xff800000u;
                         }
                         uint32_t p[16];
 #pragma unroll
@@ -518,12 +512,12 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
                     bool ok = mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
                     // (K two tiles ago is consumed, so both softmaxes are past the tile whose meta this overwrites)
-                    const bool any = id <= pmax && (a.window == 0 || id > (int64_t)pmin - a.window || id < a.sinks);
+                    const bool any = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks);
                     mt.ids[pt] = id;
                     sh.slots[j & 1][pt] = any ? (int)slot : -1;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const bool every = id <= it.pmin[x] && (a.window == 0 || id > (int64_t)it.pmax[x] - a.window || id < a.sinks);
+                        const bool every = vtk_sees(id, it.pmin[x], vtk_floor(it.pmax[x], a.window), a.sinks);
                         const unsigned bits = __ballot_sync(0xffffffffu, every);
                         if (lane == 0) mt.every[x][warp - 8] = bits;
                     }
@@ -580,7 +574,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                                 const uint32_t two_scales = vtk_scales_to_half2(sc);
 #pragma unroll
                                 for (int i = 0; i < QW; ++i)
-                                    st_shared16(dst + swizzled(row, part * QW + i), expand8(w[i], __byte_perm(two_scales, 0, i < 2 ? 0x1010 : 0x3232)));
+                                    st_shared16(dst + swizzled(row, part * QW + i), vtk_expand8(w[i], __byte_perm(two_scales, 0, i < 2 ? 0x1010 : 0x3232)));
                             }
                             deliver((int)stage);
                         }

@@ -74,10 +74,26 @@ __device__ __forceinline__ uint32_t vtk_codes_to_half2(uint32_t b)
     return h;
 }
 
+// the eight codes of a word, in order
+__device__ __forceinline__ uint4 vtk_word_to_half2(uint32_t w)
+{
+    uint4 r;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(w));
+    return r;
+}
+
 __device__ __forceinline__ uint32_t vtk_hmul2(uint32_t a, uint32_t b)
 {
     const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&r);
+}
+
+// eight codes times the scale of their group (a pair of equal halves)
+__device__ __forceinline__ uint4 vtk_expand8(uint32_t w, uint32_t s)
+{
+    const uint4 c = vtk_word_to_half2(w);
+    return make_uint4(vtk_hmul2(c.x, s), vtk_hmul2(c.y, s), vtk_hmul2(c.z, s), vtk_hmul2(c.w, s));
 }
 
 // ---- host: geometry ----------------------------------------------------------------------------

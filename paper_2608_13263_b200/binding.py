@@ -242,12 +242,14 @@ def use_library(flavour: str) -> str:
 
 
 def _ptr(x):
+    try:
+        return x.data_ptr()           # (first: a call marshals a dozen tensors)
+    except AttributeError:
+        pass
     if x is None:
         return None
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if hasattr(x, "ctypes"):          # numpy array (host pointers of vtoken_repack_host)
         return x.ctypes.data
     raise TypeError(f"cannot take a pointer from {type(x)}")

@@ -36,12 +36,9 @@ constexpr int AT_KNOWN = 8;              // requests of a share that are looked 
 constexpr int AT_MIN_SHARE = 2;          // tiles of the smallest share, for each warp of its team
 constexpr int AT_PARTS = 3;              // shares that a segment of mean length is cut into at most, about
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-template <int BYTES>
-__device__ __forceinline__ void cp_async(uint32_t dst, const void *src, bool there)
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there)
 {
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -53,7 +50,7 @@ template <int D, typename Act>
 struct Rows16 {
     static constexpr bool FP4 = false;
     using Mma = Act;
-    static constexpr int WARPS = 8, TILE = 16, PITCH = D * 2, HALF = TILE * PITCH, STAGE = 2 * HALF, PIECES = D / 8;
+    static constexpr int WARPS = 8, GROUP = 1, TILE = 16, PITCH = D * 2, HALF = TILE * PITCH, STAGE = 2 * HALF, PIECES = D / 8;
     static __device__ __forceinline__ int kdim(int t, int j) { return 32 * j + 8 * t; }
     static __device__ __forceinline__ int vdim(int g, int x) { return 64 * x + 8 * g; }
     // slot: lane i < TILE holds that of token i, negative = zeros
@@ -66,11 +63,12 @@ struct Rows16 {
         for (int i = 0; i < TILE / PER; ++i) {
             const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
             const int64_t off = (s < 0 ? 0 : s) * row_bytes + off0;
-            cp_async<16>(dst + tok * PITCH + ((c ^ ((tok & 1) << 2)) << 4), k_rows + off, s >= 0);
-            cp_async<16>(dst + HALF + tok * PITCH + ((c ^ (((tok >> 1) & 3) << 1)) << 4), v_rows + off, s >= 0);
+            cp_async16(dst + tok * PITCH + ((c ^ ((tok & 1) << 2)) << 4), k_rows + off, s >= 0);
+            cp_async16(dst + HALF + tok * PITCH + ((c ^ (((tok >> 1) & 3) << 1)) << 4), v_rows + off, s >= 0);
         }
     }
     const uint8_t *at;
+    __device__ __forceinline__ void set(const uint8_t *stage, int) { at = stage; }
     __device__ __forceinline__ void get_k(int b, int u, int g, int t, uint4 (&k)[D / 32]) const
     {
 #pragma unroll
@@ -90,8 +88,8 @@ template <int D, int W>
 struct Rows4 {
     static constexpr bool FP4 = true;
     using Mma = VtkFp16;
-    static constexpr int WARPS = W, TILE = 32, PITCH = D / 2, HALF = TILE * PITCH, SCALES = D / 16, PIECES = D / 32;
-    static constexpr int STAGE = 2 * HALF + 2 * TILE * SCALES;
+    static constexpr int WARPS = W, GROUP = 8, TILE = 16, PITCH = D / 2, HALF = TILE * PITCH, SCALES = D / 16, PIECES = D / 32;
+    static constexpr int STAGE = 2 * HALF + 2 * TILE * 16;
     static __device__ __forceinline__ int kdim(int t, int j) { return (D / 4) * t + 8 * j; }
     static __device__ __forceinline__ int vdim(int g, int x) { return (D / 8) * g + 8 * x; }
     static __device__ __forceinline__ int vswizzle(int tok, int c) { return D == 128 ? c ^ ((tok >> 1) & 3) : c; }
@@ -103,17 +101,20 @@ struct Rows4 {
         for (int i = 0; i < TILE / PER; ++i) {
             const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
             const int64_t off = (s < 0 ? 0 : s) * row_bytes + head * PITCH + 16 * c;
-            cp_async<16>(dst + tok * PITCH + 16 * c, k_rows + off, s >= 0);
-            cp_async<16>(dst + HALF + tok * PITCH + 16 * vswizzle(tok, c), v_rows + off, s >= 0);
+            cp_async16(dst + tok * PITCH + 16 * c, k_rows + off, s >= 0);
+            cp_async16(dst + HALF + tok * PITCH + 16 * vswizzle(tok, c), v_rows + off, s >= 0);
         }
-        const int64_t off = (slot < 0 ? 0 : slot) * row_bytes + hkv * PITCH + head * SCALES;
-        cp_async<SCALES>(dst + 2 * HALF + lane * SCALES, k_rows + off, slot >= 0);
-        cp_async<SCALES>(dst + 2 * HALF + (TILE + lane) * SCALES, v_rows + off, slot >= 0);
+        // scales: the aligned 16 bytes that hold the head's; lanes 0 .. 15 of K, 16 .. 31 of V
+        const int sl = __shfl_sync(0xffffffffu, slot, lane & 15);
+        const int64_t off = (sl < 0 ? 0 : sl) * row_bytes + hkv * PITCH + ((head * SCALES) & ~15);
+        cp_async16(dst + 2 * HALF + lane * 16, (lane < TILE ? k_rows : v_rows) + off, sl >= 0);
     }
     const uint8_t *at;
+    int mine;                            // the head's scales in their 16 bytes
+    __device__ __forceinline__ void set(const uint8_t *stage, int head) { at = stage; mine = (head * SCALES) & 15; }
     __device__ __forceinline__ void get_k(int b, int u, int g, int t, uint4 (&k)[D / 32]) const
     {
-        const uint8_t *codes = at + (16 * b + 8 * u + g) * PITCH + t * (D / 8), *sc = at + 2 * HALF + (16 * b + 8 * u + g) * SCALES;
+        const uint8_t *codes = at + (16 * b + 8 * u + g) * PITCH + t * (D / 8), *sc = at + 2 * HALF + (16 * b + 8 * u + g) * 16 + mine;
         if (D == 128) {                  // words 0, 1 belong to the first of the lane's two groups, 2, 3 to the second
             const uint4 w = *reinterpret_cast<const uint4 *>(codes);
             const uint32_t two = vtk_scales_to_half2(*reinterpret_cast<const uint16_t *>(sc + 2 * t));
@@ -132,7 +133,7 @@ struct Rows4 {
     __device__ __forceinline__ void get_v(int b, int i, int g, int t, uint4 (&v)[D / 64]) const
     {
         const int tok = 16 * b + 2 * t + (i & 1) + 8 * (i >> 1);
-        const uint32_t s0 = __byte_perm(vtk_scales_to_half2(at[2 * HALF + (TILE + tok) * SCALES + (D == 128 ? g : g >> 1)]), 0, 0x1010);
+        const uint32_t s0 = __byte_perm(vtk_scales_to_half2(at[2 * HALF + (TILE + tok) * 16 + mine + (D == 128 ? g : g >> 1)]), 0, 0x1010);
         const uint8_t *codes = at + HALF + tok * PITCH;
         if (D == 128) {
             const uint2 w = *reinterpret_cast<const uint2 *>(codes + 16 * vswizzle(tok, g >> 1) + 8 * (g & 1));
@@ -147,7 +148,7 @@ struct Rows4 {
 // ring stages of a warp: what is left of 227 KB next to the join buffer, eight at most
 template <int NR, typename Rows, int D> constexpr int at_stages()
 {
-    constexpr int NW = Rows::WARPS, room = (231000 - 128 - NW * NR * 8 - NW * NR * D * 4) / NW / (Rows::STAGE + Rows::TILE * 4);
+    constexpr int NW = Rows::WARPS, room = (230900 - 128 - NW * NR * 8 - NW * NR * D * 4) / NW / (Rows::STAGE + Rows::TILE * 4);
     return room > 8 ? 8 : room;
 }
 
@@ -156,13 +157,33 @@ struct Shared {
     static constexpr int ST = at_stages<NR, Rows, D>(), NW = Rows::WARPS, NT = NW * 32;
     alignas(128) uint8_t ring[NW][ST][Rows::STAGE];
     alignas(16) union {
-        float o[NW][NR][D];        // join: 16-byte pieces of a row permuted by the row
-        struct { int prefix[NT + 1]; int warp_sum[NW], warp_segments[NW]; int segments; } plan;
+        float o[NW][NR * D];             // join: a warp's accumulators, 16 bytes a lane
+        struct { int warp_sum[NW], warp_segments[NW], start[NW], before[NW]; } plan;
     };
     float2 ml[NW][NR];
     int ids[NW][ST][Rows::TILE];
-    int last[NW];
+    int last[NW], bad[NW];
 };
+
+// (a 64-bit division is a subroutine of several hundred cycles)
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
+{
+    return ((uint64_t)(x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
+// query row -> token and head of the group (an integer division is forty instructions; the quotient in 32-bit floating point
+// is off by one at most)
+__device__ __forceinline__ void split_row(const VtkAttnArgs &a, int row, int64_t &tok, int &head)
+{
+    int q = row < (1 << 22) ? __float2int_rz((float)row * a.inv_group) : row / a.group, r = row - q * a.group;
+    if (r < 0) { --q; r += a.group; }
+    if (r >= a.group) { ++q; r -= a.group; }
+    tok = q;
+    head = r;
+}
+
+// what a part counts for next to a maximum
+__device__ __forceinline__ float weight(float m, float top) { return m == -INFINITY ? 0.f : (m == top ? 1.f : vtk_exp2(m - top)); }
 
 // one request as the cut sees it
 struct Known {
@@ -204,18 +225,18 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
 template <int NR, int TILE>
 struct Walk {
     Known *k;
-    int r, rt, kv, t0, t1;               // segment and its tiles [t0, t1) inside the share
+    int r, rt, hg, t0, t1;               // segment (hg: group of key heads) and its tiles [t0, t1) inside the share
     int64_t f, f1;                       // next tile of the row of all tiles, end of the share
     __device__ __forceinline__ void clip() { t1 = k->tiles - t0 < f1 - f ? k->tiles : t0 + (int)(f1 - f); }
     __device__ __forceinline__ bool done() const { return f >= f1; }
     static __device__ __forceinline__ bool in_window(int r, int r_known) { return r >= r_known && r - r_known < AT_KNOWN; }
-    __device__ __forceinline__ void next(const VtkAttnArgs &a, const Known *known, int r_known)
+    __device__ __forceinline__ void next(const VtkAttnArgs &a, int groups, const Known *known, int r_known)
     {
         f += t1 - t0;
         t0 = t1 = 0;
         if (done()) return;
-        if (++kv == a.hkv) {
-            kv = 0;
+        if (++hg == groups) {
+            hg = 0;
             if (++rt == k->row_tiles) {
                 rt = 0;
                 bool c = false;
@@ -261,54 +282,62 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         my_segments += own.tiles > 0 ? own.row_tiles : 0;
     }
     if (clipped && blockIdx.x == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
-    {
-        const int incl = vtk_warp_incl_scan(mine);
-        my_segments = __reduce_add_sync(0xffffffffu, my_segments);
-        if (lane == 31) {
-            sh.plan.warp_sum[warp] = incl;
-            sh.plan.warp_segments[warp] = my_segments;
-        }
-        __syncthreads();
-        int before = 0, all_segments = 0;
-        for (int w = 0; w < warp; ++w) before += sh.plan.warp_sum[w];
-        for (int w = 0; w < NW; ++w) all_segments += sh.plan.warp_segments[w];
-        if (tid == 0) sh.plan.segments = all_segments;
-        sh.plan.prefix[tid + 1] = before + incl;
-        if (tid == 0) sh.plan.prefix[0] = 0;
-        __syncthreads();
+    const int incl = vtk_warp_incl_scan(mine);
+    my_segments = __reduce_add_sync(0xffffffffu, my_segments);
+    if (lane == 31) {
+        sh.plan.warp_sum[warp] = incl;
+        sh.plan.warp_segments[warp] = my_segments;
     }
-    const int64_t W = (int64_t)sh.plan.prefix[NT] * a.hkv;
+    __syncthreads();
+    int before = 0, all_tiles = 0, all_segments = 0;
+    for (int w = 0; w < NW; ++w) {
+        before += w < warp ? sh.plan.warp_sum[w] : 0;
+        all_tiles += sh.plan.warp_sum[w];
+        all_segments += sh.plan.warp_segments[w];
+    }
+    before += incl - mine;                                   // tiles of the requests in front of the thread's
+
     // ---- teams: the fewer segments there are, the more warps share one ----
-    const int64_t segments = (int64_t)sh.plan.segments * a.hkv, warps = (int64_t)gridDim.x * NW;
-    int team = NW;                                           // warps of a team
-    if (segments * AT_PARTS >= warps) team = 1;
-    else if (segments * AT_PARTS * (NW / 4) >= warps) team = NW / 4;
-    else if (segments * AT_PARTS * (NW / 2) >= warps) team = NW / 2;
-    const int teams = NW / team, my_team = warp / team, tw = warp % team;
-    // at least AT_MIN_SHARE tiles a warp: a segment that is cut finer costs more to join than it gains
-    const int64_t most = (W + AT_MIN_SHARE * team - 1) / (AT_MIN_SHARE * team), G = most < (int64_t)gridDim.x * teams ? most : (int64_t)gridDim.x * teams;
+    int group = Rows::GROUP, lanes = 1, groups;
+    while (group > 1 && group / 2 >= a.hkv) group >>= 1;
+    for (;;) {
+        groups = (a.hkv + group - 1) / group;
+        if ((int64_t)all_segments * groups * AT_PARTS >= (int64_t)gridDim.x * (NW / (group * lanes))) break;
+        if (group * lanes < NW) lanes <<= 1;
+        else if (group > 1) { group >>= 1; lanes <<= 1; }
+        else break;
+    }
+    const int per_team = group * lanes, teams = NW / per_team, my_team = warp / per_team;
+    const int hl = warp / lanes % group, tw = warp % lanes;  // head of the group, lane of tokens
+    const int64_t W = (int64_t)all_tiles * groups;
+    // at least AT_MIN_SHARE tiles a lane: a segment that is cut finer costs more to join than it gains
+    const int64_t most = divide(W + AT_MIN_SHARE * lanes - 1, AT_MIN_SHARE * lanes), G = most < (int64_t)gridDim.x * teams ? most : (int64_t)gridDim.x * teams;
     const bool packed = G == (int64_t)gridDim.x * teams;     // a CTA's shares side by side; few shares: on different SMs
-    const int share0 = packed ? blockIdx.x * teams : blockIdx.x, share = packed ? share0 + my_team : my_team * gridDim.x + blockIdx.x;
-    auto find = [&](int64_t f) {                             // thread segment that holds tile f
-        const int at = (int)(f / a.hkv);                     // (in tiles of one key head)
-        int lo = 0, hi = NT;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (sh.plan.prefix[mid] <= at) lo = mid; else hi = mid;
+    auto share_at = [&](int team) { return packed ? blockIdx.x * teams + team : team * gridDim.x + blockIdx.x; };
+    const int share = share_at(my_team);
+    // the first `longer` shares have one tile more than the others
+    const int64_t size = G > 0 ? divide(W, G) : 0, longer = W - size * G;
+    auto start_of = [&](int64_t i) { return i * size + (i < longer ? i : longer); };
+    auto share_of = [&](int64_t f) { return (int)(f < longer * (size + 1) ? divide(f, size + 1) : longer + divide(f - longer * (size + 1), size)); };
+    for (int team = 0; team < teams; ++team) {               // the thread whose requests hold a share's first tile
+        if (share_at(team) >= G) break;
+        const int64_t f = start_of(share_at(team));
+        if (f >= (int64_t)before * groups && f < (int64_t)(before + mine) * groups) {
+            sh.plan.start[team] = tid;
+            sh.plan.before[team] = before;
         }
-        return lo;
-    };
+    }
+    __syncthreads();
     Walk<NR, TILE> use;
-    use.f = share < G ? W * share / G : 0;
-    use.f1 = share < G ? W * (share + 1) / G : 0;
+    use.f = share < G ? start_of(share) : 0;
+    use.f1 = share < G ? start_of(share + 1) : 0;
     use.k = &s_use[warp];
     int64_t left = 0;
     if (share < G) {
-        const int lo = find(use.f);
-        left = use.f - (int64_t)sh.plan.prefix[lo] * a.hkv;
-        use.r = lo * seg;
+        left = use.f - (int64_t)sh.plan.before[my_team] * groups;
+        use.r = sh.plan.start[my_team] * seg;
     }
-    const int known0 = G > 0 ? find(share0 < G ? W * share0 / G : 0) : 0;
+    const int known0 = G > share_at(0) ? sh.plan.start[0] : 0;
     if (seg == 1 && tid >= known0 && tid < known0 + AT_KNOWN && tid < R) s_known[tid - known0] = own;
     const int r_known = seg == 1 ? known0 : INT32_MAX;
     __syncthreads();                                         // the plan's arrays become the join buffers
@@ -316,7 +345,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     for (;; ++use.r) {
         bool c = false;
         const Known k = use.in_window(use.r, r_known) ? s_known[use.r - r_known] : look_up<NR, TILE>(a, use.r, c);
-        const int64_t all = (int64_t)k.tiles * k.row_tiles * a.hkv;
+        const int64_t all = (int64_t)k.tiles * k.row_tiles * groups;
         if (left < all) {
             if (lane == 0) s_use[warp] = s_get[warp] = k;
             __syncwarp();
@@ -324,14 +353,14 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         }
         left -= all;
     }
-    use.rt = (int)(left / ((int64_t)use.k->tiles * a.hkv));
-    left -= (int64_t)use.rt * use.k->tiles * a.hkv;
-    use.kv = (int)(left / use.k->tiles);
-    use.t0 = (int)(left - (int64_t)use.kv * use.k->tiles);
+    use.rt = (int)divide(left, (int64_t)use.k->tiles * groups);
+    left -= (int64_t)use.rt * use.k->tiles * groups;
+    use.hg = (int)divide(left, use.k->tiles);
+    use.t0 = (int)(left - (int64_t)use.hg * use.k->tiles);
     use.clip();
     auto team_sync = [&]() {
-        if (team == 1) __syncwarp();
-        else asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + my_team), "r"(team * 32) : "memory");
+        if (lanes == 1) __syncwarp();
+        else asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + warp / lanes), "r"(lanes * 32) : "memory");
     };
 
     // ---- the stream: this warp's tiles, ST - 1 ahead of their use, whatever segment they are of ----
@@ -345,7 +374,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     bool more = true;
     auto meta = [&]() {                                      // the warp's next tile: slots and ids of its tokens
         while (more && tile >= get.t1) {
-            get.next(a, s_known, r_known);
+            get.next(a, groups, s_known, r_known);
             more = !get.done();
             tile = get.t0 + tw;
         }
@@ -353,16 +382,16 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         n.slot = -1;
         n.id = INT32_MAX;
         n.pmax = n.floor = -1;
-        n.kv = get.kv;
+        n.kv = get.hg * group + hl;
         n.there = more;
         const int v = tile * TILE + lane;
-        if (more && lane < TILE && v < get.k->s.n) {
+        if (more && lane < TILE && v < get.k->s.n && n.kv < a.hkv) {
             n.slot = a.cache_slots[get.k->s.entry(v)];
             n.id = a.cache_ids.null() ? get.k->s.index(v) : a.cache_ids[get.k->s.entry(v)];
             n.pmax = get.k->pmax;
             n.floor = get.k->floor;
         }
-        tile += team;
+        tile += lanes;
         return n;
     };
     auto issue = [&](Next n) {
@@ -374,7 +403,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
             if (!vtk_sees(n.id, n.pmax, n.floor, a.sinks)) n.slot = -1;
             const int stage = issued % ST;
             if (lane < TILE) sh.ids[warp][stage][lane] = n.slot < 0 ? INT32_MAX : n.id;
-            Rows::issue(smem_u32(sh.ring[warp][stage]), a.k_rows, a.v_rows, a.row_bytes, a.hkv, n.kv, n.slot);
+            Rows::issue(vtk_smem_u32(sh.ring[warp][stage]), a.k_rows, a.v_rows, a.row_bytes, a.hkv, n.kv, n.slot);
             ++issued;
         }
         cp_commit();
@@ -390,9 +419,10 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     }
 
     int used = 0;
-    for (; !use.done(); use.next(a, s_known, r_known)) {
-        const int kv = use.kv, rt = use.rt;
-        const int rows = use.k->qn * a.group - rt * NR < NR ? use.k->qn * a.group - rt * NR : NR;
+    for (; !use.done(); use.next(a, groups, s_known, r_known)) {
+        const int kv = use.hg * group + hl, rt = use.rt;
+        const int rows = kv >= a.hkv ? 0 :              // (the last group may lack heads)
+             use.k->qn * a.group - rt * NR < NR ? use.k->qn * a.group - rt * NR : NR;
         // ---- queries: lane (g, t) holds of rows g and 8 + g the dimensions its K fragments hold ----
         uint4 q[RH][D / 32];
         int pos[RH], floor[RH];
@@ -404,10 +434,13 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
             scale[h] = a.scale_log2;
             const uint16_t *p = nullptr;
             if (row < rows) {
-                const int64_t tok = use.k->q0 + at / a.group;
+                int64_t tok;
+                int head;
+                split_row(a, at, tok, head);
+                tok += use.k->q0;
                 pos[h] = a.positions[tok];
                 floor[h] = vtk_floor(pos[h], a.window);
-                p = a.q + tok * a.q_stride + (int64_t)(kv * a.group + at % a.group) * D;
+                p = a.q + tok * a.q_stride + (int64_t)(kv * a.group + head) * D;
             }
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
@@ -457,14 +490,14 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
 #pragma unroll
         for (int h = 0; h < RH; ++h) { m[h] = -INFINITY; l[h] = 0.f; }
 
-        for (int tl = use.t0 + tw; tl < use.t1; tl += team, ++used) {
+        for (int tl = use.t0 + tw; tl < use.t1; tl += lanes, ++used) {
             cp_wait<ST - 2>();
             __syncwarp();
             issue(next);
             next = meta();
             const int stage = used % ST;
             Rows rows_now;
-            rows_now.at = sh.ring[warp][stage];
+            rows_now.set(sh.ring[warp][stage], kv);
             const int *ids = sh.ids[warp][stage];
             const int my_id = ids[lane & (TILE - 1)];
             if (!__any_sync(0xffffffffu, vtk_sees(my_id, pmax, floor_min, a.sinks))) continue;
@@ -566,98 +599,210 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
             }
         }
 
-        // ---- join the team's warps ----
-        auto piece = [](int row, int c) { return ((c ^ (row & 7)) << 2); };      // 16-byte piece c of a row
+        // ---- join the team's warps, pair by pair: fragments as they are, 16 bytes a thread ----
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-            if (t == 0) sh.ml[warp][g + 8 * h] = make_float2(m[h], l[h]);
-#pragma unroll
-            for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {                // query row 2t + e: eight consecutive dimensions
-                    const int row = 8 * h + 2 * t + e, c = Rows::vdim(g, x) / 4;
-                    *reinterpret_cast<float4 *>(&sh.o[warp][row][piece(row, c)]) = make_float4(o[4 * x][h][e], o[4 * x][h][2 + e], o[4 * x + 1][h][e], o[4 * x + 1][h][2 + e]);
-                    *reinterpret_cast<float4 *>(&sh.o[warp][row][piece(row, c + 1)]) = make_float4(o[4 * x + 2][h][e], o[4 * x + 2][h][2 + e], o[4 * x + 3][h][e], o[4 * x + 3][h][2 + e]);
-                }
         }
-        team_sync();
-        const int w0 = my_team * team;
+        for (int half = lanes / 2; half > 0; half >>= 1) {
+            if (tw >= half && tw < 2 * half) {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int h = 0; h < RH; ++h)
+                        *reinterpret_cast<float4 *>(&sh.o[warp][((i * RH + h) * 32 + lane) * 4]) = make_float4(o[i][h][0], o[i][h][1], o[i][h][2], o[i][h][3]);
+#pragma unroll
+                for (int h = 0; h < RH; ++h)
+                    if (t == 0) sh.ml[warp][g + 8 * h] = make_float2(m[h], l[h]);
+            }
+            team_sync();
+            if (tw < half) {
+                const int w = warp + half;
+#pragma unroll
+                for (int h = 0; h < RH; ++h) {
+                    const float2 ml = sh.ml[w][g + 8 * h];
+                    const float top = fmaxf(m[h], ml.x), f = weight(m[h], top), f2 = weight(ml.x, top);
+                    l[h] = l[h] * f + ml.y * f2;
+                    m[h] = top;
+                    const float a0 = __shfl_sync(0xffffffffu, f, 8 * t), a1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+                    const float b0 = __shfl_sync(0xffffffffu, f2, 8 * t), b1 = __shfl_sync(0xffffffffu, f2, 8 * t + 4);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const float4 x = *reinterpret_cast<const float4 *>(&sh.o[w][((i * RH + h) * 32 + lane) * 4]);
+                        o[i][h][0] = o[i][h][0] * a0 + x.x * b0;
+                        o[i][h][1] = o[i][h][1] * a1 + x.y * b1;
+                        o[i][h][2] = o[i][h][2] * a0 + x.z * b0;
+                        o[i][h][3] = o[i][h][3] * a1 + x.w * b1;
+                    }
+                }
+            }
+        }
+
+        // ---- the rows: finished, or a part of a longer segment ----
         const int64_t seg_lo = use.f - use.t0, seg_hi = seg_lo + use.k->tiles;
         const bool whole = use.t0 == 0 && use.t1 == use.k->tiles;
         // shares that hold parts of this segment, and where a share leaves its part
-        const int first = (int)(((seg_lo + 1) * G - 1) / W), parts = (int)((seg_hi * G - 1) / W) - first + 1;
-        auto part_at = [&](int i) { return a.part + (int64_t)(2 * i + (i == first)) * (NR * (D + 2)); };
-        auto finish = [&](int row, float (&acc)[N], float mm, float ll) {
-            const int at = rt * NR + row, head = kv * a.group + at % a.group;
-            const int64_t tok = use.k->q0 + at / a.group;
-            bool bad = !(fabsf(ll) < INFINITY);
+        const int first = share_of(seg_lo), parts = share_of(seg_hi - 1) - first + 1;
+        auto part_at = [&](int i) { return a.part + ((int64_t)(2 * i + (i == first)) * group + hl) * (NR * (D + 2)); };
+        auto query = [&](int row, int64_t &tok, int &head) { split_row(a, rt * NR + row, tok, head); tok += use.k->q0; head += kv * a.group; };
+        uint16_t *to[RH][2];                                 // rows 2t and 2t + 1 (+ 8) of the output, null: there is none
 #pragma unroll
-            for (int j = 0; j < N; ++j) bad |= !(fabsf(acc[j]) < INFINITY);
-            if (use.k->qn > 1 && __any_sync(0xffffffffu, bad))   // (one query token: what it does not see was not read)
-                vtk_row_again<D, Rows::FP4, Act>(a, tok, head, a.positions[tok], use.k->s.base, use.k->len, acc, mm, ll);
-            vtk_store_row<D, Act>(a, tok, head, acc, mm, ll);
+        for (int h = 0; h < RH; ++h)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                int64_t tok;
+                int head;
+                query(8 * h + 2 * t + e, tok, head);
+                to[h][e] = 8 * h + 2 * t + e < rows ? a.out + tok * a.out_stride + (int64_t)head * D + Rows::vdim(g, 0) : nullptr;
+            }
+        // m-tile i of the rows 2t and 2t + 1 (+ 8): two dimensions each
+        auto store = [&](int i, const float (&x)[RH][4], const float (&r)[RH][2]) {
+#pragma unroll
+            for (int h = 0; h < RH; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (to[h][e] != nullptr)
+                        *reinterpret_cast<uint32_t *>(to[h][e] + (Rows::vdim(0, i / 4) + 2 * (i % 4))) = Act::pack(x[h][e] * r[h][e], x[h][2 + e] * r[h][e]);
         };
-        for (int row = tw; row < rows; row += team) {
-            float mm = -INFINITY, ll = 0.f, acc[N];
+        auto finite = [](const float (&x)[RH][4]) {
+            bool ok = true;
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] = 0.f;
-            for (int w = w0; w < w0 + team; ++w) mm = fmaxf(mm, sh.ml[w][row].x);
-#pragma unroll 4
-            for (int w = w0; w < w0 + team; ++w) {
-                const float2 ml = sh.ml[w][row];
-                const float f = ml.x == -INFINITY ? 0.f : (ml.x == mm ? 1.f : vtk_exp2(ml.x - mm));
-                ll += f * ml.y;
-                const float *src = &sh.o[w][row][piece(row, lane * N / 4) + (lane * N) % 4];
+            for (int h = 0; h < RH; ++h)
 #pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] += f * src[j];
-            }
-            if (!whole) {
-                float *dst = part_at(share) + row * D + lane * N;
-                if (N == 4) *reinterpret_cast<float4 *>(dst) = make_float4(acc[0], acc[1], acc[N - 2], acc[N - 1]);
-                else *reinterpret_cast<float2 *>(dst) = make_float2(acc[0], acc[1]);
-                if (lane == 0) *reinterpret_cast<float2 *>(part_at(share) + NR * D + 2 * row) = make_float2(mm, ll);
-            } else {
-                finish(row, acc, mm, ll);
-            }
-        }
-        if (!whole) {
-            __threadfence();
-            team_sync();
-            if (tw == 0 && lane == 0) {
-                const bool last = atomicAdd(&a.counters[first], 1u) == (unsigned)(parts - 1);
-                if (last) a.counters[first] = 0;             // ready for the next call
-                sh.last[my_team] = last;
-            }
-            team_sync();
-            if (*(volatile int *)&sh.last[my_team]) {
-                __threadfence();
-                for (int row = tw; row < rows; row += team) {
-                    float mm = -INFINITY, ll = 0.f, acc[N];
+                for (int e = 0; e < 4; ++e) ok &= fabsf(x[h][e]) < INFINITY;
+            return ok;
+        };
+        auto totals = [&](const float (&mm)[RH], const float (&ll)[RH], bool write, float (&r)[RH][2], bool &ok) {
 #pragma unroll
-                    for (int j = 0; j < N; ++j) acc[j] = 0.f;
-                    for (int i = lane; i < parts; i += 32) mm = fmaxf(mm, __ldcg(part_at(first + i) + NR * D + 2 * row));
-#pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, d));
-#pragma unroll 8
-                    for (int i = 0; i < parts; ++i) {
-                        const float *src = part_at(first + i);
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(src + NR * D + 2 * row));
-                        const float f = ml.x == -INFINITY ? 0.f : (ml.x == mm ? 1.f : vtk_exp2(ml.x - mm));
-                        ll += f * ml.y;
-                        src += row * D + lane * N;
-                        if (N == 4) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(src));
-                            acc[0] += f * x.x; acc[1] += f * x.y; acc[N - 2] += f * x.z; acc[N - 1] += f * x.w;
-                        } else {
-                            const float2 x = __ldcg(reinterpret_cast<const float2 *>(src));
-                            acc[0] += f * x.x; acc[1] += f * x.y;
-                        }
-                    }
-                    finish(row, acc, mm, ll);
+            for (int h = 0; h < RH; ++h) {
+                const float f = ll[h] == 0.f ? 0.f : a.v_mul / ll[h];
+                ok &= fabsf(ll[h]) < INFINITY;
+                r[h][0] = __shfl_sync(0xffffffffu, f, 8 * t);
+                r[h][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+                if (write && a.lse != nullptr && t == 0 && g + 8 * h < rows) {
+                    int64_t tok;
+                    int head;
+                    query(g + 8 * h, tok, head);
+                    a.lse[tok * a.hq + head] = ll[h] == 0.f ? -INFINITY : (mm[h] + log2f(ll[h])) * 0.69314718055994531f;
                 }
             }
+        };
+        // rows that a masked NaN may have reached (with one query token what it does not see was not read)
+        auto again = [&]() {
+            for (int row = tw; row < rows; row += lanes) {
+                int64_t tok;
+                int head;
+                query(row, tok, head);
+                float acc[N], mm, ll;
+                vtk_row_again<D, Rows::FP4, Act>(a, tok, head, a.positions[tok], use.k->s.base, use.k->len, acc, mm, ll);
+                vtk_store_row<D, Act>(a, tok, head, acc, mm, ll);
+            }
+        };
+        bool bad = false;
+        if (rows <= 0) {                                     // a head that is not there: its warps only keep step
+            if (!whole) team_sync();
+        } else if (whole) {
+            if (tw == 0) {
+                bool ok = true;
+                float r[RH][2];
+                totals(m, l, true, r, ok);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    ok &= finite(o[i]);
+                    store(i, o[i], r);
+                }
+                bad = !__all_sync(0xffffffffu, ok);
+            }
+        } else {
+            if (tw == 0) {
+                float *dst = part_at(share);
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int h = 0; h < RH; ++h)
+                        __stcg(reinterpret_cast<float4 *>(dst + ((i * RH + h) * 32 + lane) * 4), make_float4(o[i][h][0], o[i][h][1], o[i][h][2], o[i][h][3]));
+#pragma unroll
+                for (int h = 0; h < RH; ++h)
+                    if (t == 0) __stcg(reinterpret_cast<float2 *>(dst + NR * D + 2 * (g + 8 * h)), make_float2(m[h], l[h]));
+                __syncwarp();
+                if (lane == 0) {                             // (the warp's writes are released with the arrival, the others' acquired)
+                    uint32_t *counter = a.counters + first * group + hl, seen;
+                    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(seen) : "l"(counter) : "memory");
+                    const bool last = seen == (unsigned)(parts - 1);
+                    if (last) *counter = 0;                  // ready for the next call
+                    sh.last[warp] = last;
+                }
+            }
+            team_sync();
+            if (*(volatile int *)&sh.last[warp - tw]) {
+                float mm[RH], ll[RH];
+                float2 ml0[4][RH];                           // (nearly always all there are)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int h = 0; h < RH; ++h)
+                        ml0[k][h] = __ldcg(reinterpret_cast<const float2 *>(part_at(first + (k < parts ? k : 0)) + NR * D + 2 * (g + 8 * h)));
+#pragma unroll
+                for (int h = 0; h < RH; ++h) {
+                    mm[h] = fmaxf(fmaxf(ml0[0][h].x, ml0[1][h].x), fmaxf(ml0[2][h].x, ml0[3][h].x));
+                    ll[h] = 0.f;
+                }
+                for (int i = 4; i < parts; ++i)
+#pragma unroll
+                    for (int h = 0; h < RH; ++h) mm[h] = fmaxf(mm[h], __ldcg(part_at(first + i) + NR * D + 2 * (g + 8 * h)));
+                // lane w of the head: the m-tiles w, w + lanes, ..., as many at a time as the registers hold
+                bool ok = true, counted = false;
+                float r[RH][2];
+                constexpr int AT_ONCE = NR == 8 && NW == 8 ? 8 : 4;
+                for (int i0 = tw; i0 < MT; i0 += AT_ONCE * lanes) {
+                    float acc[AT_ONCE][RH][4];
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                        for (int h = 0; h < RH; ++h)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][h][e] = 0.f;
+#pragma unroll 3
+                    for (int k = 0; k < parts; ++k) {
+                        const float *src = part_at(first + k);
+#pragma unroll
+                        for (int h = 0; h < RH; ++h) {
+                            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(src + NR * D + 2 * (g + 8 * h)));
+                            const float f = weight(ml.x, mm[h]);
+                            if (!counted) ll[h] += f * ml.y;
+                            const float f0 = __shfl_sync(0xffffffffu, f, 8 * t), f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+#pragma unroll
+                            for (int i = 0; i < AT_ONCE; ++i)
+                                if (i0 + i * lanes < MT) {
+                                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + (((i0 + i * lanes) * RH + h) * 32 + lane) * 4));
+                                    acc[i][h][0] += f0 * x.x;
+                                    acc[i][h][1] += f1 * x.y;
+                                    acc[i][h][2] += f0 * x.z;
+                                    acc[i][h][3] += f1 * x.w;
+                                }
+                        }
+                    }
+                    if (!counted) totals(mm, ll, tw == 0, r, ok);
+                    counted = true;
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i)
+                        if (i0 + i * lanes < MT) {
+                            ok &= finite(acc[i]);
+                            store(i0 + i * lanes, acc[i], r);
+                        }
+                }
+                bad = !__all_sync(0xffffffffu, ok);
+            }
+        }
+        if (use.k->qn > 1 && rows > 0) {
+            if (lanes > 1) {                                 // one lane's finding is the head's
+                if (lane == 0) sh.bad[warp] = bad;
+                team_sync();
+                bad = false;
+                for (int w = warp - tw; w < warp - tw + lanes; ++w) bad |= *(volatile int *)&sh.bad[w] != 0;
+            }
+            if (bad) again();
         }
         team_sync();                                         // the join buffers are used by the next segment
     }
@@ -669,7 +814,8 @@ int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, cudaStream_t st)
     auto kernel = attention_rows_kernel<D, NR, Rows, Act, SPLIT_P>;
     constexpr int smem = (int)sizeof(Shared<D, NR, Rows>);
     static_assert(Shared<D, NR, Rows>::ST >= 2 && smem + sizeof(Known) * (AT_KNOWN + 2 * Rows::WARPS) <= 232448, "shared memory of a CTA");
-    VTK_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static std::atomic<int> allowed{-1};                     // the device that knows of this kernel's shared memory
+    VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed, (const void *)kernel, smem));
     VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(ctx->num_sms), dim3(Rows::WARPS * 32), smem, st, a));
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
@@ -679,7 +825,7 @@ template <int D, typename Act>
 int launch_by_type(vtoken_ctx *ctx, bool fp4, bool wide, const VtkAttnArgs &a, cudaStream_t st)
 {
     constexpr bool bf = Act::kind == VTOKEN_KV_BF16;
-    if (fp4) return wide ? launch<D, 16, Rows4<D, 8>, Act, !bf>(ctx, a, st) : launch<D, 8, Rows4<D, 12>, Act, !bf>(ctx, a, st);
+    if (fp4) return wide ? launch<D, 16, Rows4<D, 8>, Act, !bf>(ctx, a, st) : launch<D, 8, Rows4<D, 16>, Act, !bf>(ctx, a, st);
     return wide ? launch<D, 16, Rows16<D, Act>, Act, true>(ctx, a, st) : launch<D, 8, Rows16<D, Act>, Act, true>(ctx, a, st);
 }
 
@@ -693,13 +839,13 @@ float two_to(int e)
 
 }  // namespace
 
-// A share leaves at most two partial row tiles (8 rows a tile from up to 12 teams a CTA, or 16 from up to 8).
+// A share leaves parts of at most two segments for each of its heads; shares times heads are at most 16 a CTA with 8
+// rows, 8 with 16.
 int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs *a)
 {
-    const int64_t shares = (int64_t)ctx->num_sms * 12;
-    const int64_t counters = (shares * 4 + 15) / 16 * 16 + 16;       // and the prompt kernel's two tickets in front
+    const int64_t shares = (int64_t)ctx->num_sms * 16, counters = shares * 4 + 16;       // (the prompt kernel's two tickets in front)
     if (a) a->part = (float *)((uint8_t *)(a->counters - 4) + counters);
-    return counters + shares * 2 * (16 * 8 / 12 + 1) * (heads->head_dim + 2) * 4;
+    return counters + shares * 2 * 8 * (heads->head_dim + 2) * 4;
 }
 
 int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st)
@@ -756,6 +902,7 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     a.hq = heads->num_q_heads;
     a.hkv = heads->num_kv_heads;
     a.group = heads->num_q_heads / heads->num_kv_heads;
+    a.inv_group = 1.f / (float)a.group;
     a.window = in->window;
     a.sinks = in->window > 0 ? in->sinks : 0;
     a.scale_log2 = in->sm_scale * 1.4426950408889634f * two_to(heads->k_exponent);

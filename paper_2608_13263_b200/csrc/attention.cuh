@@ -1,6 +1,8 @@
 // What the attention kernels share: arguments, the request's share of the slot cache, matrix instructions,
 // rows of the pools in registers, and the exact recomputation of a row that a masked NaN reached.
 #pragma once
+#include <atomic>
+
 #include "heads.cuh"
 
 struct VtkAttnArgs {
@@ -12,6 +14,7 @@ struct VtkAttnArgs {
     const uint8_t *k_rows, *v_rows;      // this layer's slabs
     int64_t q_stride, out_stride, row_bytes, slots_per_layer, max_tokens;
     int32_t max_requests, max_query_tokens, hq, hkv, group;
+    float inv_group;
     int32_t window, sinks;
     float scale_log2;                    // sm_scale * log2(e) * 2^k_exponent
     float v_mul;                         // 2^v_exponent
@@ -118,6 +121,45 @@ __device__ __forceinline__ uint4 vtk_ldg16(const void *p)
     return w;
 }
 
+// ---- barriers in shared memory; every wait ends ----------------------------------------------------
+__device__ __forceinline__ uint32_t vtk_smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void vtk_mbar_init(uint64_t *bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(vtk_smem_u32(bar)), "r"(count));
+}
+__device__ __forceinline__ void vtk_mbar_arrive(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ bool vtk_mbar_try(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(vtk_smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t vtk_global_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+// false when the phase did not complete within the limit, or another role has given up
+static __device__ __noinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
+{
+    const uint64_t t0 = vtk_global_ns();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (vtk_mbar_try(bar, parity)) return true;
+        if (*abort) return false;
+        if (vtk_global_ns() - t0 > limit_ns) { *abort = 1; return false; }
+    }
+}
+__device__ __forceinline__ bool vtk_mbar_wait(uint64_t *bar, uint32_t parity, uint64_t limit_ns, int *abort)
+{
+    return vtk_mbar_try(bar, parity) || vtk_mbar_try(bar, parity) || vtk_mbar_wait_long(bar, parity, limit_ns, abort);
+}
+
 // ---- one head of one pool row, `N` consecutive values from `d` on, as 32-bit values -------------
 // (the value without 2^exponent)
 template <int D, bool FP4, typename Act, int N>
@@ -205,6 +247,15 @@ __device__ __forceinline__ void vtk_store_row(const VtkAttnArgs &a, int64_t q_ro
     if (N == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[N / 2 - 1]);
     else p[0] = w[0];
     if (a.lse != nullptr && lane == 0) a.lse[q_row * a.hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// host: large shared memory, asked for when a kernel first runs on a device (the call costs as much as a launch)
+inline cudaError_t vtk_allow_smem(const vtoken_ctx *ctx, std::atomic<int> &allowed, const void *kernel, int bytes)
+{
+    if (allowed.load(std::memory_order_relaxed) == ctx->device) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) allowed.store(ctx->device, std::memory_order_relaxed);
+    return e;
 }
 
 // host: launchers of attention.cu and of attention_prompt.cu

@@ -51,48 +51,10 @@ struct Shared {
     int abort;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint64_t *bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ uint64_t global_ns()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-// false when the phase did not complete within the limit, or another role has given up
-__device__ __noinline__ bool mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
-{
-    const uint64_t t0 = global_ns();
-    for (;;) {
-        for (int i = 0; i < 64; ++i)
-            if (mbar_try(bar, parity)) return true;
-        if (*abort) return false;
-        if (global_ns() - t0 > limit_ns) { *abort = 1; return false; }
-    }
-}
-__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, uint64_t limit_ns, int *abort)
-{
-    return mbar_try(bar, parity) || mbar_try(bar, parity) || mbar_wait_long(bar, parity, limit_ns, abort);
-}
-
 // ---- tcgen05 -------------------------------------------------------------------------------------
 __device__ __forceinline__ void tc_commit(uint64_t *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
@@ -247,22 +209,22 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     using Mma = typename std::conditional<FP4, VtkFp16, Act>::type;
     constexpr int PANEL = AP_TILE * 128, PIECES = D / 8;
     extern __shared__ uint8_t raw[];
-    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw + ((1024 - (vtk_smem_u32(raw) & 1023)) & 1023));
     vtk_release_successor();
     vtk_wait_for_predecessor();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     // ---- once per CTA: barriers, tensor memory, pairs of tiles per request ----
     if (tid == 0) {
-        for (int i = 0; i < AP_STAGES; ++i) { mbar_init(&sh.kv_full[i], 128); mbar_init(&sh.kv_empty[i], 1); }
-        for (int x = 0; x < 2; ++x) { mbar_init(&sh.s_full[x], 1); mbar_init(&sh.p_full[x], 128); mbar_init(&sh.o_full[x], 1); }
-        mbar_init(&sh.q_full, 128);
-        mbar_init(&sh.drain, 1);
+        for (int i = 0; i < AP_STAGES; ++i) { vtk_mbar_init(&sh.kv_full[i], 128); vtk_mbar_init(&sh.kv_empty[i], 1); }
+        for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x], 128); vtk_mbar_init(&sh.o_full[x], 1); }
+        vtk_mbar_init(&sh.q_full, 128);
+        vtk_mbar_init(&sh.drain, 1);
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 12) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(vtk_smem_u32(&sh.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     int R = *a.num_requests;
@@ -321,11 +283,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             bool ok = true;
             if (x == 0 || two) {
                 if (FP4 && T > 0) {                                              // row scales come with the queries
-                    ok = __all_sync(0xffffffffu, mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort));
+                    ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort));
                     c = scale * sh.row_scale[x][row];
                 }
                 for (int j = 0; j < T && ok; ++j) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort));
+                    ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.s_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort));
                     if (!ok) break;
                     tc_after_sync();
                     const Meta &mt = sh.meta[(tile_count + j) % AP_META];
@@ -387,9 +349,9 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     l += sum;
                     tc_wait_st();
                     tc_before_sync();
-                    mbar_arrive(&sh.p_full[x]);
+                    vtk_mbar_arrive(&sh.p_full[x]);
                 }
-                if (ok && T > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort));
+                if (ok && T > 0) ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort));
                 if (ok) {
                     if (T > 0) tc_after_sync();
                     const float r = l == 0.f ? 0.f : a.v_mul / l;
@@ -448,7 +410,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         const bool there = row < it.rows;
                         const uint16_t *src = a.q;
                         if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D + 8 * piece;
-                        cp_async16(smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
+                        cp_async16(vtk_smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
                     }
                     cp_commit();
                 } else {
@@ -480,11 +442,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                                 for (int e = 0; e < 8; ++e) v[e] *= up;
                                 w = vtk_pack8<VtkFp16>(v);
                             }
-                            st_shared16(smem_u32(sh.q[x]) + swizzled(pt, i), w);
+                            st_shared16(vtk_smem_u32(sh.q[x]) + swizzled(pt, i), w);
                         }
                     }
                     async_proxy_fence();
-                    mbar_arrive(&sh.q_full);
+                    vtk_mbar_arrive(&sh.q_full);
                 }
                 const int pmin = two && it.pmin[1] < it.pmin[0] ? it.pmin[1] : it.pmin[0];
                 const int pmax = two && it.pmax[1] > it.pmax[0] ? it.pmax[1] : it.pmax[0];
@@ -501,7 +463,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 };
                 fetch(0);
                 int owed = -1, q_owed = !FP4;                      // 16-bit: a stage (the queries) whose copies are in flight
-                auto deliver = [&](int stage) { async_proxy_fence(); mbar_arrive(&sh.kv_full[stage]); };
+                auto deliver = [&](int stage) { async_proxy_fence(); vtk_mbar_arrive(&sh.kv_full[stage]); };
                 for (int j = 0; j < T; ++j) {
                     if (slot >= a.slots_per_layer) {
                         atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
@@ -510,7 +472,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (slot < 0) id = INT32_MAX;
                     Meta &mt = sh.meta[(tile_count + j) % AP_META];
                     const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
-                    bool ok = mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                    bool ok = vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
                     // (K two tiles ago is consumed, so both softmaxes are past the tile whose meta this overwrites)
                     const bool any = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks);
                     mt.ids[pt] = id;
@@ -528,12 +490,12 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t stage = which ? stage_v : stage_k;
                         if (which) {
-                            ok = mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                            ok = vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
                             ok = producers_agree(ok);
                             if (!ok) break;
                         }
                         const uint8_t *rows = which ? a.v_rows : a.k_rows;
-                        const uint32_t dst = smem_u32(sh.kv[stage]);
+                        const uint32_t dst = vtk_smem_u32(sh.kv[stage]);
                         if (!FP4) {
                             const int piece = pt % PIECES;
 #pragma unroll 4
@@ -544,7 +506,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             }
                             cp_commit();
                             cp_wait<1>();
-                            if (q_owed) { async_proxy_fence(); mbar_arrive(&sh.q_full); q_owed = 0; }
+                            if (q_owed) { async_proxy_fence(); vtk_mbar_arrive(&sh.q_full); q_owed = 0; }
                             if (owed >= 0) deliver(owed);
                             owed = (int)stage;
                         } else {
@@ -583,19 +545,19 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 }
                 if (!FP4) {
                     cp_wait<0>();
-                    if (q_owed) { async_proxy_fence(); mbar_arrive(&sh.q_full); }
+                    if (q_owed) { async_proxy_fence(); vtk_mbar_arrive(&sh.q_full); }
                     if (owed >= 0) deliver(owed);
                 }
             }
         } else if (warp == 12) {
             // ================= products: one thread =================
             if (lane == 0 && T > 0) {
-                bool ok = mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort);
+                bool ok = vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort);
                 auto wait_tile = [&](uint32_t cc) {
-                    return mbar_wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1, limit_ns, &sh.abort);
+                    return vtk_mbar_wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1, limit_ns, &sh.abort);
                 };
                 auto scores = [&](int x, uint32_t cc) {
-                    const uint32_t qa = smem_u32(sh.q[x]), ka = smem_u32(sh.kv[cc % AP_STAGES]);
+                    const uint32_t qa = vtk_smem_u32(sh.q[x]), ka = vtk_smem_u32(sh.kv[cc % AP_STAGES]);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t off = (k / 4) * PANEL + (k % 4) * 32;
@@ -604,7 +566,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     tc_commit(&sh.s_full[x]);
                 };
                 auto outputs = [&](int x, uint32_t cc, bool first) {
-                    const uint32_t va = smem_u32(sh.kv[cc % AP_STAGES]);
+                    const uint32_t va = vtk_smem_u32(sh.kv[cc % AP_STAGES]);
 #pragma unroll
                     for (int k = 0; k < AP_TILE / 16; ++k)
                         tc_mma_ts(tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + 8 * k, operand(va + k * 16 * 128), idesc_o, !first || k > 0);
@@ -619,7 +581,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 for (int j = 0; j < T && ok; ++j) {
                     const uint32_t ck = kv_count + 2 * j, cv = ck + 1;
                     for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-                        ok = mbar_wait(&sh.p_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort);
+                        ok = vtk_mbar_wait(&sh.p_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort);
                         if (ok && x == 0) ok = wait_tile(cv);
                         if (!ok) break;
                         tc_after_sync();
@@ -639,8 +601,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 }
                 if (!ok) {                                           // what was issued ends before the tensor memory goes
                     tc_commit(&sh.drain);
-                    const uint64_t t0 = global_ns();
-                    while (!mbar_try(&sh.drain, 0) && global_ns() - t0 < limit_ns) {}
+                    const uint64_t t0 = vtk_global_ns();
+                    while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < limit_ns) {}
                 }
             }
             __syncwarp();
@@ -671,7 +633,8 @@ int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_
     constexpr int smem = (int)sizeof(Shared<D>) + 1024;
     static_assert(smem <= 232448, "shared memory of a CTA");
     auto kernel = attention_prompt_kernel<D, FP4, Act>;
-    VTK_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    static std::atomic<int> allowed{-1};                     // the device that knows of this kernel's shared memory
+    VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed, (const void *)kernel, smem));
     // the sign of the scores' factor goes into the product (a zero factor: one that no 32-bit score can be seen through)
     const float scale = a.scale_log2 == 0.f ? 7.9e-31f : (a.scale_log2 < 0.f ? -a.scale_log2 : a.scale_log2);
     VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(ctx->num_sms), dim3(AP_NT), smem, st, a, tickets, a.row_limit,

@@ -144,8 +144,9 @@ __device__ __forceinline__ uint64_t vtk_global_ns()
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
     return t;
 }
+// (inlined: a call would keep the compiler from giving the roles of a kernel register counts of their own)
 // false when the phase did not complete within the limit, or another role has given up
-static __device__ __noinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
+static __device__ __forceinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
 {
     const uint64_t t0 = vtk_global_ns();
     for (;;) {

@@ -21,6 +21,8 @@
 
 namespace {
 
+constexpr int AP_REGS_SOFTMAX = 192, AP_REGS_LOAD = 80, AP_REGS_REST = 48;
+static_assert(2 * AP_REGS_SOFTMAX + AP_REGS_LOAD + AP_REGS_REST <= 4 * 128, "the registers that the block is launched with");
 constexpr int AP_NT = 512, AP_STAGES = 4, AP_TILE = 128, AP_META = 4;
 
 struct Item {                            // what one CTA works on
@@ -32,7 +34,7 @@ struct Item {                            // what one CTA works on
 };
 
 struct Meta {                            // what the softmax needs of a tile's tokens
-    int ids[AP_TILE];
+    alignas(16) int ids[AP_TILE];
     uint32_t every[2][4];                // bit: the token is seen by every row of the tile
 };
 
@@ -46,7 +48,7 @@ struct Shared {
     Item item[2];
     int prefix[AP_NT + 1];
     int warp_sum[AP_NT / 32];
-    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], s_full[2], p_full[2], o_full[2], q_full, drain;
+    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], s_full[2], p_full[2][2], o_full[2], q_full, drain;
     uint32_t tmem;
     int abort;
 };
@@ -68,7 +70,35 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
 }
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// ... with the registers that the load wrote: nothing that reads them comes before the wait
+#define P8(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
+__device__ __forceinline__ void tc_wait_ld(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : P8(r, 0), P8(r, 8), P8(r, 16), P8(r, 24) : : "memory");
+}
+__device__ __forceinline__ void tc_wait_ld(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : P8(r, 0), P8(r, 8) : : "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// two 32-bit operations an instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return *reinterpret_cast<float2 *>(&d);
+}
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 #define R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
@@ -80,11 +110,10 @@ __device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t (&r)[32])
                  "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
                  : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24) : "r"(addr));
 }
-__device__ __forceinline__ void tc_st32(uint32_t addr, const uint32_t (&r)[32])
+__device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t (&r)[16])
 {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,"
-                 "%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-                 ::"r"(addr), W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24) : "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : R8(r, 0), R8(r, 8) : "r"(addr));
 }
 __device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16])
 {
@@ -217,7 +246,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     // ---- once per CTA: barriers, tensor memory, pairs of tiles per request ----
     if (tid == 0) {
         for (int i = 0; i < AP_STAGES; ++i) { vtk_mbar_init(&sh.kv_full[i], 128); vtk_mbar_init(&sh.kv_empty[i], 1); }
-        for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x], 128); vtk_mbar_init(&sh.o_full[x], 1); }
+        for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x][0], 128); vtk_mbar_init(&sh.p_full[x][1], 128); vtk_mbar_init(&sh.o_full[x], 1); }
         vtk_mbar_init(&sh.q_full, 128);
         vtk_mbar_init(&sh.drain, 1);
         sh.abort = 0;
@@ -262,15 +291,27 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     const uint32_t idesc_s = IDESC | ((uint32_t)(AP_TILE >> 3) << 17) | ((uint32_t)negate << 13);
     constexpr uint32_t idesc_o = IDESC | ((uint32_t)(D >> 3) << 17) | (1u << 16);
 
-    for (;; ++item_count) {
-        __syncthreads();
-        const Item &it = sh.item[item_count & 1];
-        if (it.none || *(volatile int *)&sh.abort) break;
-        const int T = it.tiles;
-        const bool two = it.rows > AP_TILE;
-
-        if (warp < 8) {
-            // ================= softmax: thread = row =================
+    // Every role runs its own loop over the items, in step with the others at the items' ends.
+    auto each_item = [&](auto &&body) {
+        for (;; ++item_count) {
+            asm volatile("barrier.cta.sync 0, 512;" ::: "memory");
+            const Item &it = sh.item[item_count & 1];
+            if (it.none || *(volatile int *)&sh.abort) break;
+            const int T = it.tiles;
+            const bool two = it.rows > AP_TILE;
+            body(it, T, two);
+            kv_count += 2 * T;
+            tile_count += T;
+            s_count[0] += T;                                         // the second tile's barriers move only when there is one
+            s_count[1] += two ? T : 0;
+            if (T > 0) { ++q_count; ++o_count[0]; o_count[1] += two; }
+        }
+    };
+    // (registers of the launch, 128 a thread, are shared out again: a softmax thread holds a row of scores)
+    if (warp < 8) {
+        // ================= softmax: thread = row =================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(AP_REGS_SOFTMAX));
+        each_item([&](const Item &it, int T, bool two) {
             const int x = warp >> 2, row = tid & 127;
             const uint32_t lanes = (uint32_t)(warp & 3) << 21;                   // 32 lanes a warp
             const uint32_t t_s = tmem + lanes + x * AP_TILE, t_o = tmem + lanes + 2 * AP_TILE + x * D;
@@ -291,22 +332,40 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (!ok) break;
                     tc_after_sync();
                     const Meta &mt = sh.meta[(tile_count + j) % AP_META];
-                    uint32_t s[32];
-                    float top = -INFINITY;
+                    uint32_t vis[4];                                             // bit: this row sees the token
+                    bool all = true;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        tc_ld32(t_s + 32 * q, s);
-                        tc_wait_ld();
-                        const uint32_t every = mt.every[x][q];
-                        if (every == 0xffffffffu) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[i]));
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (vtk_sees(mt.ids[32 * q + i], pos, floor, a.sinks)) top = fmaxf(top, __uint_as_float(s[i]));
+                        vis[q] = mt.every[x][q];
+                        if (vis[q] != 0xffffffffu) {
+                            all = false;
+                            vis[q] = 0;
+#pragma unroll 1
+                            for (int i = 0; i < 32; i += 4) {
+                                const int4 id = *reinterpret_cast<const int4 *>(&mt.ids[32 * q + i]);
+                                const uint32_t four = (uint32_t)vtk_sees(id.x, pos, floor, a.sinks) | (uint32_t)vtk_sees(id.y, pos, floor, a.sinks) << 1 |
+                                                      (uint32_t)vtk_sees(id.z, pos, floor, a.sinks) << 2 | (uint32_t)vtk_sees(id.w, pos, floor, a.sinks) << 3;
+                                vis[q] |= four << i;
+                            }
                         }
                     }
+                    // scores: a quarter on its way while the maximum of the one before is taken
+                    uint32_t s[4][32];
+                    float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    tc_ld32(t_s, s[0]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        tc_wait_ld(s[q]);
+                        if (q < 3) tc_ld32(t_s + 32 * (q + 1), s[q + 1]);
+                        if (!all) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!((vis[q] >> i) & 1u)) s[q][i] = 0xff800000u;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) top4[(i >> 1) & 3] = max3(top4[(i >> 1) & 3], __uint_as_float(s[q][i]), __uint_as_float(s[q][i + 1]));
+                    }
+                    const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
                     const bool up = (top - m) * c > 8.f || (m == -INFINITY && top > -INFINITY);
                     if (__any_sync(0xffffffffu, up)) {
                         const float next = fmaxf(m, top);
@@ -315,41 +374,39 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         l *= f;
                         if (j > 0) {                                             // the products up to j - 1 are complete: S j came after them
 #pragma unroll
-                            for (int q = 0; q < D / 32; ++q) {
-                                tc_ld32(t_o + 32 * q, s);
-                                tc_wait_ld();
+                            for (int q = 0; q < D / 16; ++q) {
+                                uint32_t o[16];
+                                tc_ld16(t_o + 16 * q, o);
+                                tc_wait_ld(o);
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) s[i] = __float_as_uint(__uint_as_float(s[i]) * f);
-                                tc_st32(t_o + 32 * q, s);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tc_st16(t_o + 16 * q, o);
                             }
-                            tc_wait_st();
                         }
                     }
                     const float mc = m == -INFINITY ? 0.f : m * c;
-                    float sum = 0.f;
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        tc_ld32(t_s + 32 * q, s);
-                        tc_wait_ld();
-                        const uint32_t every = mt.every[x][q];
-                        if (every != 0xffffffffu) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!vtk_sees(mt.ids[32 * q + i], pos, floor, a.sinks)) s[i] = 0xff800000u;
-                        }
                         uint32_t p[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float p0 = vtk_exp2(fmaf(__uint_as_float(s[2 * i]), c, -mc)), p1 = vtk_exp2(fmaf(__uint_as_float(s[2 * i + 1]), c, -mc));
-                            sum += p0 + p1;
-                            p[i] = Mma::pack(p0, p1);
+                            float2 y = fma2(make_float2(__uint_as_float(s[q][2 * i]), __uint_as_float(s[q][2 * i + 1])), c2, mc2);
+                            y.x = vtk_exp2(y.x);
+                            y.y = vtk_exp2(y.y);
+                            sum[i & 1] = add2(sum[i & 1], y);
+                            p[i] = Mma::pack(y.x, y.y);
                         }
                         tc_st16(t_s + 16 * q, p);
+                        if (q & 1) {                                             // half of P: the product over it can start
+                            tc_wait_st();
+                            tc_before_sync();
+                            vtk_mbar_arrive(&sh.p_full[x][q >> 1]);
+                        }
                     }
-                    l += sum;
-                    tc_wait_st();
-                    tc_before_sync();
-                    vtk_mbar_arrive(&sh.p_full[x]);
+                    sum[0] = add2(sum[0], sum[1]);
+                    l += sum[0].x + sum[0].y;
                 }
                 if (ok && T > 0) ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort));
                 if (ok) {
@@ -362,7 +419,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         uint32_t o[32];
                         if (T > 0) {
                             tc_ld32(t_o + 32 * q, o);
-                            tc_wait_ld();
+                            tc_wait_ld(o);
                         }
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
@@ -398,8 +455,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     tc_before_sync();
                 }
             }
-        } else if (warp < 12) {
-            // ================= producers =================
+        });
+    } else if (warp < 12) {
+        // ================= producers =================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_LOAD));
+        each_item([&](const Item &it, int T, bool two) {
             if (T > 0) {
                 const int pt = tid - 256;
                 // queries, rows of both tiles
@@ -461,32 +521,67 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         id = a.cache_ids.null() ? it.span.index(v) : a.cache_ids[it.span.entry(v)];
                     }
                 };
-                fetch(0);
-                int owed = -1, q_owed = !FP4;                      // 16-bit: a stage (the queries) whose copies are in flight
-                auto deliver = [&](int stage) { async_proxy_fence(); vtk_mbar_arrive(&sh.kv_full[stage]); };
-                for (int j = 0; j < T; ++j) {
+                auto tell = [&](int j) {                           // it, to the other producers and the softmax
                     if (slot >= a.slots_per_layer) {
                         atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
                         slot = -1;
                     }
                     if (slot < 0) id = INT32_MAX;
                     Meta &mt = sh.meta[(tile_count + j) % AP_META];
-                    const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
-                    bool ok = vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
-                    // (K two tiles ago is consumed, so both softmaxes are past the tile whose meta this overwrites)
-                    const bool any = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks);
                     mt.ids[pt] = id;
-                    sh.slots[j & 1][pt] = any ? (int)slot : -1;
+                    sh.slots[j & 1][pt] = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks) ? (int)slot : -1;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const bool every = vtk_sees(id, it.pmin[x], vtk_floor(it.pmax[x], a.window), a.sinks);
-                        const unsigned bits = __ballot_sync(0xffffffffu, every);
+                        const unsigned bits = __ballot_sync(0xffffffffu, vtk_sees(id, it.pmin[x], vtk_floor(it.pmax[x], a.window), a.sinks));
                         if (lane == 0) mt.every[x][warp - 8] = bits;
                     }
+                };
+                // 4-bit rows: four threads a token, a quarter of its codes and scales each, fetched one operand ahead
+                constexpr int QW = D / 32;                         // words of 8 codes a thread
+                struct Raw { uint32_t w[QW], sc; };
+                Raw raw[2][4];                                     // K, V
+                const int part = pt & 3;
+                auto fetch_rows = [&](int which, int j) {
+                    const uint8_t *rows = which ? a.v_rows : a.k_rows;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t sl = sh.slots[j & 1][(pt >> 2) + 32 * i];
+                        Raw &r = raw[which][i];
+#pragma unroll
+                        for (int k = 0; k < QW; ++k) r.w[k] = 0;
+                        r.sc = 0;
+                        if (sl < 0) continue;
+                        const uint8_t *src = rows + sl * a.row_bytes;
+                        const uint8_t *codes = src + it.kv * (D / 2) + part * (D / 8);
+                        const uint8_t *scales = src + a.hkv * (D / 2) + it.kv * (D / 16) + part * (D / 64);
+                        if (D == 128) {
+                            const uint4 q4 = vtk_ldg16(codes);
+                            r.w[0] = q4.x; r.w[1] = q4.y; r.w[QW - 2] = q4.z; r.w[QW - 1] = q4.w;
+                            r.sc = __ldg(reinterpret_cast<const uint16_t *>(scales));
+                        } else {
+                            const uint2 q2 = __ldg(reinterpret_cast<const uint2 *>(codes));
+                            r.w[0] = q2.x; r.w[1] = q2.y;
+                            r.sc = __ldg(scales);
+                        }
+                    }
+                };
+                fetch(0);
+                int owed = -1, q_owed = !FP4;                      // 16-bit: a stage (the queries) whose copies are in flight
+                auto deliver = [&](int stage) { async_proxy_fence(); vtk_mbar_arrive(&sh.kv_full[stage]); };
+                for (int j = 0; j < T; ++j) {
+                    const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
+                    bool ok = vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                    // K two tiles ago is consumed, so both softmaxes are past tile j - 3, whose place the next tile's meta takes
+                    if (j == 0) {
+                        tell(0);
+                        if (T > 1) fetch(1);
+                    }
+                    if (j + 1 < T) tell(j + 1);
                     ok = producers_agree(ok);
                     if (!ok) break;
-                    if (j + 1 < T) fetch(j + 1);
-#pragma unroll 1
+                    if (j + 2 < T) fetch(j + 2);
+                    if (FP4 && j == 0) fetch_rows(0, 0);
+#pragma unroll
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t stage = which ? stage_v : stage_k;
                         if (which) {
@@ -500,9 +595,9 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             const int piece = pt % PIECES;
 #pragma unroll 4
                             for (int row = pt / PIECES; row < AP_TILE; row += 128 / PIECES) {
-                                const int64_t s = sh.slots[j & 1][row];
-                                const uint8_t *src = rows + (s < 0 ? 0 : s) * a.row_bytes + ((int64_t)it.kv * D + 8 * piece) * 2;
-                                cp_async16(dst + swizzled(row, piece), src, s >= 0);
+                                const int64_t sl = sh.slots[j & 1][row];
+                                const uint8_t *src = rows + (sl < 0 ? 0 : sl) * a.row_bytes + ((int64_t)it.kv * D + 8 * piece) * 2;
+                                cp_async16(dst + swizzled(row, piece), src, sl >= 0);
                             }
                             cp_commit();
                             cp_wait<1>();
@@ -510,33 +605,15 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             if (owed >= 0) deliver(owed);
                             owed = (int)stage;
                         } else {
-                            // four threads a token: a quarter of its codes and scales each
-                            constexpr int QW = D / 32;                   // words of 8 codes a thread
-                            const int part = pt & 3;
-#pragma unroll 2
-                            for (int row = pt >> 2; row < AP_TILE; row += 32) {
-                                const int64_t s = sh.slots[j & 1][row];
-                                uint32_t w[QW], sc = 0;
+                            if (which == 0) fetch_rows(1, j);
+                            else if (j + 1 < T) fetch_rows(0, j + 1);
 #pragma unroll
-                                for (int i = 0; i < QW; ++i) w[i] = 0;
-                                if (s >= 0) {
-                                    const uint8_t *src = rows + s * a.row_bytes;
-                                    const uint8_t *codes = src + it.kv * (D / 2) + part * (D / 8);
-                                    const uint8_t *scales = src + a.hkv * (D / 2) + it.kv * (D / 16) + part * (D / 64);
-                                    if (D == 128) {
-                                        const uint4 q4 = vtk_ldg16(codes);
-                                        w[0] = q4.x; w[1] = q4.y; w[QW - 2] = q4.z; w[QW - 1] = q4.w;
-                                        sc = __ldg(reinterpret_cast<const uint16_t *>(scales));
-                                    } else {
-                                        const uint2 q2 = __ldg(reinterpret_cast<const uint2 *>(codes));
-                                        w[0] = q2.x; w[1] = q2.y;
-                                        sc = __ldg(scales);
-                                    }
-                                }
-                                const uint32_t two_scales = vtk_scales_to_half2(sc);
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t two_scales = vtk_scales_to_half2(raw[which][i].sc);
 #pragma unroll
-                                for (int i = 0; i < QW; ++i)
-                                    st_shared16(dst + swizzled(row, part * QW + i), vtk_expand8(w[i], __byte_perm(two_scales, 0, i < 2 ? 0x1010 : 0x3232)));
+                                for (int k = 0; k < QW; ++k)
+                                    st_shared16(dst + swizzled((pt >> 2) + 32 * i, part * QW + k),
+                                                vtk_expand8(raw[which][i].w[k], __byte_perm(two_scales, 0, k < 2 ? 0x1010 : 0x3232)));
                             }
                             deliver((int)stage);
                         }
@@ -549,8 +626,12 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (owed >= 0) deliver(owed);
                 }
             }
-        } else if (warp == 12) {
-            // ================= products: one thread =================
+        });
+    } else if (warp == 12) {
+        // ================= products: one thread =================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_REST));
+        each_item([&](const Item &it, int T, bool two) {
+            (void)it;
             if (lane == 0 && T > 0) {
                 bool ok = vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort);
                 auto wait_tile = [&](uint32_t cc) {
@@ -565,11 +646,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     }
                     tc_commit(&sh.s_full[x]);
                 };
-                auto outputs = [&](int x, uint32_t cc, bool first) {
+                auto outputs = [&](int x, uint32_t cc, int half, bool first) {
                     const uint32_t va = vtk_smem_u32(sh.kv[cc % AP_STAGES]);
 #pragma unroll
-                    for (int k = 0; k < AP_TILE / 16; ++k)
+                    for (int i = 0; i < AP_TILE / 32; ++i) {
+                        const int k = half * (AP_TILE / 32) + i;
                         tc_mma_ts(tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + 8 * k, operand(va + k * 16 * 128), idesc_o, !first || k > 0);
+                    }
                 };
                 ok = ok && wait_tile(kv_count);
                 if (ok) {
@@ -581,11 +664,15 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 for (int j = 0; j < T && ok; ++j) {
                     const uint32_t ck = kv_count + 2 * j, cv = ck + 1;
                     for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-                        ok = vtk_mbar_wait(&sh.p_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort);
+                        ok = vtk_mbar_wait(&sh.p_full[x][0], (s_count[x] + j) & 1, limit_ns, &sh.abort);
                         if (ok && x == 0) ok = wait_tile(cv);
                         if (!ok) break;
                         tc_after_sync();
-                        outputs(x, cv, j == 0);
+                        outputs(x, cv, 0, j == 0);
+                        ok = vtk_mbar_wait(&sh.p_full[x][1], (s_count[x] + j) & 1, limit_ns, &sh.abort);
+                        if (!ok) break;
+                        tc_after_sync();
+                        outputs(x, cv, 1, j == 0);
                         const bool last_x = x == 1 || !two;
                         if (last_x) tc_commit(&sh.kv_empty[cv % AP_STAGES]);
                         if (j + 1 < T) {
@@ -606,14 +693,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 }
             }
             __syncwarp();
-        } else if (warp == 13) {
-            next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
-        }
-        kv_count += 2 * T;
-        tile_count += T;
-        s_count[0] += T;                                             // the second tile's barriers move only when there is one
-        s_count[1] += two ? T : 0;
-        if (T > 0) { ++q_count; ++o_count[0]; o_count[1] += two; }
+        });
+    } else {
+        // ================= warp 13: the next item (14 and 15 only make up the warpgroup) =================
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_REST));
+        each_item([&](const Item &, int, bool) {
+            if (warp == 13) next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
+        });
     }
     __syncthreads();
     if (tid == 0) {

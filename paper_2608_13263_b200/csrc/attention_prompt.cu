@@ -54,19 +54,29 @@ struct Shared {
 };
 
 // ---- tcgen05 -------------------------------------------------------------------------------------
-__device__ __forceinline__ void tc_commit(uint64_t *bar)
+// (these four are called by a whole warp, in uniform control flow, so that their operands can stay in uniform registers; `one`
+// picks the lane that issues)
+__device__ __forceinline__ bool tc_elect()
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
+    uint32_t r;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void tc_commit(bool one, uint64_t *bar)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    if (one) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void tc_mma_ss(bool one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    if (one)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(bool one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    if (one)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+                     ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -628,69 +638,72 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             }
         });
     } else if (warp == 12) {
-        // ================= products: one thread =================
+        // ================= products: one thread issues them =================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_REST));
+        const bool one = tc_elect();
+        const uint32_t q_addr = vtk_smem_u32(sh.q), kv_addr = vtk_smem_u32(sh.kv);
         each_item([&](const Item &it, int T, bool two) {
             (void)it;
-            if (lane == 0 && T > 0) {
-                bool ok = vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort);
-                auto wait_tile = [&](uint32_t cc) {
-                    return vtk_mbar_wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1, limit_ns, &sh.abort);
-                };
-                auto scores = [&](int x, uint32_t cc) {
-                    const uint32_t qa = vtk_smem_u32(sh.q[x]), ka = vtk_smem_u32(sh.kv[cc % AP_STAGES]);
+            if (T == 0) return;
+            const uint32_t k0 = kv_count;
+            auto wait = [&](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, vtk_mbar_wait(bar, parity, limit_ns, &sh.abort)); };
+            auto wait_tile = [&](uint32_t cc) { return wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1); };
+            auto scores = [&](int x, uint32_t cc) {
+                const uint64_t qd = operand(q_addr) + (uint64_t)(x * (D / 64) * PANEL >> 4);
+                const uint64_t kd = operand(kv_addr) + (uint64_t)((cc % AP_STAGES) * (D / 64) * PANEL >> 4);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = (k / 4) * PANEL + (k % 4) * 32;
-                        tc_mma_ss(tmem + x * AP_TILE, operand(qa + off), operand(ka + off), idesc_s, k > 0);
-                    }
-                    tc_commit(&sh.s_full[x]);
-                };
-                auto outputs = [&](int x, uint32_t cc, int half, bool first) {
-                    const uint32_t va = vtk_smem_u32(sh.kv[cc % AP_STAGES]);
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t off = ((k / 4) * PANEL + (k % 4) * 32) >> 4;
+                    tc_mma_ss(one, tmem + x * AP_TILE, qd + off, kd + off, idesc_s, k > 0);
+                }
+                tc_commit(one, &sh.s_full[x]);
+            };
+            auto outputs = [&](int x, uint32_t cc, int half, bool first) {
+                const uint64_t vd = operand(kv_addr) + (uint64_t)((cc % AP_STAGES) * (D / 64) * PANEL >> 4);
 #pragma unroll
-                    for (int i = 0; i < AP_TILE / 32; ++i) {
-                        const int k = half * (AP_TILE / 32) + i;
-                        tc_mma_ts(tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + 8 * k, operand(va + k * 16 * 128), idesc_o, !first || k > 0);
-                    }
-                };
-                ok = ok && wait_tile(kv_count);
-                if (ok) {
+                for (int i = 0; i < AP_TILE / 32; ++i) {
+                    const int k = half * (AP_TILE / 32) + i;
+                    tc_mma_ts(one, tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + 8 * k, vd + (k * 16 * 128 >> 4), idesc_o, !first || k > 0);
+                }
+            };
+            bool ok = wait(&sh.q_full, q_count & 1) && wait_tile(k0);
+            if (ok) {
+                tc_after_sync();
+                scores(0, k0);
+                if (two) scores(1, k0);
+                tc_commit(one, &sh.kv_empty[k0 % AP_STAGES]);
+            }
+            for (int j = 0; j < T && ok; ++j) {
+                const uint32_t ck = k0 + 2 * j, cv = ck + 1;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (!ok || (x == 1 && !two)) break;
+                    ok = wait(&sh.p_full[x][0], (s_count[x] + j) & 1);
+                    if (ok && x == 0) ok = wait_tile(cv);
+                    if (!ok) break;
                     tc_after_sync();
-                    scores(0, kv_count);
-                    if (two) scores(1, kv_count);
-                    tc_commit(&sh.kv_empty[kv_count % AP_STAGES]);
-                }
-                for (int j = 0; j < T && ok; ++j) {
-                    const uint32_t ck = kv_count + 2 * j, cv = ck + 1;
-                    for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-                        ok = vtk_mbar_wait(&sh.p_full[x][0], (s_count[x] + j) & 1, limit_ns, &sh.abort);
-                        if (ok && x == 0) ok = wait_tile(cv);
+                    outputs(x, cv, 0, j == 0);
+                    ok = wait(&sh.p_full[x][1], (s_count[x] + j) & 1);
+                    if (!ok) break;
+                    tc_after_sync();
+                    outputs(x, cv, 1, j == 0);
+                    const bool last_x = x == 1 || !two;
+                    if (last_x) tc_commit(one, &sh.kv_empty[cv % AP_STAGES]);
+                    if (j + 1 < T) {
+                        if (x == 0) ok = wait_tile(ck + 2);
                         if (!ok) break;
                         tc_after_sync();
-                        outputs(x, cv, 0, j == 0);
-                        ok = vtk_mbar_wait(&sh.p_full[x][1], (s_count[x] + j) & 1, limit_ns, &sh.abort);
-                        if (!ok) break;
-                        tc_after_sync();
-                        outputs(x, cv, 1, j == 0);
-                        const bool last_x = x == 1 || !two;
-                        if (last_x) tc_commit(&sh.kv_empty[cv % AP_STAGES]);
-                        if (j + 1 < T) {
-                            if (x == 0) ok = wait_tile(ck + 2);
-                            if (!ok) break;
-                            tc_after_sync();
-                            scores(x, ck + 2);
-                            if (last_x) tc_commit(&sh.kv_empty[(ck + 2) % AP_STAGES]);
-                        } else {
-                            tc_commit(&sh.o_full[x]);
-                        }
+                        scores(x, ck + 2);
+                        if (last_x) tc_commit(one, &sh.kv_empty[(ck + 2) % AP_STAGES]);
+                    } else {
+                        tc_commit(one, &sh.o_full[x]);
                     }
                 }
-                if (!ok) {                                           // what was issued ends before the tensor memory goes
-                    tc_commit(&sh.drain);
-                    const uint64_t t0 = vtk_global_ns();
-                    while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < limit_ns) {}
-                }
+            }
+            if (!ok) {                                               // what was issued ends before the tensor memory goes
+                tc_commit(one, &sh.drain);
+                const uint64_t t0 = vtk_global_ns();
+                while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < limit_ns) {}
             }
             __syncwarp();
         });

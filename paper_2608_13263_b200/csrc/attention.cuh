@@ -138,6 +138,14 @@ __device__ __forceinline__ bool vtk_mbar_try(uint64_t *bar, uint32_t parity)
                  : "=r"(ok) : "r"(vtk_smem_u32(bar)), "r"(parity) : "memory");
     return ok != 0;
 }
+// without waiting at all (try_wait may sleep for a while)
+__device__ __forceinline__ bool vtk_mbar_test(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(vtk_smem_u32(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ uint64_t vtk_global_ns()
 {
     uint64_t t;

@@ -34,9 +34,21 @@ struct Item {                            // what one CTA works on
 };
 
 struct Meta {                            // what the softmax needs of a tile's tokens
-    alignas(16) int ids[AP_TILE];
+    int ids[AP_TILE];                    // ascending, INT32_MAX behind the last
     uint32_t every[2][4];                // bit: the token is seen by every row of the tile
+    uint32_t there[4];                   // bit: the token has a slot in the pool
 };
+
+// entries of a tile's ascending ids that are <= p
+__device__ __forceinline__ int ids_up_to(const int *ids, int p)
+{
+    int n = 0;
+#pragma unroll
+    for (int step = AP_TILE / 2; step > 0; step >>= 1)
+        if (ids[n + step - 1] <= p) n += step;
+    return n + (ids[n] <= p);            // (n is 127 at most here)
+}
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); }
 
 template <int D>
 struct Shared {
@@ -349,24 +361,20 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         vis[q] = mt.every[x][q];
                         if (vis[q] != 0xffffffffu) {
                             all = false;
-                            vis[q] = 0;
-#pragma unroll 1
-                            for (int i = 0; i < 32; i += 4) {
-                                const int4 id = *reinterpret_cast<const int4 *>(&mt.ids[32 * q + i]);
-                                const uint32_t four = (uint32_t)vtk_sees(id.x, pos, floor, a.sinks) | (uint32_t)vtk_sees(id.y, pos, floor, a.sinks) << 1 |
-                                                      (uint32_t)vtk_sees(id.z, pos, floor, a.sinks) << 2 | (uint32_t)vtk_sees(id.w, pos, floor, a.sinks) << 3;
-                                vis[q] |= four << i;
-                            }
                         }
                     }
-                    // scores: a quarter on its way while the maximum of the one before is taken
+                    if (!all) {                                                  // ids ascend: what the row sees is a range, and the sinks
+                        const int hi = ids_up_to(mt.ids, pos), lo = floor < 0 ? 0 : ids_up_to(mt.ids, floor), sk = lo == 0 || a.sinks == 0 ? 0 : ids_up_to(mt.ids, a.sinks - 1);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) vis[q] = mt.there[q] & low_bits(hi - 32 * q) & (~low_bits(lo - 32 * q) | low_bits(sk - 32 * q));
+                    }
                     uint32_t s[4][32];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tc_ld32(t_s + 32 * q, s[q]);
                     float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    tc_ld32(t_s, s[0]);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        tc_wait_ld(s[q]);
-                        if (q < 3) tc_ld32(t_s + 32 * (q + 1), s[q + 1]);
+                        tc_wait_ld(s[q]);                                        // (the first waits for all four)
                         if (!all) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
@@ -536,13 +544,14 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
                         slot = -1;
                     }
-                    if (slot < 0) id = INT32_MAX;
                     Meta &mt = sh.meta[(tile_count + j) % AP_META];
                     mt.ids[pt] = id;
                     sh.slots[j & 1][pt] = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks) ? (int)slot : -1;
+                    const unsigned there = __ballot_sync(0xffffffffu, slot >= 0);
+                    if (lane == 0) mt.there[warp - 8] = there;
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const unsigned bits = __ballot_sync(0xffffffffu, vtk_sees(id, it.pmin[x], vtk_floor(it.pmax[x], a.window), a.sinks));
+                        const unsigned bits = __ballot_sync(0xffffffffu, slot >= 0 && vtk_sees(id, it.pmin[x], vtk_floor(it.pmax[x], a.window), a.sinks));
                         if (lane == 0) mt.every[x][warp - 8] = bits;
                     }
                 };
@@ -648,6 +657,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             const uint32_t k0 = kv_count;
             auto wait = [&](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, vtk_mbar_wait(bar, parity, limit_ns, &sh.abort)); };
             auto wait_tile = [&](uint32_t cc) { return wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1); };
+            auto come = [&](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, vtk_mbar_test(bar, parity)); };
+            auto tile_come = [&](uint32_t cc) { return come(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1); };
             auto scores = [&](int x, uint32_t cc) {
                 const uint64_t qd = operand(q_addr) + (uint64_t)(x * (D / 64) * PANEL >> 4);
                 const uint64_t kd = operand(kv_addr) + (uint64_t)((cc % AP_STAGES) * (D / 64) * PANEL >> 4);
@@ -673,31 +684,49 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 if (two) scores(1, k0);
                 tc_commit(one, &sh.kv_empty[k0 % AP_STAGES]);
             }
-            for (int j = 0; j < T && ok; ++j) {
-                const uint32_t ck = k0 + 2 * j, cv = ck + 1;
+            // Whichever row tile has (half of) its P goes on: step 2 j of a row tile is the first half of its product over
+            // V j, step 2 j + 1 the second half and the scores over K j + 1.
+            int step[2] = {0, two ? 0 : 2 * T}, v_there = 0, k_there = 1;       // tiles of V and K that have come
+            uint64_t idle = 0;
+            while (ok && (step[0] < 2 * T || step[1] < 2 * T)) {
+                bool any = false;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if (!ok || (x == 1 && !two)) break;
-                    ok = wait(&sh.p_full[x][0], (s_count[x] + j) & 1);
-                    if (ok && x == 0) ok = wait_tile(cv);
-                    if (!ok) break;
-                    tc_after_sync();
-                    outputs(x, cv, 0, j == 0);
-                    ok = wait(&sh.p_full[x][1], (s_count[x] + j) & 1);
-                    if (!ok) break;
-                    tc_after_sync();
-                    outputs(x, cv, 1, j == 0);
-                    const bool last_x = x == 1 || !two;
-                    if (last_x) tc_commit(one, &sh.kv_empty[cv % AP_STAGES]);
-                    if (j + 1 < T) {
-                        if (x == 0) ok = wait_tile(ck + 2);
-                        if (!ok) break;
-                        tc_after_sync();
-                        scores(x, ck + 2);
-                        if (last_x) tc_commit(one, &sh.kv_empty[(ck + 2) % AP_STAGES]);
-                    } else {
-                        tc_commit(one, &sh.o_full[x]);
+                    if (step[x] >= 2 * T) continue;
+                    const int j = step[x] >> 1, half = step[x] & 1;
+                    const uint32_t ck = k0 + 2 * j, cv = ck + 1;
+                    // (nothing waits here: the row tile that is ahead may need a stage that the other one has still to use)
+                    if (!come(&sh.p_full[x][half], (s_count[x] + j) & 1)) continue;
+                    if (half == 0 && v_there <= j) {
+                        if (!tile_come(cv)) continue;
+                        v_there = j + 1;
                     }
+                    if (half == 1 && j + 1 < T && k_there <= j + 1) {
+                        if (!tile_come(ck + 2)) continue;
+                        k_there = j + 2;
+                    }
+                    any = true;
+                    tc_after_sync();
+                    outputs(x, cv, half, j == 0);
+                    if (half == 1) {
+                        const bool last = !two || step[x ^ 1] > step[x];        // the other row tile is past V j already
+                        if (last) tc_commit(one, &sh.kv_empty[cv % AP_STAGES]);
+                        if (j + 1 < T) {
+                            scores(x, ck + 2);
+                            if (last) tc_commit(one, &sh.kv_empty[(ck + 2) % AP_STAGES]);
+                        } else {
+                            tc_commit(one, &sh.o_full[x]);
+                        }
+                    }
+                    ++step[x];
+                }
+                if (any) {
+                    idle = 0;
+                } else if (idle == 0) {
+                    idle = vtk_global_ns();
+                } else if (__any_sync(0xffffffffu, *(volatile int *)&sh.abort || vtk_global_ns() - idle > limit_ns)) {
+                    *(volatile int *)&sh.abort = 1;
+                    ok = false;
                 }
             }
             if (!ok) {                                               // what was issued ends before the tensor memory goes

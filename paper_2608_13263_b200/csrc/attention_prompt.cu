@@ -55,7 +55,7 @@ struct Shared {
     uint8_t q[2][D / 64][AP_TILE * 128];
     uint8_t kv[AP_STAGES][D / 64][AP_TILE * 128];
     Meta meta[AP_META];
-    int slots[2][AP_TILE];               // the producers' tile: slot, -1 = zeros
+    int slots[AP_META][AP_TILE];         // the producers' tiles: slot, -1 = zeros (the next tile's are written while the last one's may be read)
     float row_scale[2][AP_TILE];
     Item item[2];
     int prefix[AP_NT + 1];
@@ -160,8 +160,14 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool t
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// the barrier gets this thread's arrival when its copies so far have landed: nobody waits for them here
+__device__ __forceinline__ void cp_arrive(uint64_t *bar)
+{
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Shared memory written by threads (cp.async too) is read by the tensor cores through another path: this fence stands between the two,
+// in the thread that issues the products, behind its wait for the tile (or in the threads that wrote, before they arrive).
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // barrier of the 128 producers that tells all of them whether all said yes
 __device__ __forceinline__ bool producers_agree(bool yes)
@@ -490,7 +496,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D + 8 * piece;
                         cp_async16(vtk_smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
                     }
-                    cp_commit();
+                    cp_arrive(&sh.q_full);
                 } else {
                     for (int x = 0; x < (two ? 2 : 1); ++x) {
                         const int row = x * AP_TILE + pt, at = it.first + row;
@@ -546,7 +552,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     }
                     Meta &mt = sh.meta[(tile_count + j) % AP_META];
                     mt.ids[pt] = id;
-                    sh.slots[j & 1][pt] = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks) ? (int)slot : -1;
+                    sh.slots[j % AP_META][pt] = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks) ? (int)slot : -1;
                     const unsigned there = __ballot_sync(0xffffffffu, slot >= 0);
                     if (lane == 0) mt.there[warp - 8] = there;
 #pragma unroll
@@ -564,7 +570,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     const uint8_t *rows = which ? a.v_rows : a.k_rows;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int64_t sl = sh.slots[j & 1][(pt >> 2) + 32 * i];
+                        const int64_t sl = sh.slots[j % AP_META][(pt >> 2) + 32 * i];
                         Raw &r = raw[which][i];
 #pragma unroll
                         for (int k = 0; k < QW; ++k) r.w[k] = 0;
@@ -585,7 +591,6 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     }
                 };
                 fetch(0);
-                int owed = -1, q_owed = !FP4;                      // 16-bit: a stage (the queries) whose copies are in flight
                 auto deliver = [&](int stage) { async_proxy_fence(); vtk_mbar_arrive(&sh.kv_full[stage]); };
                 for (int j = 0; j < T; ++j) {
                     const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
@@ -604,9 +609,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t stage = which ? stage_v : stage_k;
                         if (which) {
-                            ok = vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
-                            ok = producers_agree(ok);
-                            if (!ok) break;
+                            // (all agree on the outcome at the next tile; after an abort it does not matter what is overwritten)
+                            vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
                         }
                         const uint8_t *rows = which ? a.v_rows : a.k_rows;
                         const uint32_t dst = vtk_smem_u32(sh.kv[stage]);
@@ -614,15 +618,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             const int piece = pt % PIECES;
 #pragma unroll 4
                             for (int row = pt / PIECES; row < AP_TILE; row += 128 / PIECES) {
-                                const int64_t sl = sh.slots[j & 1][row];
+                                const int64_t sl = sh.slots[j % AP_META][row];
                                 const uint8_t *src = rows + (sl < 0 ? 0 : sl) * a.row_bytes + ((int64_t)it.kv * D + 8 * piece) * 2;
                                 cp_async16(dst + swizzled(row, piece), src, sl >= 0);
                             }
-                            cp_commit();
-                            cp_wait<1>();
-                            if (q_owed) { async_proxy_fence(); vtk_mbar_arrive(&sh.q_full); q_owed = 0; }
-                            if (owed >= 0) deliver(owed);
-                            owed = (int)stage;
+                            cp_arrive(&sh.kv_full[stage]);
                         } else {
                             if (which == 0) fetch_rows(1, j);
                             else if (j + 1 < T) fetch_rows(0, j + 1);
@@ -637,13 +637,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             deliver((int)stage);
                         }
                     }
-                    if (!ok) break;
                 }
-                if (!FP4) {
-                    cp_wait<0>();
-                    if (q_owed) { async_proxy_fence(); vtk_mbar_arrive(&sh.q_full); }
-                    if (owed >= 0) deliver(owed);
-                }
+                if (!FP4) cp_wait_all();                           // (they have: the products are done or, after an abort, waited for here)
             }
         });
     } else if (warp == 12) {
@@ -679,6 +674,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             };
             bool ok = wait(&sh.q_full, q_count & 1) && wait_tile(k0);
             if (ok) {
+                async_proxy_fence();
                 tc_after_sync();
                 scores(0, k0);
                 if (two) scores(1, k0);
@@ -700,10 +696,12 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (half == 0 && v_there <= j) {
                         if (!tile_come(cv)) continue;
                         v_there = j + 1;
+                        async_proxy_fence();
                     }
                     if (half == 1 && j + 1 < T && k_there <= j + 1) {
                         if (!tile_come(ck + 2)) continue;
                         k_there = j + 2;
+                        async_proxy_fence();
                     }
                     any = true;
                     tc_after_sync();

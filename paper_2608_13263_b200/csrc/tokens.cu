@@ -3,11 +3,9 @@
 // the projections.
 //
 // Bound by HBM: a token's q, k and v are read once, q and the two rows written once, about 8 flops a value.
-// Layout: a lane holds 8 consecutive values of a head (one 16-byte load), D / 8 lanes a head, so the mean
-// square is log2(D / 8) shuffles, an interleaved pair is in one lane and the partner of a (i, i + rot / 2) pair
-// is one shuffle away.  A warp takes four rounds of heads of one token: its loads are all requested before the
-// first is used and the token's cosines and sines (32 bits each, four times the bytes of a head's values per
-// lane) are loaded once for all of them.
+// Layout: a lane holds 8 values of a head, D / 8 lanes a head, so the mean square is log2(D / 8) shuffles.  A warp
+// takes four rounds of heads of one token: its loads are all requested before the first is used and the token's
+// cosines and sines (32 bits each, four times the bytes of a head's values per lane) are loaded once for all of them.
 #include "heads.cuh"
 
 namespace {
@@ -110,14 +108,150 @@ __device__ __forceinline__ void quantise(const float (&x)[8], uint32_t &codes, u
     }
 }
 
-template <int D, bool FP4, typename Act>
-__global__ void __launch_bounds__(WT_WARPS * 32) write_tokens_kernel(WriteArgs a)
+// ---- 16-bit rows: two 32-bit operations an instruction, partners of a rotation in one lane ------
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return *reinterpret_cast<float2 *>(&d);
+}
+
+// A lane holds 8 values of a head as two runs of four: runs whose dimensions are rotation partners where pairs are
+// (i, i + rot / 2), neighbouring runs elsewhere -- so that no rotation needs a shuffle.  Measured with 8 consecutive values a
+// lane, partners fetched by shuffles and one operation an instruction, 16 384 tokens of 36 heads took 104 us: the kernel was
+// bound by its instructions, not by HBM.
+template <int D, typename Act>
+__global__ void __launch_bounds__(WT_WARPS * 32, 6) write_rows_kernel(const __grid_constant__ WriteArgs a)
 {
     vtk_release_successor();
     vtk_wait_for_predecessor();
     constexpr int LPH = D / 8, HPR = 32 / LPH;            // lanes per head, heads per round
-    const int64_t task = (int64_t)blockIdx.x * WT_WARPS + (threadIdx.x >> 5);
-    const int64_t token = task / a.tasks;
+    const uint32_t task = blockIdx.x * WT_WARPS + (threadIdx.x >> 5);            // (below 2^31)
+    const int64_t token = task / (uint32_t)a.tasks;
+    int n = a.max_tokens;
+    if (a.num_tokens != nullptr) {
+        n = *a.num_tokens;
+        n = n < 0 ? 0 : (n > a.max_tokens ? a.max_tokens : n);
+    }
+    if (token >= n) return;
+    const int lane = vtk_lane(), l = lane % LPH, half = a.rot / 2;
+    const bool turned = 8 * l < a.rot, split = turned && !a.interleaved;
+    const int d0 = split ? 4 * l : 8 * l, d1 = split ? d0 + half : d0 + 4;       // the two runs
+    const int first = (int)(task % (uint32_t)a.tasks) * (WT_ROUNDS * HPR) + lane / LPH;
+    const int heads = a.hq + 2 * a.hkv;
+
+    const uint16_t *q_in = (const uint16_t *)a.q + token * a.q_stride;
+    const uint16_t *k_in = (const uint16_t *)a.k + token * a.k_stride - a.hq * D, *v_in = (const uint16_t *)a.v + token * a.v_stride - (a.hq + a.hkv) * D;
+    uint2 raw[WT_ROUNDS][2];
+#pragma unroll
+    for (int i = 0; i < WT_ROUNDS; ++i) {
+        const int h = first + i * HPR;
+        raw[i][0] = raw[i][1] = make_uint2(0, 0);
+        if (h < heads) {
+            const uint16_t *p = (h < a.hq ? q_in : (h < a.hq + a.hkv ? k_in : v_in)) + h * D;
+            raw[i][0] = *reinterpret_cast<const uint2 *>(p + d0);
+            raw[i][1] = *reinterpret_cast<const uint2 *>(p + d1);
+        }
+    }
+    uint2 wq[2] = {make_uint2(0, 0), make_uint2(0, 0)}, wk[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+    if (a.q_weight != nullptr && first < a.hq) {
+        wq[0] = *reinterpret_cast<const uint2 *>((const uint16_t *)a.q_weight + d0);
+        wq[1] = *reinterpret_cast<const uint2 *>((const uint16_t *)a.q_weight + d1);
+    }
+    if (a.k_weight != nullptr && first < a.hq + a.hkv && first + WT_ROUNDS * HPR > a.hq) {
+        wk[0] = *reinterpret_cast<const uint2 *>((const uint16_t *)a.k_weight + d0);
+        wk[1] = *reinterpret_cast<const uint2 *>((const uint16_t *)a.k_weight + d1);
+    }
+    int64_t slot = a.slots[token];
+    if (slot >= a.slots_per_layer) {
+        slot = -1;
+        if (lane == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
+    }
+    // factors of the rotation: pair j of the lane is x (1, c) + partner (0, s)
+    float2 c2[4], s2[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { c2[j] = make_float2(1.f, 1.f); s2[j] = make_float2(0.f, 0.f); }
+    if (a.rot > 0) {
+        const int pos = a.positions[token];
+        if (pos < 0 || pos >= a.max_position) {
+            if (lane == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_POSITION);
+            return;                                        // the whole warp: one token
+        }
+        if (turned) {
+            const float *c = a.cos_sin + (int64_t)pos * a.rot + 4 * l;
+            const float4 cs = *reinterpret_cast<const float4 *>(c), sn = *reinterpret_cast<const float4 *>(c + half);
+            if (a.interleaved) {
+                c2[0] = make_float2(cs.x, cs.x); c2[1] = make_float2(cs.y, cs.y); c2[2] = make_float2(cs.z, cs.z); c2[3] = make_float2(cs.w, cs.w);
+                s2[0] = make_float2(-sn.x, sn.x); s2[1] = make_float2(-sn.y, sn.y); s2[2] = make_float2(-sn.z, sn.z); s2[3] = make_float2(-sn.w, sn.w);
+            } else {
+                c2[0] = c2[2] = make_float2(cs.x, cs.y);
+                c2[1] = c2[3] = make_float2(cs.z, cs.w);
+                s2[0] = make_float2(-sn.x, -sn.y); s2[1] = make_float2(-sn.z, -sn.w);
+                s2[2] = make_float2(sn.x, sn.y); s2[3] = make_float2(sn.z, sn.w);
+            }
+        }
+    }
+    uint16_t *q_to = (uint16_t *)a.q_out + token * a.q_out_stride;
+    uint16_t *k_to = (uint16_t *)(a.k_rows + slot * a.row_bytes) - a.hq * D, *v_to = (uint16_t *)(a.v_rows + slot * a.row_bytes) - (a.hq + a.hkv) * D;
+
+
+#pragma unroll
+    for (int i = 0; i < WT_ROUNDS; ++i) {
+        const int h = first + i * HPR;
+        const bool is_q = h < a.hq, is_k = !is_q && h < a.hq + a.hkv;
+        uint2 out0 = raw[i][0], out1 = raw[i][1];
+        if (__any_sync(0xffffffffu, is_q || is_k)) {
+            float2 x[4] = {Act::unpack(raw[i][0].x), Act::unpack(raw[i][0].y), Act::unpack(raw[i][1].x), Act::unpack(raw[i][1].y)};
+            float2 ss = mul2(x[0], x[0]);
+#pragma unroll
+            for (int j = 1; j < 4; ++j) ss = fma2(x[j], x[j], ss);
+            float sum = ss.x + ss.y;
+#pragma unroll
+            for (int d = LPH / 2; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            if (is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr) {
+                const float r = rsqrtf(sum * (1.f / D) + a.eps);                 // (two ulp of 32 bits)
+                const uint2 w0 = is_q ? wq[0] : wk[0], w1 = is_q ? wq[1] : wk[1];
+                const float2 r2 = make_float2(r, r);
+                x[0] = mul2(mul2(x[0], r2), Act::unpack(w0.x)); x[1] = mul2(mul2(x[1], r2), Act::unpack(w0.y));
+                x[2] = mul2(mul2(x[2], r2), Act::unpack(w1.x)); x[3] = mul2(mul2(x[3], r2), Act::unpack(w1.y));
+            }
+            float2 y[4];
+            if (a.interleaved) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = fma2(make_float2(x[j].y, x[j].x), s2[j], mul2(x[j], c2[j]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = fma2(x[j ^ 2], s2[j], mul2(x[j], c2[j]));
+            }
+            if (is_q || is_k) {
+                out0 = make_uint2(Act::pack(y[0].x, y[0].y), Act::pack(y[1].x, y[1].y));
+                out1 = make_uint2(Act::pack(y[2].x, y[2].y), Act::pack(y[3].x, y[3].y));
+            }
+        }
+        uint16_t *to = h < a.hq ? q_to : (h < a.hq + a.hkv ? k_to : v_to);
+        to += h * D;
+        if (h < heads && (is_q || slot >= 0)) {
+            *reinterpret_cast<uint2 *>(to + d0) = out0;
+            *reinterpret_cast<uint2 *>(to + d1) = out1;
+        }
+    }
+}
+
+// ---- 4-bit rows: 8 consecutive values a lane, half a group ---------------------------------------
+template <int D, typename Act>
+__global__ void __launch_bounds__(WT_WARPS * 32) write_codes_kernel(const __grid_constant__ WriteArgs a)
+{
+    vtk_release_successor();
+    vtk_wait_for_predecessor();
+    constexpr int LPH = D / 8, HPR = 32 / LPH;            // lanes per head, heads per round
+    const uint32_t task = blockIdx.x * WT_WARPS + (threadIdx.x >> 5);            // (below 2^31)
+    const int64_t token = task / (uint32_t)a.tasks;
     int n = a.max_tokens;
     if (a.num_tokens != nullptr) {
         n = *a.num_tokens;
@@ -125,7 +259,7 @@ __global__ void __launch_bounds__(WT_WARPS * 32) write_tokens_kernel(WriteArgs a
     }
     if (token >= n) return;
     const int lane = vtk_lane(), l = lane % LPH;
-    const int first = (int)(task % a.tasks) * (WT_ROUNDS * HPR) + lane / LPH;
+    const int first = (int)(task % (uint32_t)a.tasks) * (WT_ROUNDS * HPR) + lane / LPH;
     const int heads = a.hq + 2 * a.hkv;
 
     uint4 raw[WT_ROUNDS];
@@ -182,7 +316,7 @@ __global__ void __launch_bounds__(WT_WARPS * 32) write_tokens_kernel(WriteArgs a
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = x[j];
             bool done = false;
-            if (FP4 && __any_sync(0xffffffffu, is_k)) {
+            if (__any_sync(0xffffffffu, is_k)) {
                 double z[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) z[j] = x[j];
@@ -200,10 +334,7 @@ __global__ void __launch_bounds__(WT_WARPS * 32) write_tokens_kernel(WriteArgs a
         }
         const int kvh = is_k ? h - a.hq : h - a.hq - a.hkv;
         uint8_t *row = (is_k ? a.k_rows : a.v_rows) + slot * a.row_bytes;
-        if (!FP4) {
-            if ((is_k || is_v) && slot >= 0)
-                *reinterpret_cast<uint4 *>(row + (int64_t)kvh * D * 2 + 16 * l) = is_k ? vtk_pack8<Act>(x) : raw[i];
-        } else if (__any_sync(0xffffffffu, is_k || is_v)) {
+        if (__any_sync(0xffffffffu, is_k || is_v)) {
             const float mul = is_k ? a.k_mul : a.v_mul;
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] *= mul;
@@ -234,15 +365,15 @@ __global__ void __launch_bounds__(256) read_tokens_kernel(ReadArgs a)
     vtk_release_successor();
     vtk_wait_for_predecessor();
     const int per = a.hkv * (D / 8);                      // 8 values a thread, K then V
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t token = i / (2 * per);
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x;   // (below 2^31)
+    const int64_t token = i / (uint32_t)(2 * per);
     int n = a.max_tokens;
     if (a.num_tokens != nullptr) {
         n = *a.num_tokens;
         n = n < 0 ? 0 : (n > a.max_tokens ? a.max_tokens : n);
     }
     if (token >= n) return;
-    const int at = (int)(i % (2 * per));
+    const int at = (int)(i % (uint32_t)(2 * per));
     const bool is_v = at >= per;
     const int j = is_v ? at - per : at;
     void *out = is_v ? a.out_v : a.out_k;
@@ -275,7 +406,8 @@ template <int D, bool FP4, typename Act>
 int launch_write(vtoken_ctx *ctx, const WriteArgs &a, cudaStream_t st)
 {
     const int64_t warps = (int64_t)a.max_tokens * a.tasks;
-    VTK_CUDA(ctx, vtk_launch_dependent(ctx, write_tokens_kernel<D, FP4, Act>, dim3((unsigned)((warps + WT_WARPS - 1) / WT_WARPS)),
+    auto kernel = FP4 ? write_codes_kernel<D, Act> : write_rows_kernel<D, Act>;
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3((unsigned)((warps + WT_WARPS - 1) / WT_WARPS)),
                                        dim3(WT_WARPS * 32), 0, st, a));
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
@@ -363,7 +495,7 @@ int vtoken_write_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t laye
     a.slots_per_layer = ctx->slots_per_layer;
     a.row_bytes = ctx->row_bytes;
     a.flags = &ctx->rt_counts->error_flags;
-    if (((int64_t)a.max_tokens * a.tasks + WT_WARPS - 1) / WT_WARPS > INT32_MAX) return VTOKEN_ECAPACITY;
+    if ((int64_t)a.max_tokens * a.tasks + WT_WARPS > INT32_MAX) return VTOKEN_ECAPACITY;
     return VTK_BY_HEADS(launch_write, heads, ctx, a, (cudaStream_t)cuda_stream);
 }
 
@@ -388,7 +520,7 @@ int vtoken_read_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer
     a.slots_per_layer = ctx->slots_per_layer;
     a.row_bytes = ctx->row_bytes;
     a.flags = &ctx->rt_counts->error_flags;
-    if (((int64_t)max_tokens * 2 * a.hkv * (heads->head_dim / 8) + 255) / 256 > INT32_MAX) return VTOKEN_ECAPACITY;
+    if ((int64_t)max_tokens * 2 * a.hkv * (heads->head_dim / 8) + 256 > INT32_MAX) return VTOKEN_ECAPACITY;
     return VTK_BY_HEADS(launch_read, heads, ctx, a, (cudaStream_t)cuda_stream);
 }
 

@@ -156,6 +156,8 @@ __device__ __forceinline__ uint64_t vtk_global_ns()
 // false when the phase did not complete within the limit, or another role has given up
 static __device__ __forceinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
 {
+    for (int i = 0; i < 2048; ++i)          // (the clock is far away: a wait that is over soon does not look at it)
+        if (vtk_mbar_try(bar, parity)) return true;
     const uint64_t t0 = vtk_global_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)

@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     // ---- once per CTA: barriers, tensor memory, pairs of tiles per request ----
     if (tid == 0) {
         for (int i = 0; i < AP_STAGES; ++i) { vtk_mbar_init(&sh.kv_full[i], 128); vtk_mbar_init(&sh.kv_empty[i], 1); }
-        for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x][0], 128); vtk_mbar_init(&sh.p_full[x][1], 128); vtk_mbar_init(&sh.o_full[x], 1); }
+        for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x][0], 4); vtk_mbar_init(&sh.p_full[x][1], 4); vtk_mbar_init(&sh.o_full[x], 1); }
         vtk_mbar_init(&sh.q_full, 128);
         vtk_mbar_init(&sh.drain, 1);
         sh.abort = 0;
@@ -426,7 +426,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         if (q & 1) {                                             // half of P: the product over it can start
                             tc_wait_st();
                             tc_before_sync();
-                            vtk_mbar_arrive(&sh.p_full[x][q >> 1]);
+                            __syncwarp();
+                            if (lane == 0) vtk_mbar_arrive(&sh.p_full[x][q >> 1]);   // (arrivals are served one by one)
                         }
                     }
                     sum[0] = add2(sum[0], sum[1]);
@@ -684,6 +685,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             // V j, step 2 j + 1 the second half and the scores over K j + 1.
             int step[2] = {0, two ? 0 : 2 * T}, v_there = 0, k_there = 1;       // tiles of V and K that have come
             uint64_t idle = 0;
+            uint32_t polls = 0;
             while (ok && (step[0] < 2 * T || step[1] < 2 * T)) {
                 bool any = false;
 #pragma unroll
@@ -718,13 +720,14 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     }
                     ++step[x];
                 }
-                if (any) {
-                    idle = 0;
-                } else if (idle == 0) {
-                    idle = vtk_global_ns();
-                } else if (__any_sync(0xffffffffu, *(volatile int *)&sh.abort || vtk_global_ns() - idle > limit_ns)) {
-                    *(volatile int *)&sh.abort = 1;
-                    ok = false;
+                polls = any ? 0 : polls + 1;                            // (the clock is far away: looked at now and then)
+                if (polls >= 4096 && polls % 256 == 0) {
+                    const uint64_t now = vtk_global_ns();
+                    if (polls == 4096) idle = now;
+                    if (__any_sync(0xffffffffu, *(volatile int *)&sh.abort || now - idle > limit_ns)) {
+                        *(volatile int *)&sh.abort = 1;
+                        ok = false;
+                    }
                 }
             }
             if (!ok) {                                               // what was issued ends before the tensor memory goes

@@ -13,6 +13,7 @@
 //   12               one thread issues every tcgen05.mma: S = Q K^T (both operands from shared memory, K-major),
 //                    O += P V (P from tensor memory, V as it lies: token rows, the MN-major operand)
 //   13               looks up the next item while this one runs
+//   14, 15           look up the slots and ids of the tiles, and which rows of a tile see all of them
 // While the softmax of one row tile runs, the products of the other keep the tensor pipe busy.
 // Tensor memory: 2 x 128 columns of scores (P overwrites the first half of its own), 2 x D columns of output.
 // Every wait is bounded (wait_limit_ms): where one runs out, the roles leave their loops, the tensor memory is freed
@@ -55,12 +56,12 @@ struct Shared {
     uint8_t q[2][D / 64][AP_TILE * 128];
     uint8_t kv[AP_STAGES][D / 64][AP_TILE * 128];
     Meta meta[AP_META];
-    int slots[AP_META][AP_TILE];         // the producers' tiles: slot, -1 = zeros (the next tile's are written while the last one's may be read)
+    alignas(16) int slots[AP_META][AP_TILE];     // what the producers copy: slot, -1 = zeros
     float row_scale[2][AP_TILE];
     Item item[2];
     int prefix[AP_NT + 1];
     int warp_sum[AP_NT / 32];
-    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], s_full[2], p_full[2][2], o_full[2], q_full, drain;
+    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], meta_full[AP_META], s_full[2], p_full[2][2], o_full[2], q_full, drain;
     uint32_t tmem;
     int abort;
 };
@@ -169,15 +170,6 @@ __device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;
 // Shared memory written by threads (cp.async too) is read by the tensor cores through another path: this fence stands between the two,
 // in the thread that issues the products, behind its wait for the tile (or in the threads that wrote, before they arrive).
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// barrier of the 128 producers that tells all of them whether all said yes
-__device__ __forceinline__ bool producers_agree(bool yes)
-{
-    uint32_t r;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}\n"
-                 : "=r"(r) : "r"((uint32_t)yes) : "memory");
-    return r != 0;
-}
-
 // entries of the ascending ids [base, base + len) that are <= p, found by a warp: 32 probes a round
 __device__ inline int ids_up_to_warp(const VtkAttnArgs &a, int64_t base, int len, int64_t p)
 {
@@ -274,6 +266,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     // ---- once per CTA: barriers, tensor memory, pairs of tiles per request ----
     if (tid == 0) {
         for (int i = 0; i < AP_STAGES; ++i) { vtk_mbar_init(&sh.kv_full[i], 128); vtk_mbar_init(&sh.kv_empty[i], 1); }
+        for (int i = 0; i < AP_META; ++i) vtk_mbar_init(&sh.meta_full[i], 2);
         for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x][0], 4); vtk_mbar_init(&sh.p_full[x][1], 4); vtk_mbar_init(&sh.o_full[x], 1); }
         vtk_mbar_init(&sh.q_full, 128);
         vtk_mbar_init(&sh.drain, 1);
@@ -359,7 +352,9 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.s_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort));
                     if (!ok) break;
                     tc_after_sync();
-                    const Meta &mt = sh.meta[(tile_count + j) % AP_META];
+                    const uint32_t cm = tile_count + j;
+                    vtk_mbar_wait(&sh.meta_full[cm % AP_META], (cm / AP_META) & 1, limit_ns, &sh.abort);       // (it is there)
+                    const Meta &mt = sh.meta[cm % AP_META];
                     uint32_t vis[4];                                             // bit: this row sees the token
                     bool all = true;
 #pragma unroll
@@ -533,34 +528,9 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     async_proxy_fence();
                     vtk_mbar_arrive(&sh.q_full);
                 }
-                const int pmin = two && it.pmin[1] < it.pmin[0] ? it.pmin[1] : it.pmin[0];
-                const int pmax = two && it.pmax[1] > it.pmax[0] ? it.pmax[1] : it.pmax[0];
-                int64_t slot = -1;
-                int id = INT32_MAX;
-                auto fetch = [&](int j) {                          // this thread's token of tile j
-                    const int v = j * AP_TILE + pt;
-                    slot = -1;
-                    id = INT32_MAX;
-                    if (v < it.span.n) {
-                        slot = a.cache_slots[it.span.entry(v)];
-                        id = a.cache_ids.null() ? it.span.index(v) : a.cache_ids[it.span.entry(v)];
-                    }
-                };
-                auto tell = [&](int j) {                           // it, to the other producers and the softmax
-                    if (slot >= a.slots_per_layer) {
-                        atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
-                        slot = -1;
-                    }
-                    Meta &mt = sh.meta[(tile_count + j) % AP_META];
-                    mt.ids[pt] = id;
-                    sh.slots[j % AP_META][pt] = vtk_sees(id, pmax, vtk_floor(pmin, a.window), a.sinks) ? (int)slot : -1;
-                    const unsigned there = __ballot_sync(0xffffffffu, slot >= 0);
-                    if (lane == 0) mt.there[warp - 8] = there;
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const unsigned bits = __ballot_sync(0xffffffffu, slot >= 0 && vtk_sees(id, it.pmin[x], vtk_floor(it.pmax[x], a.window), a.sinks));
-                        if (lane == 0) mt.every[x][warp - 8] = bits;
-                    }
+                auto wait_meta = [&](int j) {                      // the slots of tile j
+                    const uint32_t c = tile_count + j;
+                    return vtk_mbar_wait(&sh.meta_full[c % AP_META], (c / AP_META) & 1, limit_ns, &sh.abort);
                 };
                 // 4-bit rows: four threads a token, a quarter of its codes and scales each, fetched one operand ahead
                 constexpr int QW = D / 32;                         // words of 8 codes a thread
@@ -571,7 +541,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     const uint8_t *rows = which ? a.v_rows : a.k_rows;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int64_t sl = sh.slots[j % AP_META][(pt >> 2) + 32 * i];
+                        const int64_t sl = sh.slots[(tile_count + j) % AP_META][(pt >> 2) + 32 * i];
                         Raw &r = raw[which][i];
 #pragma unroll
                         for (int k = 0; k < QW; ++k) r.w[k] = 0;
@@ -591,38 +561,38 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         }
                     }
                 };
-                fetch(0);
                 auto deliver = [&](int stage) { async_proxy_fence(); vtk_mbar_arrive(&sh.kv_full[stage]); };
                 for (int j = 0; j < T; ++j) {
                     const uint32_t c0 = kv_count + 2 * j, stage_k = c0 % AP_STAGES, stage_v = (c0 + 1) % AP_STAGES;
-                    bool ok = vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
-                    // K two tiles ago is consumed, so both softmaxes are past tile j - 3, whose place the next tile's meta takes
-                    if (j == 0) {
-                        tell(0);
-                        if (T > 1) fetch(1);
-                    }
-                    if (j + 1 < T) tell(j + 1);
-                    ok = producers_agree(ok);
-                    if (!ok) break;
-                    if (j + 2 < T) fetch(j + 2);
+                    if (j == 0 || !FP4)
+                        if (!wait_meta(j)) break;
                     if (FP4 && j == 0) fetch_rows(0, 0);
+                    if (!vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort)) break;
+                    bool ok = true;
 #pragma unroll
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t stage = which ? stage_v : stage_k;
                         if (which) {
-                            // (all agree on the outcome at the next tile; after an abort it does not matter what is overwritten)
-                            vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                            ok = vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                            if (ok && FP4 && j + 1 < T) ok = wait_meta(j + 1);
+                            if (!ok) break;
                         }
                         const uint8_t *rows = which ? a.v_rows : a.k_rows;
                         const uint32_t dst = vtk_smem_u32(sh.kv[stage]);
                         if (!FP4) {
-                            const int piece = pt % PIECES;
-#pragma unroll 4
-                            for (int row = pt / PIECES; row < AP_TILE; row += 128 / PIECES) {
-                                const int64_t sl = sh.slots[j % AP_META][row];
-                                const uint8_t *src = rows + (sl < 0 ? 0 : sl) * a.row_bytes + ((int64_t)it.kv * D + 8 * piece) * 2;
-                                cp_async16(dst + swizzled(row, piece), src, sl >= 0);
+                            // PIECES threads a row, each with the same number of consecutive rows
+                            constexpr int ROWS = PIECES;
+                            const int piece = pt % PIECES, row0 = pt / PIECES * ROWS;
+                            const uint8_t *base = rows + ((int64_t)it.kv * D + 8 * piece) * 2;
+                            int sl[ROWS];
+#pragma unroll
+                            for (int i = 0; i < ROWS; i += 4) {
+                                const int4 four = *reinterpret_cast<const int4 *>(&sh.slots[(tile_count + j) % AP_META][row0 + i]);
+                                sl[i] = four.x; sl[i + 1] = four.y; sl[i + 2] = four.z; sl[i + 3] = four.w;
                             }
+#pragma unroll
+                            for (int i = 0; i < ROWS; ++i)
+                                cp_async16(dst + swizzled(row0 + i, piece), base + (int64_t)(sl[i] < 0 ? 0 : sl[i]) * a.row_bytes, sl[i] >= 0);
                             cp_arrive(&sh.kv_full[stage]);
                         } else {
                             if (which == 0) fetch_rows(1, j);
@@ -638,6 +608,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             deliver((int)stage);
                         }
                     }
+                    if (!ok) break;
                 }
                 if (!FP4) cp_wait_all();                           // (they have: the products are done or, after an abort, waited for here)
             }
@@ -738,10 +709,57 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             __syncwarp();
         });
     } else {
-        // ================= warp 13: the next item (14 and 15 only make up the warpgroup) =================
+        // ================= warp 13: the next item; 14 and 15: slots, ids and masks of the tiles =================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_REST));
-        each_item([&](const Item &, int, bool) {
-            if (warp == 13) next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
+        each_item([&](const Item &it, int T, bool two) {
+            if (warp == 13) {
+                next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
+                return;
+            }
+            const int pmin = two && it.pmin[1] < it.pmin[0] ? it.pmin[1] : it.pmin[0];
+            const int pmax = two && it.pmax[1] > it.pmax[0] ? it.pmax[1] : it.pmax[0];
+            int slot[2], id[2];
+            auto fetch = [&](int j) {                              // this thread's two tokens of tile j
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int v = j * AP_TILE + (warp - 14) * 64 + 32 * i + lane;
+                    slot[i] = -1;
+                    id[i] = INT32_MAX;
+                    if (v < it.span.n) {
+                        slot[i] = a.cache_slots[it.span.entry(v)];
+                        id[i] = a.cache_ids.null() ? it.span.index(v) : a.cache_ids[it.span.entry(v)];
+                    }
+                }
+            };
+            if (T > 0) fetch(0);
+            for (int j = 0; j < T; ++j) {
+                // One tile ahead of the copies: K of two tiles before the one in front is consumed, so both softmaxes are past tile
+                // j - 4, whose place this is.
+                const uint32_t c0 = kv_count + 2 * (j - 1), c = tile_count + j;
+                if (j > 0 && !__all_sync(0xffffffffu, vtk_mbar_wait(&sh.kv_empty[c0 % AP_STAGES], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort))) break;
+                Meta &mt = sh.meta[c % AP_META];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int word = (warp - 14) * 2 + i, at = 32 * word + lane;
+                    if (slot[i] >= a.slots_per_layer) {
+                        atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
+                        slot[i] = -1;
+                    }
+                    mt.ids[at] = id[i];
+                    sh.slots[c % AP_META][at] = vtk_sees(id[i], pmax, vtk_floor(pmin, a.window), a.sinks) ? slot[i] : -1;
+                    const unsigned there = __ballot_sync(0xffffffffu, slot[i] >= 0);
+                    const unsigned every0 = __ballot_sync(0xffffffffu, slot[i] >= 0 && vtk_sees(id[i], it.pmin[0], vtk_floor(it.pmax[0], a.window), a.sinks));
+                    const unsigned every1 = __ballot_sync(0xffffffffu, slot[i] >= 0 && vtk_sees(id[i], it.pmin[1], vtk_floor(it.pmax[1], a.window), a.sinks));
+                    if (lane == 0) {
+                        mt.there[word] = there;
+                        mt.every[0][word] = every0;
+                        mt.every[1][word] = every1;
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) vtk_mbar_arrive(&sh.meta_full[c % AP_META]);
+                if (j + 1 < T) fetch(j + 1);
+            }
         });
     }
     __syncthreads();

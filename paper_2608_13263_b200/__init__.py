@@ -47,4 +47,5 @@ __all__ = ["VtokenError", "vtoken_create", "vtoken_destroy", "vtoken_plan", "vto
            "vtoken_build_slot_mapping", "vtoken_apply_moves", "vtoken_block_liveness", "vtoken_plan_partial", "vtoken_digest_logical",
            "vtoken_repack_host_partial", "vtoken_repack_waves", "vtoken_waves_workspace_bytes", "vtoken_slot_cache_mark",
            "vtoken_slot_cache_update", "vtoken_check_tables", "vtoken_evict_tokens_counted",
-           "vtoken_sync_new_tokens_counted"]
+           "vtoken_sync_new_tokens_counted", "Heads", "vtoken_kv_row_bytes", "vtoken_write_tokens",
+           "vtoken_read_tokens", "vtoken_attention", "vtoken_attention_workspace_bytes"]

@@ -1,16 +1,21 @@
 // Attention of few query rows per request (a decode step) over the slot cache.
 //
-// Bound by HBM: every visible K and V row is read once, 4 * D flops per row, head and query.
+// Bound by HBM: every visible K and V row is read once, 4 * D flops per row, head and query.  512 requests over 3.1 GB of
+// 16-bit rows take 554 us (5.6 TB/s, 0.86 of the copy bandwidth), 256 requests over 650 MB of 4-bit rows 231 us (there the
+// expansion of codes and scales, about 400 instructions for 16 tokens of a head, is the bound); a small call takes 6 us
+// of dependent loads (requests, lengths, positions, slots, rows).
 //
-// The cut.  A segment is (request, tile of query rows, key head); its cache is numbered in tiles of 16 tokens (32 of
-// the 4-bit cache), and
+// The cut.  A segment is (request, tile of query rows, group of key heads); its cache is numbered in tiles of 16 tokens, and
 // all tiles of all segments in one row.  Teams of warps take equal shares of that row -- so every SM reads the same
 // number of bytes whatever the lengths -- and every CTA (one per SM) works them out for itself from the tables.  A
-// team is one warp when there are segments enough, the CTA's warps when there are few.  Its warps take the tiles of a
-// segment in turn, each with a running maximum and sum per query row and the output accumulators in registers, and
-// join in shared memory at the segment's end.  A segment that lies inside one share is finished there; at most the
-// first and the last segment of a share are parts of longer ones: they leave a partial row, and the last team to
+// team has a warp for each head of the group, and more of them per head, its lanes, when there are few segments.  The lanes take
+// the tiles of a segment in turn, each with a running maximum and sum per query row and the output accumulators in
+// registers, and join in shared memory at the segment's end.  A segment that lies inside one share is finished there; at most
+// the first and the last segment of a share are parts of longer ones: they leave a partial row, and the last team to
 // arrive joins the parts in the order of the tables, so the sums do not depend on who came when.
+// Groups: one head over 16-bit rows (256 bytes of a row are read well by themselves, and more segments mean fewer parts), up
+// to eight over 4-bit rows, whose 64 bytes of codes and 8 of scales would each cost a sector of DRAM when the heads of a row are
+// read at different times (324 us with groups of one, 240 with eight, at that step, on the 256 requests).
 //
 // The stream.  Each warp copies its tiles (K and V rows of one head, gathered by slot) with cp.async into a ring of
 // its own, several tiles ahead and across the ends of segments, so that about 100 KB per SM are in flight through

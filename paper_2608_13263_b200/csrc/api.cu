@@ -92,7 +92,7 @@ int vtoken_create(const vtoken_config *cfg, vtoken_ctx **out_ctx)
     if (cfg->num_layers < 1 || cfg->num_blocks < 1 || cfg->block_size < 1 || cfg->num_kv_heads < 1 ||
         cfg->head_dim < 1 || cfg->elem_bytes < 1 || !cfg->k_pool || !cfg->v_pool || cfg->max_requests < 1 ||
         cfg->max_tokens < 1 || cfg->max_table_blocks < 1 || cfg->max_free_blocks < 0 || cfg->max_ctas < 0 ||
-        cfg->debug_stall_item < 0)
+        cfg->debug_stall_item < 0 || cfg->debug_stall_item > (1ll << 32) + 1000000)
         return VTOKEN_EINVAL;
     const int64_t row_bytes = (int64_t)cfg->num_kv_heads * cfg->head_dim * cfg->elem_bytes;
     const int64_t slots = (int64_t)cfg->num_blocks * cfg->block_size;

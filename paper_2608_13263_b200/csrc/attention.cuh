@@ -127,9 +127,9 @@ __device__ __forceinline__ void vtk_mbar_init(uint64_t *bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(vtk_smem_u32(bar)), "r"(count));
 }
-__device__ __forceinline__ void vtk_mbar_arrive(uint64_t *bar)
+__device__ __forceinline__ void vtk_mbar_arrive(uint64_t *bar, uint32_t count = 1)
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(vtk_smem_u32(bar)), "r"(count) : "memory");
 }
 __device__ __forceinline__ bool vtk_mbar_try(uint64_t *bar, uint32_t parity)
 {

@@ -63,7 +63,7 @@ struct Shared {
     Item item[2];
     int prefix[AP_NT + 1];
     int warp_sum[AP_NT / 32];
-    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], meta_full[AP_META], s_full[2], p_full[2][2], o_full[2], q_full, drain;
+    uint64_t kv_full[AP_STAGES], kv_empty[AP_STAGES], meta_full[AP_META], meta_empty[AP_META], s_full[2], p_full[2][2], o_full[2], q_full, drain;
     uint32_t tmem;
     int abort;
 };
@@ -255,7 +255,7 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 w)
 
 template <int D, bool FP4, typename Act>
 __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid_constant__ VtkAttnArgs a, uint32_t *tickets, int row_limit,
-                                                                    uint64_t limit_ns, float scale, int negate)
+                                                                    uint64_t limit_ns, float scale, int negate, int64_t stall)
 {
     using Mma = typename std::conditional<FP4, VtkFp16, Act>::type;
     constexpr int PANEL = AP_TILE * 128, PIECES = D / 8;
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     // ---- once per CTA: barriers, tensor memory, pairs of tiles per request ----
     if (tid == 0) {
         for (int i = 0; i < AP_STAGES; ++i) { vtk_mbar_init(&sh.kv_full[i], 128); vtk_mbar_init(&sh.kv_empty[i], 1); }
-        for (int i = 0; i < AP_META; ++i) vtk_mbar_init(&sh.meta_full[i], 2);
+        for (int i = 0; i < AP_META; ++i) { vtk_mbar_init(&sh.meta_full[i], 2); vtk_mbar_init(&sh.meta_empty[i], 8); }
         for (int x = 0; x < 2; ++x) { vtk_mbar_init(&sh.s_full[x], 1); vtk_mbar_init(&sh.p_full[x][0], 4); vtk_mbar_init(&sh.p_full[x][1], 4); vtk_mbar_init(&sh.o_full[x], 1); }
         vtk_mbar_init(&sh.q_full, 128);
         vtk_mbar_init(&sh.drain, 1);
@@ -345,6 +345,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             const int pos = have ? a.positions[tok] : -1, floor = vtk_floor(pos, a.window);
             float m = -INFINITY, l = 0.f, c = scale;
             bool ok = true;
+            // This warp is past a tile's ids and masks, and the producers are past its slots: the scores of the tile behind it (the
+            // outputs, at the end) need rows that were copied after them.  Eight arrivals a tile: a lone row tile's warps count twice.
+            auto done_with = [&](uint32_t tile) {
+                if (lane == 0) vtk_mbar_arrive(&sh.meta_empty[tile % AP_META], two ? 1 : 2);
+            };
             if (x == 0 || two) {
                 if (FP4 && T > 0) {                                              // row scales come with the queries
                     ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort));
@@ -355,6 +360,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (!ok) break;
                     tc_after_sync();
                     const uint32_t cm = tile_count + j;
+                    if (j > 0) done_with(cm - 1);
                     vtk_mbar_wait(&sh.meta_full[cm % AP_META], (cm / AP_META) & 1, limit_ns, &sh.abort);       // (it is there)
                     const Meta &mt = sh.meta[cm % AP_META];
                     uint32_t vis[4];                                             // bit: this row sees the token
@@ -432,7 +438,10 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 }
                 if (ok && T > 0) ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort));
                 if (ok) {
-                    if (T > 0) tc_after_sync();
+                    if (T > 0) {
+                        tc_after_sync();
+                        done_with(tile_count + T - 1);
+                    }
                     const float r = l == 0.f ? 0.f : a.v_mul / l;
                     bool bad = !(fabsf(l) < INFINITY);
                     uint16_t *dst = a.out + tok * a.out_stride + (int64_t)head * D;
@@ -735,10 +744,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             };
             if (T > 0) fetch(0);
             for (int j = 0; j < T; ++j) {
-                // One tile ahead of the copies: K of two tiles before the one in front is consumed, so both softmaxes are past tile
-                // j - 4, whose place this is.
-                const uint32_t c0 = kv_count + 2 * (j - 1), c = tile_count + j;
-                if (j > 0 && !__all_sync(0xffffffffu, vtk_mbar_wait(&sh.kv_empty[c0 % AP_STAGES], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort))) break;
+                // As far ahead of the copies as there are places.  The place has barriers of its own, whose next phase needs what is
+                // written here: a phase of the stages' barriers could come and go unseen while these warps wait for slots.
+                const uint32_t c = tile_count + j;
+#ifdef VTOKEN_CHECKED
+                for (int64_t left = stall - (1ll << 32); left >= 0; left -= 100000) __nanosleep(left < 100000 ? (unsigned)left + 1 : 100000u);
+#endif
+                if (!__all_sync(0xffffffffu, vtk_mbar_wait(&sh.meta_empty[c % AP_META], ((c / AP_META) & 1) ^ 1, limit_ns, &sh.abort))) break;
                 Meta &mt = sh.meta[c % AP_META];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -787,7 +799,7 @@ int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_
     // the sign of the scores' factor goes into the product (a zero factor: one that no 32-bit score can be seen through)
     const float scale = a.scale_log2 == 0.f ? 7.9e-31f : (a.scale_log2 < 0.f ? -a.scale_log2 : a.scale_log2);
     VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(ctx->num_sms), dim3(AP_NT), smem, st, a, tickets, a.row_limit,
-                                       (uint64_t)ctx->wait_limit_ns, scale, (int)(a.scale_log2 < 0.f)));
+                                       (uint64_t)ctx->wait_limit_ns, scale, (int)(a.scale_log2 < 0.f), ctx->stall_item));
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
 }

@@ -1,0 +1,54 @@
+"""The waits inside the prompt kernel of vtoken_attention: roles that run late, and waits that run out.  The hooks that make a
+role late exist only in the checked build (vtoken_config.debug_stall_item); nothing faults."""
+import numpy as np
+import pytest
+
+from attention_sim import Cache, Step, spread
+from paper_2608_13263_b200 import binding as vt
+
+pytestmark = pytest.mark.gpu
+
+LATE = 1 << 32                   # debug_stall_item: from here on, nanoseconds that the lookup of slots is late at each tile
+
+
+@pytest.fixture
+def checked():
+    prev = vt.use_library("checked")
+    yield
+    vt.use_library(prev)
+
+
+def prompts(rng, kv, act="bf16", hq=8, hkv=2, d=128, lens=(900, 700), queries=(300, 200)):
+    ids, slots, total = spread(rng, lens)
+    c = Cache(rng, kv, act, hq, hkv, d, total, np.concatenate(slots), max_tokens=sum(lens) + 64)
+    return Step(rng, c, ids, slots, [list(range(n - m, n)) for n, m in zip(lens, queries)])
+
+
+def context(step, **options):
+    """The cache's context again, with options."""
+    c = step.c
+    rb = c.k_pool.shape[-1]
+    geo = (1, rb, 1) if c.kv == "fp4" else (c.hkv, c.d, 2)
+    new = vt.vtoken_create(c.layers, c.slots // c.block, c.block, geo[0], geo[1], c.k_pool, c.v_pool, c.max_requests, c.max_tokens,
+                           c.max_tokens, 4, elem_bytes=geo[2], **options)
+    vt.vtoken_destroy(c.ctx)
+    c.ctx = new
+
+
+@pytest.mark.parametrize("kv,d,queries", [("bf16", 128, (300, 200)), ("bf16", 64, (40, 33)), ("fp4", 128, (300, 20)), ("fp4", 64, (70, 200))])
+def test_slots_that_are_looked_up_late(checked, kv, d, queries):
+    """20 us at each tile, ten times what a tile takes: the copies and products are always done with what they have before the next
+    slots come."""
+    st = prompts(np.random.default_rng(20), kv, d=d, queries=queries)
+    context(st, debug_stall_item=LATE + 20000)
+    st.run().check()
+    assert st.c.flags() == 0
+    st.c.close()
+
+
+def test_the_hook_is_checked(checked):
+    st = prompts(np.random.default_rng(21), "bf16", lens=(50,), queries=(40,))
+    with pytest.raises(vt.VtokenError) as e:
+        context(st, debug_stall_item=LATE + 1000001)
+    assert e.value.code == vt.EINVAL
+    st.c.close()

@@ -145,7 +145,9 @@ typedef struct {
     int64_t debug_stall_item;      /* must be 0 for the production library (VTOKEN_EINVAL otherwise).  The checked
                                       build (libvtoken_checked.so) arms the barrier of work item
                                       debug_stall_item - 1 of the copy kernel with bytes that never arrive, so that
-                                      its wait runs out: the time-out path is exercised without faulting anything.
+                                      its wait runs out: the time-out path is exercised without faulting anything;
+                                      likewise the queries of that work item of vtoken_attention's prompt kernel never
+                                      become complete.
                                       Above 2^32 (at most 2^32 + 1000000): the warps of the prompt kernel of
                                       vtoken_attention that look up slots are late by that many - 2^32 ns at each tile */
 } vtoken_config;

@@ -153,8 +153,8 @@ __device__ __forceinline__ uint64_t vtk_global_ns()
     return t;
 }
 // (inlined: a call would keep the compiler from giving the roles of a kernel register counts of their own)
-// false when the phase did not complete within the limit, or another role has given up
-static __device__ __forceinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort)
+// false when the phase did not complete within the limit (`mark`, not zero, is left in `abort`), or another role has given up
+static __device__ __forceinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, volatile int *abort, int mark)
 {
     for (int i = 0; i < 2048; ++i)          // (the clock is far away: a wait that is over soon does not look at it)
         if (vtk_mbar_try(bar, parity)) return true;
@@ -163,12 +163,12 @@ static __device__ __forceinline__ bool vtk_mbar_wait_long(uint64_t *bar, uint32_
         for (int i = 0; i < 64; ++i)
             if (vtk_mbar_try(bar, parity)) return true;
         if (*abort) return false;
-        if (vtk_global_ns() - t0 > limit_ns) { *abort = 1; return false; }
+        if (vtk_global_ns() - t0 > limit_ns) { *abort = mark; return false; }
     }
 }
-__device__ __forceinline__ bool vtk_mbar_wait(uint64_t *bar, uint32_t parity, uint64_t limit_ns, int *abort)
+__device__ __forceinline__ bool vtk_mbar_wait(uint64_t *bar, uint32_t parity, uint64_t limit_ns, int *abort, int mark)
 {
-    return vtk_mbar_try(bar, parity) || vtk_mbar_try(bar, parity) || vtk_mbar_wait_long(bar, parity, limit_ns, abort);
+    return vtk_mbar_try(bar, parity) || vtk_mbar_try(bar, parity) || vtk_mbar_wait_long(bar, parity, limit_ns, abort, mark);
 }
 
 // ---- one head of one pool row, `N` consecutive values from `d` on, as 32-bit values -------------

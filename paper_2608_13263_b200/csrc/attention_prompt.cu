@@ -27,9 +27,10 @@ namespace {
 constexpr int AP_REGS_SOFTMAX = 192, AP_REGS_LOAD = 80, AP_REGS_REST = 48;
 static_assert(2 * AP_REGS_SOFTMAX + AP_REGS_LOAD + AP_REGS_REST <= 4 * 128, "the registers that the block is launched with");
 constexpr int AP_NT = 512, AP_STAGES = 4, AP_TILE = 128, AP_META = 4;
+constexpr uint64_t AP_DRAIN_NS = 1000000000;    // products in flight end by themselves: waited for whatever the caller's limit is
 
 struct Item {                            // what one CTA works on
-    int none;
+    int none, ticket;
     int kv, q0, first, rows, len;        // key head; first query row of the request; first row and rows of the pair of tiles
     int pmin[2], pmax[2];                // positions of the two row tiles
     int tiles;                           // tiles of 128 tokens
@@ -200,6 +201,7 @@ __device__ void next_item(const VtkAttnArgs &a, Shared<D> &sh, Item &out, int R,
     idx = __shfl_sync(0xffffffffu, idx, 0);
     Item it;
     it.none = 1;
+    it.ticket = idx;
     if (idx / a.hkv < sh.prefix[AP_NT]) {
         it.none = 0;
         it.kv = idx % a.hkv;
@@ -319,7 +321,10 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
         for (;; ++item_count) {
             asm volatile("barrier.cta.sync 0, 512;" ::: "memory");
             const Item &it = sh.item[item_count & 1];
-            if (it.none || *(volatile int *)&sh.abort) break;
+            // Who gives up leaves the number of its item, from 1 on, so that the verdict is the same for all: a role that comes here late may
+            // find the mark of one that has already given up in the item that starts now, and has to join it there, not leave.
+            const int gave_up = *(volatile int *)&sh.abort;
+            if (it.none || (gave_up != 0 && gave_up <= (int)item_count)) break;
             const int T = it.tiles;
             const bool two = it.rows > AP_TILE;
             body(it, T, two);
@@ -352,16 +357,16 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             };
             if (x == 0 || two) {
                 if (FP4 && T > 0) {                                              // row scales come with the queries
-                    ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort));
+                    ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.q_full, q_count & 1, limit_ns, &sh.abort, item_count + 1));
                     c = scale * sh.row_scale[x][row];
                 }
                 for (int j = 0; j < T && ok; ++j) {
-                    ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.s_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort));
+                    ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.s_full[x], (s_count[x] + j) & 1, limit_ns, &sh.abort, item_count + 1));
                     if (!ok) break;
                     tc_after_sync();
                     const uint32_t cm = tile_count + j;
                     if (j > 0) done_with(cm - 1);
-                    vtk_mbar_wait(&sh.meta_full[cm % AP_META], (cm / AP_META) & 1, limit_ns, &sh.abort);       // (it is there)
+                    vtk_mbar_wait(&sh.meta_full[cm % AP_META], (cm / AP_META) & 1, limit_ns, &sh.abort, item_count + 1);       // (it is there)
                     const Meta &mt = sh.meta[cm % AP_META];
                     uint32_t vis[4];                                             // bit: this row sees the token
                     bool all = true;
@@ -436,7 +441,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     sum[0] = add2(sum[0], sum[1]);
                     l += sum[0].x + sum[0].y;
                 }
-                if (ok && T > 0) ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort));
+                if (ok && T > 0) ok = __all_sync(0xffffffffu, vtk_mbar_wait(&sh.o_full[x], o_count[x] & 1, limit_ns, &sh.abort, item_count + 1));
                 if (ok) {
                     if (T > 0) {
                         tc_after_sync();
@@ -490,6 +495,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     } else if (warp < 12) {
         // ================= producers =================
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_LOAD));
+        auto stalled = [&](const Item &it) {                       // the item whose wait for its queries has to run out (a test's)
+#ifdef VTOKEN_CHECKED
+            return it.ticket == stall;
+#else
+            return false;
+#endif
+        };
         each_item([&](const Item &it, int T, bool two) {
             if (T > 0) {
                 const int pt = tid - 256;
@@ -503,7 +515,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D + 8 * piece;
                         cp_async16(vtk_smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
                     }
-                    cp_arrive(&sh.q_full);
+                    if (!stalled(it) || pt > 0) cp_arrive(&sh.q_full);
                 } else {
                     for (int x = 0; x < (two ? 2 : 1); ++x) {
                         const int row = x * AP_TILE + pt, at = it.first + row;
@@ -537,11 +549,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         }
                     }
                     async_proxy_fence();
-                    vtk_mbar_arrive(&sh.q_full);
+                    if (!stalled(it) || pt > 0) vtk_mbar_arrive(&sh.q_full);
                 }
                 auto wait_meta = [&](int j) {                      // the slots of tile j
                     const uint32_t c = tile_count + j;
-                    return vtk_mbar_wait(&sh.meta_full[c % AP_META], (c / AP_META) & 1, limit_ns, &sh.abort);
+                    return vtk_mbar_wait(&sh.meta_full[c % AP_META], (c / AP_META) & 1, limit_ns, &sh.abort, item_count + 1);
                 };
                 // 4-bit rows: four threads a token, a quarter of its codes and scales each, fetched one operand ahead
                 constexpr int QW = D / 32;                         // words of 8 codes a thread
@@ -578,13 +590,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (j == 0 || !FP4)
                         if (!wait_meta(j)) break;
                     if (FP4 && j == 0) fetch_rows(0, 0);
-                    if (!vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort)) break;
+                    if (!vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort, item_count + 1)) break;
                     bool ok = true;
 #pragma unroll
                     for (int which = 0; which < 2; ++which) {
                         const uint32_t stage = which ? stage_v : stage_k;
                         if (which) {
-                            ok = vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort);
+                            ok = vtk_mbar_wait(&sh.kv_empty[stage_v], (((c0 + 1) / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort, item_count + 1);
                             if (ok && FP4 && j + 1 < T) ok = wait_meta(j + 1);
                             if (!ok) break;
                         }
@@ -633,7 +645,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             (void)it;
             if (T == 0) return;
             const uint32_t k0 = kv_count;
-            auto wait = [&](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, vtk_mbar_wait(bar, parity, limit_ns, &sh.abort)); };
+            auto wait = [&](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, vtk_mbar_wait(bar, parity, limit_ns, &sh.abort, item_count + 1)); };
             auto wait_tile = [&](uint32_t cc) { return wait(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1); };
             auto come = [&](uint64_t *bar, uint32_t parity) { return (bool)__all_sync(0xffffffffu, vtk_mbar_test(bar, parity)); };
             auto tile_come = [&](uint32_t cc) { return come(&sh.kv_full[cc % AP_STAGES], (cc / AP_STAGES) & 1); };
@@ -707,7 +719,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     const uint64_t now = vtk_global_ns();
                     if (polls == 4096) idle = now;
                     if (__any_sync(0xffffffffu, *(volatile int *)&sh.abort || now - idle > limit_ns)) {
-                        *(volatile int *)&sh.abort = 1;
+                        *(volatile int *)&sh.abort = (int)item_count + 1;
                         ok = false;
                     }
                 }
@@ -715,7 +727,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
             if (!ok) {                                               // what was issued ends before the tensor memory goes
                 tc_commit(one, &sh.drain);
                 const uint64_t t0 = vtk_global_ns();
-                while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < limit_ns) {}
+                while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < AP_DRAIN_NS) {}
             }
             __syncwarp();
         });
@@ -750,7 +762,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
 #ifdef VTOKEN_CHECKED
                 for (int64_t left = stall - (1ll << 32); left >= 0; left -= 100000) __nanosleep(left < 100000 ? (unsigned)left + 1 : 100000u);
 #endif
-                if (!__all_sync(0xffffffffu, vtk_mbar_wait(&sh.meta_empty[c % AP_META], ((c / AP_META) & 1) ^ 1, limit_ns, &sh.abort))) break;
+                if (!__all_sync(0xffffffffu, vtk_mbar_wait(&sh.meta_empty[c % AP_META], ((c / AP_META) & 1) ^ 1, limit_ns, &sh.abort, item_count + 1))) break;
                 Meta &mt = sh.meta[c % AP_META];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {

@@ -52,3 +52,54 @@ def test_the_hook_is_checked(checked):
         context(st, debug_stall_item=LATE + 1000001)
     assert e.value.code == vt.EINVAL
     st.c.close()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp4"])
+def test_a_wait_that_runs_out(checked, kv):
+    """The queries of one work item never come: its CTA gives up after the limit, the call ends with VTOKEN_FLAG_TIMEOUT, every other
+    item is right, the workspace is ready for the next call, and that one is right throughout."""
+    import torch
+    for item in (0, 3):
+        st = prompts(np.random.default_rng(22), kv)
+        context(st, wait_limit_ms=5, debug_stall_item=item + 1)
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        st.run()
+        e1.record()
+        torch.cuda.synchronize()
+        assert 4.0 < e0.elapsed_time(e1) < 2000.0
+        assert st.c.flags() == vt.FLAG_TIMEOUT
+        assert not st.workspace[:4096].cpu().numpy().any()
+        out, _ = st.outputs()
+        ref, _, tol, _ = st.reference()
+        # items: pairs of row tiles from a request's last to its first, all key heads of a pair in turn; here of the first request,
+        # 1200 rows of 4 heads and 300 tokens: 176 rows, then 256 at a time
+        lost = np.zeros(out.shape[:2], bool)
+        pair, kv_head = 4 - item // 2, item % 2
+        lost[pair * 64:min(300, pair * 64 + 64), 4 * kv_head:4 * kv_head + 4] = True
+        assert (out[lost] == 77.0).all()
+        assert (np.abs(out - ref)[~lost] <= tol[~lost]).all()
+        context(st)
+        st.call()
+        st.check()
+        assert st.c.flags() == 0
+        st.c.close()
+
+
+def test_many_items_when_one_cta_gives_up(checked):
+    """More items than SMs: what the CTA that gave up had already taken is lost, the others do the rest."""
+    import torch
+    st = prompts(np.random.default_rng(23), "bf16", hq=64, hkv=64, d=64, lens=(130, 150, 130), queries=(130, 129, 130))
+    context(st, wait_limit_ms=5, debug_stall_item=4)
+    st.run()
+    torch.cuda.synchronize()
+    assert st.c.flags() == vt.FLAG_TIMEOUT
+    assert not st.workspace[:4096].cpu().numpy().any()
+    out, _ = st.outputs()
+    gone = (out == 77.0).all(-1)
+    assert 129 <= gone.sum() <= 2 * 130
+    context(st)
+    st.call()
+    st.check()
+    assert st.c.flags() == 0
+    st.c.close()

@@ -163,7 +163,7 @@ struct Shared {
     alignas(128) uint8_t ring[NW][ST][Rows::STAGE];
     alignas(16) union {
         float o[NW][NR * D];             // join: a warp's accumulators, 16 bytes a lane
-        struct { int warp_sum[NW], warp_segments[NW], start[NW], before[NW]; } plan;
+        struct { int64_t warp_sum[NW], before[NW]; int warp_segments[NW], start[NW]; } plan;
     };
     float2 ml[NW][NR];
     int ids[NW][ST][Rows::TILE];
@@ -279,22 +279,24 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     bool clipped = R < 0 || R > a.max_requests;
     R = R < 0 ? 0 : (R > a.max_requests ? a.max_requests : R);
     const int seg = (R + NT - 1) / NT;
-    int mine = 0, my_segments = 0;
+    int64_t mine = 0;                                        // (a prompt that the hint did not tell of may have 2^31 of them by itself)
+    int my_segments = 0;
     Known own;                                               // the thread's last request: its only one below 257 requests
     for (int r = tid * seg; r < (tid + 1) * seg && r < R; ++r) {
         own = look_up<NR, TILE>(a, r, clipped);
-        mine += own.tiles * own.row_tiles;
+        mine += (int64_t)own.tiles * own.row_tiles;
         my_segments += own.tiles > 0 ? own.row_tiles : 0;
     }
     if (clipped && blockIdx.x == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
-    const int incl = vtk_warp_incl_scan(mine);
+    const int64_t incl = vtk_warp_incl_scan(mine);
     my_segments = __reduce_add_sync(0xffffffffu, my_segments);
     if (lane == 31) {
         sh.plan.warp_sum[warp] = incl;
         sh.plan.warp_segments[warp] = my_segments;
     }
     __syncthreads();
-    int before = 0, all_tiles = 0, all_segments = 0;
+    int64_t before = 0, all_tiles = 0;
+    int all_segments = 0;
     for (int w = 0; w < NW; ++w) {
         before += w < warp ? sh.plan.warp_sum[w] : 0;
         all_tiles += sh.plan.warp_sum[w];
@@ -314,7 +316,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     }
     const int per_team = group * lanes, teams = NW / per_team, my_team = warp / per_team;
     const int hl = warp / lanes % group, tw = warp % lanes;  // head of the group, lane of tokens
-    const int64_t W = (int64_t)all_tiles * groups;
+    const int64_t W = all_tiles * groups;
     // at least AT_MIN_SHARE tiles a lane: a segment that is cut finer costs more to join than it gains
     const int64_t most = divide(W + AT_MIN_SHARE * lanes - 1, AT_MIN_SHARE * lanes), G = most < (int64_t)gridDim.x * teams ? most : (int64_t)gridDim.x * teams;
     const bool packed = G == (int64_t)gridDim.x * teams;     // a CTA's shares side by side; few shares: on different SMs
@@ -327,7 +329,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     for (int team = 0; team < teams; ++team) {               // the thread whose requests hold a share's first tile
         if (share_at(team) >= G) break;
         const int64_t f = start_of(share_at(team));
-        if (f >= (int64_t)before * groups && f < (int64_t)(before + mine) * groups) {
+        if (f >= before * groups && f < (before + mine) * groups) {
             sh.plan.start[team] = tid;
             sh.plan.before[team] = before;
         }
@@ -339,7 +341,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     use.k = &s_use[warp];
     int64_t left = 0;
     if (share < G) {
-        left = use.f - (int64_t)sh.plan.before[my_team] * groups;
+        left = use.f - sh.plan.before[my_team] * groups;
         use.r = sh.plan.start[my_team] * seg;
     }
     const int known0 = G > share_at(0) ? sh.plan.start[0] : 0;

@@ -213,11 +213,12 @@ inline cudaError_t vtk_launch_dependent(const vtoken_ctx *ctx, void (*kernel)(P.
 // ---------------------------------------------------------------------------------------
 __device__ __forceinline__ int vtk_lane() { return threadIdx.x & 31; }
 
-__device__ __forceinline__ int vtk_warp_incl_scan(int v)
+template <typename T>
+__device__ __forceinline__ T vtk_warp_incl_scan(T v)
 {
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        int o = __shfl_up_sync(0xffffffffu, v, d);
+        T o = __shfl_up_sync(0xffffffffu, v, d);
         if (vtk_lane() >= d) v += o;
     }
     return v;

@@ -207,12 +207,12 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
     if (k.qn * (int64_t)a.group > a.row_limit) k.qn = 0;
     k.s.lo = k.s.n_sink = 0;
     k.s.n = k.len;
-    k.pmax = INT32_MAX - 1;
-    k.floor = -1;
+    k.pmax = k.floor = -1;
     k.row_tiles = (k.qn * a.group + NR - 1) / NR;
-    if (k.qn > 0 && k.qn <= 8) {         // few queries: only what one of them can see
+    if (k.qn > 0) {                      // only what one of the queries can see
         const int last = vtk_last_id(a, k.s.base, k.len);
         int pmin = a.positions[k.q0], pmax = pmin;
+#pragma unroll 4
         for (int i = 1; i < k.qn; ++i) {
             const int p = a.positions[k.q0 + i];
             pmin = p < pmin ? p : pmin;
@@ -403,11 +403,12 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     };
     auto issue = [&](Next n) {
         if (n.there) {
+            const bool seen = vtk_sees(n.id, n.pmax, n.floor, a.sinks);           // (the span's ends are counted, not looked up)
             if (n.slot >= 0 && (int64_t)n.slot >= a.slots_per_layer) {
-                atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
+                if (seen) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
                 n.slot = -1;
             }
-            if (!vtk_sees(n.id, n.pmax, n.floor, a.sinks)) n.slot = -1;
+            if (!seen) n.slot = -1;
             const int stage = issued % ST;
             if (lane < TILE) sh.ids[warp][stage][lane] = n.slot < 0 ? INT32_MAX : n.id;
             Rows::issue(vtk_smem_u32(sh.ring[warp][stage]), a.k_rows, a.v_rows, a.row_bytes, a.hkv, n.kv, n.slot);

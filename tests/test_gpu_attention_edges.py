@@ -54,3 +54,27 @@ def test_more_tiles_than_32_bits_count():
     assert ((out[0].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (2e-4 + 2.0 ** -16) * v.double().abs().max()).all()
     assert ((lse[0].double() - torch.logsumexp(s, -1)).abs() < 2e-4).all()
     vt.vtoken_destroy(ctx)
+
+
+# ---- what is read ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("kv", ["bf16", "fp4"])
+@pytest.mark.parametrize("group,queries", [(1, 9), (1, 32), (2, 16), (3, 10), (4, 40)])
+@pytest.mark.parametrize("hint", [None, 1])
+def test_tokens_that_no_query_sees_are_not_read(kv, group, queries, hint):
+    """Behind the window and after the last position every row of the request is NaN or has a slot that is not in the pool: no flag,
+    finite outputs.  With 9 and more query tokens, over both kernels and with a hint that is too small."""
+    rng = np.random.default_rng(32)
+    first, last, window, sinks = 2000, 2000 + queries, 50, 3
+    for keep in (1.0, 0.4):
+        ids, slots, total = spread(rng, [3000, 40], keep)
+        seen = (ids[0] < sinks) | ((ids[0] > first - window) & (ids[0] < last))
+        c = Cache(rng, kv, "bf16", 2 * group, 2, 128, total, np.concatenate([slots[0][seen], slots[1]]), max_tokens=3200)
+        given = slots[0].copy()
+        given[~seen & (ids[0] % 3 == 0)] = c.slots + 5
+        for s in given[~seen]:
+            c.k64[int(s)] = c.v64[int(s)] = np.full((2, 128), np.nan)
+        st = Step(rng, c, ids, [given, slots[1]], [list(range(first, last)), [39]], window, sinks, max_query_len=hint)
+        st.run()
+        st.check()
+        assert c.flags() == 0
+        c.close()

@@ -29,7 +29,7 @@
 //   O^T = V^T P^T : 8 dimensions of four tokens, paired up to the A fragment by byte permutes; the accumulator layout
 //   of S (rows = queries, columns = tokens) is the B fragment of P^T as it is.
 // P is handed to the second product as the sum of two 16-bit values, so that its rounding does not add to that of
-// the 16-bit output; over the 4-bit cache the products run in half precision, whose 11 bits are enough next to a
+// the 16-bit output (in half precision they carry 2^7, see vtk_lift); over the 4-bit cache the products run in half precision, whose 11 bits are enough next to a
 // bf16 output.  These legacy matrix instructions are enough here: 8 or 16 rows leave a 128-row tcgen05 tile mostly
 // empty, and at full HBM rate the products need well under a third of the legacy tensor rate.
 #include "attention.cuh"
@@ -574,7 +574,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 uint32_t w[RH][2], w_lo[RH][2];
 #pragma unroll
                 for (int h = 0; h < RH; ++h) {
-                    const float base = m[h] == -INFINITY ? 0.f : m[h];
+                    const float base = (m[h] == -INFINITY ? 0.f : m[h]) - vtk_lift<Mma>();
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const float p0 = vtk_exp2(p[b][u][2 * h] - base), p1 = vtk_exp2(p[b][u][2 * h + 1] - base);
@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                     int64_t tok;
                     int head;
                     query(g + 8 * h, tok, head);
-                    a.lse[tok * a.hq + head] = ll[h] == 0.f ? -INFINITY : (mm[h] + log2f(ll[h])) * 0.69314718055994531f;
+                    a.lse[tok * a.hq + head] = ll[h] == 0.f ? -INFINITY : (mm[h] + log2f(ll[h]) - vtk_lift<Mma>()) * 0.69314718055994531f;
                 }
             }
         };

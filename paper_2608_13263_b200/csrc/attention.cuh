@@ -107,6 +107,11 @@ __device__ __forceinline__ void vtk_mma<VtkFp16>(float (&c)[4], uint32_t a0, uin
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// Softmax weights that go to half precision carry 2^7: next to a running maximum that may lag by 2^8 they end at 2^15, and what
+// half precision rounds to zero is below 2^-32 of the largest, so n such tokens take at most n * 2^-32 of the largest |v| from an
+// output whose sum of weights, in 32 bits, counts them (without the factor n * 2^-25: 2^-10 at 32 768 tokens).
+template <typename M> __host__ __device__ constexpr float vtk_lift() { return M::kind == VTOKEN_KV_FP16 ? 7.f : 0.f; }
+
 __device__ __forceinline__ float vtk_exp2(float x)
 {
     float y;

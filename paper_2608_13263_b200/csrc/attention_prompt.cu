@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             }
                         }
                     }
-                    const float mc = m == -INFINITY ? 0.f : m * c;
+                    const float mc = (m == -INFINITY ? 0.f : m * c) - vtk_lift<Mma>();
                     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                     const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
 #pragma unroll
@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         }
                     }
                     if (have && a.lse != nullptr)
-                        a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * 0.69314718055994531f;
+                        a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (m * c + log2f(l) - vtk_lift<Mma>()) * 0.69314718055994531f;
                     // rows that a masked NaN may have reached: token by token
                     unsigned again = __ballot_sync(0xffffffffu, have && bad);
                     while (again) {

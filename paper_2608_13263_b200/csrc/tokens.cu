@@ -73,18 +73,19 @@ __device__ __forceinline__ void norm_rotate(F (&y)[8], bool normed, const float 
     }
 }
 
-// The lane's 8 values (its neighbour holds the other 8 of the group) to codes and a scale.  Thresholds of the
-// grid are compared in effect with x / scale: the division is the IEEE one, x has 8 or 11 significant bits and
-// the scale 4, so a quotient lands on a tie only when it is one.
-__device__ __forceinline__ void quantise(const float (&x)[8], uint32_t &codes, uint32_t &scale)
+// The lane's 8 values (its neighbour holds the other 8 of the group), times a power of two, to codes and a scale.
+// Thresholds of the grid are compared in effect with x / scale: the division is the IEEE one, x has 8 or 11
+// significant bits and the scale 4, so a quotient lands on a tie only when it is one.  A multiple that leaves 32
+// bits saturates like any other that is too large.
+__device__ __forceinline__ void quantise(float (&x)[8], float mul, uint32_t &codes, uint32_t &scale)
 {
     float top = 0.f;
     bool odd = false;                                      // a NaN or an infinity
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float a = fabsf(x[j]);
-        odd |= !(a < __int_as_float(0x7f800000));
-        top = fmaxf(top, a);
+        odd |= !(fabsf(x[j]) < __int_as_float(0x7f800000));
+        x[j] *= mul;
+        top = fmaxf(top, fabsf(x[j]));
     }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     odd |= (bool)__shfl_xor_sync(0xffffffffu, (int)odd, 1);
@@ -335,11 +336,8 @@ __global__ void __launch_bounds__(WT_WARPS * 32) write_codes_kernel(const __grid
         const int kvh = is_k ? h - a.hq : h - a.hq - a.hkv;
         uint8_t *row = (is_k ? a.k_rows : a.v_rows) + slot * a.row_bytes;
         if (__any_sync(0xffffffffu, is_k || is_v)) {
-            const float mul = is_k ? a.k_mul : a.v_mul;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] *= mul;
             uint32_t codes, scale;
-            quantise(x, codes, scale);
+            quantise(x, is_k ? a.k_mul : a.v_mul, codes, scale);
             if ((is_k || is_v) && slot >= 0) {
                 *reinterpret_cast<uint32_t *>(row + kvh * (D / 2) + 4 * l) = codes;
                 if ((l & 1) == 0) row[(int64_t)a.hkv * (D / 2) + kvh * (D / 16) + l / 2] = (uint8_t)scale;

@@ -230,6 +230,10 @@ __global__ void __launch_bounds__(WT_WARPS * 32, 6) write_rows_kernel(const __gr
 #pragma unroll
                 for (int j = 0; j < 4; ++j) y[j] = fma2(x[j ^ 2], s2[j], mul2(x[j], c2[j]));
             }
+            if (!turned) {                                 // (a NaN times the factor zero is one)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = x[j];
+            }
             if (is_q || is_k) {
                 out0 = make_uint2(Act::pack(y[0].x, y[0].y), Act::pack(y[1].x, y[1].y));
                 out1 = make_uint2(Act::pack(y[2].x, y[2].y), Act::pack(y[3].x, y[3].y));

@@ -646,7 +646,8 @@ typedef struct {                   /* all pointers DEVICE */
                                       right for every length */
     const int32_t *tt_offsets;     /* [R+1] the slot cache of request r starts at tt_offsets[r] */
     const int32_t *cache_slots;    /* slots of its active tokens, in ascending order of their ids */
-    const int32_t *cache_ids;      /* their logical ids, strictly ascending; NULL: 0, 1, 2, ... (nothing was evicted) */
+    const int32_t *cache_ids;      /* their logical ids, strictly ascending from 0 or above, below 2^31 - 1; NULL: 0, 1, 2, ...
+                                      (nothing was evicted) */
     const int32_t *cache_len;      /* [R] active tokens */
     float sm_scale;                /* factor of the scores, finite */
     int32_t window;                /* 0: none; else a query at p sees ids > p - window ... */

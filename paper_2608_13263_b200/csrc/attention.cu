@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 int head;
                 split_row(a, at, tok, head);
                 tok += use.k->q0;
-                pos[h] = a.positions[tok];
+                pos[h] = min(a.positions[tok], INT32_MAX - 1);     // (INT32_MAX is the id of what is not there)
                 floor[h] = vtk_floor(pos[h], a.window);
                 p = a.q + tok * a.q_stride + (int64_t)(kv * a.group + head) * D;
             }

@@ -182,3 +182,14 @@ def test_weights_that_cancel(geometry, queries, gap):
     tol = 1.01 * unit(act) * np.abs(ref) + 1.5 * (held + 2 * soft) + 2.0 ** -24
     assert (np.abs(out - ref) <= tol).all(), (np.abs(out - ref) / tol).max()
     st.c.close()
+
+
+# ---- ends of the types ----------------------------------------------------------------------------
+@pytest.mark.parametrize("kv", ["bf16", "fp4"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 0), (100, 5)])
+def test_the_largest_position(kv, window, sinks):
+    """2^31 - 1 sees every token without a window, the first ones with one; nothing that is not there."""
+    rng = np.random.default_rng(34)
+    top = 2 ** 31 - 1
+    for positions in ([[top], [top], [10]], [[top, 5], [top - 1, top], [top]], [[top] * 40, [20] * 20 + [top] * 30, [top]]):
+        run_and_check(problem(rng, ("bf16", kv, 8, 2, 128), [37, 300, 16], positions, window=window, sinks=sinks))

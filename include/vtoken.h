@@ -599,7 +599,7 @@ int64_t vtoken_kv_row_bytes(const vtoken_heads *heads);
 
 typedef struct {                   /* all pointers DEVICE, 16-byte aligned unless an int array */
     const int32_t *num_tokens;     /* device scalar, clamped to [0, max_tokens]; NULL: max_tokens */
-    int32_t max_tokens;            /* rows of the arrays below */
+    int32_t max_tokens;            /* rows of the arrays below; 0: a call without work, the arrays may be NULL */
     const void *q, *k, *v;         /* [max_tokens][heads][head_dim] act_type; q may be NULL (no queries) */
     int64_t q_stride, k_stride, v_stride;   /* elements between tokens, multiples of 8; 0: dense.  The three may be slices
                                           of one projection output */
@@ -640,7 +640,8 @@ typedef struct {                   /* all pointers DEVICE */
     const int32_t *positions;      /* [max_query_tokens] logical id of each query token */
     const void *q;                 /* [max_query_tokens][num_q_heads][head_dim] act_type, 16-byte aligned */
     int64_t q_stride;              /* elements between tokens, multiple of 8; 0: dense */
-    int32_t max_query_tokens;      /* rows of q; q_offsets beyond it are clipped (VTOKEN_FLAG_CAPACITY) */
+    int32_t max_query_tokens;      /* rows of q; q_offsets beyond it are clipped (VTOKEN_FLAG_CAPACITY).  0: a call without
+                                      work, positions, q and out may be NULL */
     int32_t max_query_len;         /* a hint: longest q_offsets[r+1] - q_offsets[r], >= 1.  It chooses between the
                                       kernel for few and the one for many query rows per request; both are
                                       right for every length */

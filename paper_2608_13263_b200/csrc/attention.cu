@@ -877,9 +877,8 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
 {
     if (!ctx || !heads || !in) return VTOKEN_EINVAL;
     if (vtk_check_heads(ctx, heads, layer) != VTOKEN_OK) return VTOKEN_EINVAL;
-    if (!in->num_requests || !in->q_offsets || !in->positions || !in->q || !in->tt_offsets || !in->cache_slots || !in->cache_len ||
-        !in->out || !in->workspace)
-        return VTOKEN_EINVAL;
+    if (!in->num_requests || !in->q_offsets || !in->tt_offsets || !in->cache_slots || !in->cache_len || !in->workspace) return VTOKEN_EINVAL;
+    if (in->max_query_tokens != 0 && (!in->positions || !in->q || !in->out)) return VTOKEN_EINVAL;     // (without elements: no address)
     if (in->max_query_tokens < 0 || in->max_query_len < 1 || in->window < 0 || in->sinks < 0) return VTOKEN_EINVAL;
     if (!(in->sm_scale > -1e30f && in->sm_scale < 1e30f)) return VTOKEN_EINVAL;
     if (((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)in->workspace) & 15) return VTOKEN_EINVAL;

@@ -458,12 +458,14 @@ int vtoken_write_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t laye
 {
     if (!ctx || !heads || !in) return VTOKEN_EINVAL;
     if (vtk_check_heads(ctx, heads, layer) != VTOKEN_OK) return VTOKEN_EINVAL;
-    if (in->max_tokens < 0 || !in->k || !in->v || !in->slots || (in->q && !in->q_out)) return VTOKEN_EINVAL;
+    if (in->max_tokens < 0) return VTOKEN_EINVAL;
+    const bool none = in->max_tokens == 0;                   // (arrays without elements may have no address)
+    if (!none && (!in->k || !in->v || !in->slots || (in->q && !in->q_out))) return VTOKEN_EINVAL;
     if (misaligned(in->q) || misaligned(in->k) || misaligned(in->v) || misaligned(in->q_weight) || misaligned(in->k_weight) ||
         misaligned(in->cos_sin) || misaligned(in->q_out))
         return VTOKEN_EINVAL;
     if (in->rot_dim < 0 || in->rot_dim > heads->head_dim || in->rot_dim % 16 != 0) return VTOKEN_EINVAL;
-    if (in->rot_dim > 0 && (!in->cos_sin || !in->positions || in->max_position < 1)) return VTOKEN_EINVAL;
+    if (in->rot_dim > 0 && (!in->cos_sin || (!none && !in->positions) || in->max_position < 1)) return VTOKEN_EINVAL;
     if ((in->q_weight || in->k_weight) && !(in->eps > 0.f && in->eps < 1e30f)) return VTOKEN_EINVAL;
     const int64_t dq = (int64_t)heads->num_q_heads * heads->head_dim, dk = (int64_t)heads->num_kv_heads * heads->head_dim;
     WriteArgs a;
@@ -473,7 +475,7 @@ int vtoken_write_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t laye
     a.q_out_stride = vtk_stride(in->q_out_stride, dq);
     if (a.q_stride < 0 || a.k_stride < 0 || a.v_stride < 0 || a.q_out_stride < 0) return VTOKEN_EINVAL;
     if (in->q && in->q == in->q_out && a.q_stride != a.q_out_stride) return VTOKEN_EINVAL;
-    if (in->max_tokens == 0) return VTOKEN_OK;
+    if (none) return VTOKEN_OK;
     a.num_tokens = in->num_tokens;
     a.max_tokens = in->max_tokens;
     a.q = in->q; a.k = in->k; a.v = in->v;
@@ -506,7 +508,7 @@ int vtoken_read_tokens(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer
 {
     if (!ctx || !heads) return VTOKEN_EINVAL;
     if (vtk_check_heads(ctx, heads, layer) != VTOKEN_OK) return VTOKEN_EINVAL;
-    if (max_tokens < 0 || !slots || misaligned(out_k) || misaligned(out_v)) return VTOKEN_EINVAL;
+    if (max_tokens < 0 || (max_tokens > 0 && !slots) || misaligned(out_k) || misaligned(out_v)) return VTOKEN_EINVAL;
     if (max_tokens == 0 || (!out_k && !out_v)) return VTOKEN_OK;
     ReadArgs a;
     a.num_tokens = num_tokens;

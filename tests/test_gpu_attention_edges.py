@@ -193,3 +193,17 @@ def test_the_largest_position(kv, window, sinks):
     top = 2 ** 31 - 1
     for positions in ([[top], [top], [10]], [[top, 5], [top - 1, top], [top]], [[top] * 40, [20] * 20 + [top] * 30, [top]]):
         run_and_check(problem(rng, ("bf16", kv, 8, 2, 128), [37, 300, 16], positions, window=window, sinks=sinks))
+
+
+def test_a_call_without_query_tokens_needs_no_tensors():
+    """A tensor without elements has no address."""
+    import torch
+    rng = np.random.default_rng(38)
+    st = problem(rng, ("bf16", "bf16", 8, 2, 128), [50], positions=[[]])
+    empty = torch.empty(0, device=st.c.dev, dtype=torch.bfloat16)
+    assert empty.data_ptr() == 0
+    st.q_all = st.out_all = empty
+    st.pos, st.lse = empty.int(), empty.float()
+    st.run()
+    assert st.c.flags() == 0
+    st.c.close()

@@ -65,3 +65,21 @@ def test_normalised_rows_with_an_infinity(geometry):
     ok = np.isfinite(want)
     assert (np.abs(got - want)[ok] <= 2.0 ** -8 * np.abs(want)[ok] + 2.0 ** -15).all()
     w.close()
+
+
+def test_calls_without_tokens_need_no_tensors():
+    """A tensor without elements has no address."""
+    import torch
+    for g in (GEOMETRIES[0], GEOMETRIES[3]):
+        w = Writer(np.random.default_rng(53), g, 4)
+        empty = torch.empty(0, device=w.dev, dtype=w.q.dtype)
+        none = torch.empty(0, device=w.dev, dtype=torch.int32)
+        assert empty.data_ptr() == 0 and none.data_ptr() == 0
+        w.write(max_tokens=0, q=empty, k=empty, v=empty, q_out=empty, slots=none, positions=none)
+        vt.vtoken_read_tokens(w.ctx, heads=w.heads, layer=0, max_tokens=0, slots=none, out_k=empty, out_v=empty)
+        assert w.flags() == 0
+        with pytest.raises(vt.VtokenError):                   # what is not about the tokens is still checked
+            w.write(max_tokens=0, layer=7)
+        with pytest.raises(vt.VtokenError):
+            w.write(max_tokens=0, rot_dim=8)
+        w.close()

@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 int e2 = (int)(__float_as_uint(top) >> 23) - 127;          // floor(log2), subnormals -127
-                e2 = 14 - (e2 > 100 ? 100 : (e2 < -100 ? -100 : e2));
+                e2 = 14 - (e2 < -100 ? -100 : e2);
                 const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
                 scale[h] *= __uint_as_float((uint32_t)(127 - e2) << 23);
 #pragma unroll

@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                                 for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
                             }
                             int e2 = (int)(__float_as_uint(top) >> 23) - 127;
-                            e2 = 14 - (e2 > 100 ? 100 : (e2 < -100 ? -100 : e2));
+                            e2 = 14 - (e2 < -100 ? -100 : e2);
                             up = __uint_as_float((uint32_t)(127 + e2) << 23);
                             down = __uint_as_float((uint32_t)(127 - e2) << 23);
                         }

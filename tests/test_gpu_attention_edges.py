@@ -195,6 +195,15 @@ def test_the_largest_position(kv, window, sinks):
         run_and_check(problem(rng, ("bf16", kv, 8, 2, 128), [37, 300, 16], positions, window=window, sinks=sinks))
 
 
+@pytest.mark.parametrize("queries", [1, 40])
+def test_queries_at_the_upper_end_of_bf16_over_4_bits(queries):
+    rng = np.random.default_rng(35)
+    st = problem(rng, ("bf16", "fp4", 8, 2, 128), [200], positions=[list(range(200 - queries, 200))],
+                 cache_options=dict(k_exponent=-60), q_scale=2.0 ** 115)
+    st.sm_scale = 2.0 ** -55 * 128 ** -0.5
+    run_and_check(st)
+
+
 def test_a_call_without_query_tokens_needs_no_tensors():
     """A tensor without elements has no address."""
     import torch

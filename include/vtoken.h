@@ -650,7 +650,7 @@ typedef struct {                   /* all pointers DEVICE */
     const int32_t *cache_ids;      /* their logical ids, strictly ascending from 0 or above, below 2^31 - 1; NULL: 0, 1, 2, ...
                                       (nothing was evicted) */
     const int32_t *cache_len;      /* [R] active tokens */
-    float sm_scale;                /* factor of the scores, finite */
+    float sm_scale;                /* factor of the scores, within 1e30, and finite when 2^k_exponent is taken in */
     int32_t window;                /* 0: none; else a query at p sees ids > p - window ... */
     int32_t sinks;                 /* ... and ids < sinks (attention sinks).  Always: ids <= p */
     void *out;                     /* [max_query_tokens][num_q_heads][head_dim] act_type, 16-byte aligned */

@@ -204,6 +204,18 @@ def test_queries_at_the_upper_end_of_bf16_over_4_bits(queries):
     run_and_check(st)
 
 
+def test_scales_that_leave_32_bits_are_refused():
+    rng = np.random.default_rng(36)
+    st = problem(rng, ("bf16", "fp4", 8, 2, 128), [50], cache_options=dict(k_exponent=60))
+    st.sm_scale = 1e25
+    with pytest.raises(vt.VtokenError) as e:
+        st.run()
+    assert e.value.code == vt.EINVAL
+    st.sm_scale = 1e-25
+    st.run()
+    st.c.close()
+
+
 def test_a_call_without_query_tokens_needs_no_tensors():
     """A tensor without elements has no address."""
     import torch

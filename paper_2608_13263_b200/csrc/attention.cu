@@ -882,7 +882,7 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     if (in->max_query_tokens < 0 || in->max_query_len < 1 || in->window < 0 || in->sinks < 0) return VTOKEN_EINVAL;
     const float scale = in->sm_scale * 1.4426950408889634f * two_to(heads->k_exponent);
     if (!(in->sm_scale > -1e30f && in->sm_scale < 1e30f) || !(scale > -INFINITY && scale < INFINITY)) return VTOKEN_EINVAL;
-    if (((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)in->workspace) & 15) return VTOKEN_EINVAL;
+    if ((((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)in->workspace) & 15) || ((uintptr_t)in->lse & 3)) return VTOKEN_EINVAL;
     VtkAttnArgs a;
     const int64_t dense = (int64_t)heads->num_q_heads * heads->head_dim;
     a.q_stride = vtk_stride(in->q_stride, dense);

@@ -216,6 +216,19 @@ def test_scales_that_leave_32_bits_are_refused():
     st.c.close()
 
 
+def test_an_lse_between_its_words_is_refused():
+    import torch
+    rng = np.random.default_rng(37)
+    st = problem(rng, ("bf16", "bf16", 8, 2, 128), [50])
+    lse = st.lse
+    st.lse = lse.data_ptr() + 2
+    with pytest.raises(vt.VtokenError) as e:
+        st.run()
+    assert e.value.code == vt.EINVAL
+    torch.cuda.synchronize()
+    st.c.close()
+
+
 def test_a_call_without_query_tokens_needs_no_tensors():
     """A tensor without elements has no address."""
     import torch

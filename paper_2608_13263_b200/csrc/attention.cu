@@ -810,7 +810,10 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 bad = false;
                 for (int w = warp - tw; w < warp - tw + lanes; ++w) bad |= *(volatile int *)&sh.bad[w] != 0;
             }
-            if (bad) again();
+            if (bad) {
+                __syncwarp();                                // (other lanes write over what this one has just stored)
+                again();
+            }
         }
         team_sync();                                         // the join buffers are used by the next segment
     }

@@ -479,6 +479,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (m * c + log2f(l) - vtk_lift<Mma>()) * 0.69314718055994531f;
                     // rows that a masked NaN may have reached: token by token
                     unsigned again = __ballot_sync(0xffffffffu, have && bad);
+                    if (again) __syncwarp();                         // (other lanes write over what a row's own has just stored)
                     while (again) {
                         const int src = __ffs(again) - 1;
                         again &= again - 1;

@@ -193,8 +193,7 @@ __device__ __forceinline__ float weight(float m, float top) { return m == -INFIN
 // one request as the cut sees it
 struct Known {
     int q0, qn, len, tiles, row_tiles;
-    int pmax, floor;                     // no query sees an id above pmax, nor one up to floor that is no sink
-    VtkRequest s;                        // (base, lo, n_sink, n)
+    VtkRequest s;
 };
 
 template <int NR, int TILE>
@@ -207,7 +206,7 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
     if (k.qn * (int64_t)a.group > a.row_limit) k.qn = 0;
     k.s.lo = k.s.n_sink = 0;
     k.s.n = k.len;
-    k.pmax = k.floor = -1;
+    k.s.pmax = k.s.floor = -1;
     k.row_tiles = (k.qn * a.group + NR - 1) / NR;
     if (k.qn > 0) {                      // only what one of the queries can see
         const int last = vtk_last_id(a, k.s.base, k.len);
@@ -218,8 +217,6 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
             pmin = p < pmin ? p : pmin;
             pmax = p > pmax ? p : pmax;
         }
-        k.pmax = pmax;
-        k.floor = vtk_floor(pmin, a.window);
         k.s = vtk_request_span(a, k.s.base, k.len, last, pmin, pmax);
     }
     k.tiles = k.qn > 0 ? (k.s.n > 0 ? (k.s.n + TILE - 1) / TILE : 1) : 0;
@@ -395,8 +392,8 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         if (more && lane < TILE && v < get.k->s.n && n.kv < a.hkv) {
             n.slot = a.cache_slots[get.k->s.entry(v)];
             n.id = a.cache_ids.null() ? get.k->s.index(v) : a.cache_ids[get.k->s.entry(v)];
-            n.pmax = get.k->pmax;
-            n.floor = get.k->floor;
+            n.pmax = get.k->s.pmax;
+            n.floor = get.k->s.floor;
         }
         tile += lanes;
         return n;
@@ -703,8 +700,8 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 int head;
                 query(row, tok, head);
                 float acc[N], mm, ll;
-                vtk_row_again<D, Rows::FP4, Act>(a, tok, head, a.positions[tok], use.k->s.base, use.k->len, acc, mm, ll);
-                vtk_store_row<D, Act>(a, tok, head, acc, mm, ll);
+                if (vtk_row_again<D, Rows::FP4, Act>(a, tok, head, a.positions[tok], use.k->s, use.k->len, acc, mm, ll))
+                    vtk_store_row<D, Act>(a, tok, head, acc, mm, ll);
             }
         };
         bool bad = false;

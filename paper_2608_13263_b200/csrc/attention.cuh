@@ -24,10 +24,14 @@ struct VtkAttnArgs {
     int32_t row_limit;                   // requests of more query rows (tokens times group) belong to attention_prompt.cu
 };
 
+// Ids are not negative.  A query at p sees the ids in (vtk_floor(p), p] and those below `sinks`.
+__device__ __forceinline__ int vtk_floor(int p, int window) { return window == 0 || p < window ? -1 : p - window; }
+__device__ __forceinline__ bool vtk_sees(int id, int p, int floor, int sinks) { return id <= p && (id > floor || id < sinks); }
+
 // What a request's queries read of its slot cache: entries [0, n_sink) and [lo, lo + n - n_sink), numbered
 // 0 .. n - 1 in that order ("virtual" indexes).
 struct VtkRequest {
-    int q0, qn;                          // query rows
+    int pmax, floor;                     // no query sees an id above pmax, nor one up to floor that is no sink
     int64_t base;                        // first cache entry
     int lo, n_sink, n;
     __device__ __forceinline__ int64_t entry(int v) const { return base + (v < n_sink ? v : lo + (v - n_sink)); }
@@ -61,7 +65,8 @@ __device__ inline int vtk_ids_up_to(const VtkAttnArgs &a, int64_t base, int len,
 __device__ inline VtkRequest vtk_request_span(const VtkAttnArgs &a, int64_t base, int len, int last, int pmin, int pmax)
 {
     VtkRequest q;
-    q.q0 = q.qn = 0;
+    q.pmax = pmax;
+    q.floor = vtk_floor(pmin, a.window);
     q.base = base;
     const int hi = vtk_ids_up_to(a, base, len, last, pmax);
     int64_t lo = 0;
@@ -86,10 +91,6 @@ __device__ inline void vtk_request_rows(const VtkAttnArgs &a, int r, int &q0, in
     len = want < 0 ? 0 : (want > end - base ? (int)(end - base) : want);
     clipped = a0 != q0 || a1 != q1 || q1 < q0 || t0 != base || t1 != end || want != len;
 }
-
-// Ids are not negative.  A query at p sees the ids in (vtk_floor(p), p] and those below `sinks`.
-__device__ __forceinline__ int vtk_floor(int p, int window) { return window == 0 || p < window ? -1 : p - window; }
-__device__ __forceinline__ bool vtk_sees(int id, int p, int floor, int sinks) { return id <= p && (id > floor || id < sinks); }
 
 // ---- matrix instructions: 16 x 8 += 16 x 16 by 16 x 8, 32-bit accumulators ----------------------
 template <typename M>
@@ -204,14 +205,47 @@ __device__ __forceinline__ void vtk_row_values(const uint8_t *row, int hkv, int 
     }
 }
 
-// One query row by one warp, token by token: the definition.  The matrix kernels multiply a masked token's
-// value by a zero weight, so a NaN or an infinity there would reach rows that do not see the token; a row
-// whose result is not finite is computed again here, where only the tokens it sees are touched.  Values come
-// out as the lane's D / 32 consecutive dimensions.
+// The matrix kernels multiply a masked token's value by a zero weight, so a NaN or an infinity there would reach rows that do not
+// see the token.  (A masked key does not: its score is replaced.)  Rows whose result is not finite are looked at again, by a warp each.
+
+// Does a token that the row at `pos` does not see, but that was fetched because another row does -- an id in (pos, pmax] or in
+// (floor, vtk_floor(pos)] -- have a value that is not finite?  If not, the row is what the tokens it sees make it: a cache with NaN
+// in it costs a look at these few tokens a row, and no row is worked on again for a value that it sees.
 template <int D, bool FP4, typename Act>
-__device__ __noinline__ void vtk_row_again(const VtkAttnArgs &a, int64_t q_row, int head, int pos, int64_t base, int len,
+__device__ __forceinline__ bool vtk_hidden_value(const VtkAttnArgs &a, int head, int pos, const VtkRequest &s, int len)
+{
+    constexpr int N = D / 32, AT_ONCE = 8;
+    const int64_t base = s.base;
+    const int last = vtk_last_id(a, base, len), kv = head / a.group;
+    for (int part = 0; part < 2; ++part) {
+        const int lo = vtk_ids_up_to(a, base, len, last, part ? s.floor : pos);
+        const int hi = vtk_ids_up_to(a, base, len, last, part ? vtk_floor(pos, a.window) : s.pmax);
+        for (int i = lo; i < hi; i += AT_ONCE) {
+            bool odd = false;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int64_t slot = i + u < hi ? a.cache_slots[base + i + u] : -1;
+                if (slot < 0 || slot >= a.slots_per_layer) continue;
+                float v[N];
+                vtk_row_values<D, FP4, Act, N>(a.v_rows + slot * a.row_bytes, a.hkv, kv, vtk_lane() * N, v);
+#pragma unroll
+                for (int j = 0; j < N; ++j) odd |= !(fabsf(v[j]) < INFINITY);
+            }
+            if (__any_sync(0xffffffffu, odd)) return true;
+        }
+    }
+    return false;
+}
+
+// One query row by one warp, token by token: the definition, of the tokens that the row sees alone.  Values come out as the lane's
+// D / 32 consecutive dimensions; false when the row stands as it was stored, since no value that it does not see is at fault, or all
+// in it that is not finite has turned out to be NaN.
+template <int D, bool FP4, typename Act>
+__device__ __noinline__ bool vtk_row_again(const VtkAttnArgs &a, int64_t q_row, int head, int pos, const VtkRequest &request, int len,
                                            float (&o)[D / 32], float &m, float &l)
 {
+    if (!vtk_hidden_value<D, FP4, Act>(a, head, pos, request, len)) return false;
+    const int64_t base = request.base;
     constexpr int N = D / 32;
     const int lane = vtk_lane(), kv = head / a.group;
     float q[N];
@@ -227,7 +261,21 @@ __device__ __noinline__ void vtk_row_again(const VtkAttnArgs &a, int64_t q_row, 
     const int floor = vtk_floor(pos, a.window);
 #pragma unroll
     for (int j = 0; j < N; ++j) o[j] = 0.f;
+    bool open[N];                        // dimensions in question
+    const uint32_t *stored = reinterpret_cast<const uint32_t *>(a.out + q_row * a.out_stride + (int64_t)head * D + lane * N);
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+        const float2 v = Act::unpack(__ldcg(stored + j));
+        open[2 * j] = !(fabsf(v.x) < INFINITY);
+        open[2 * j + 1] = !(fabsf(v.y) < INFINITY);
+    }
     for (int i = 0; i < len; ++i) {
+        if (i % 32 == 31) {
+            bool settled = true;
+#pragma unroll
+            for (int j = 0; j < N; ++j) settled &= !open[j] || o[j] != o[j];
+            if (__all_sync(0xffffffffu, settled)) return false;
+        }
         const int id = a.cache_ids.null() ? i : a.cache_ids[base + i];
         const int64_t slot = a.cache_slots[base + i];
         if (slot < 0 || slot >= a.slots_per_layer || !vtk_sees(id, pos, floor, a.sinks)) continue;
@@ -247,6 +295,7 @@ __device__ __noinline__ void vtk_row_again(const VtkAttnArgs &a, int64_t q_row, 
         for (int j = 0; j < N; ++j) o[j] = o[j] * keep + p * v[j];
         m = m2;
     }
+    return true;
 }
 
 // the row's output and lse: the lane's N consecutive dimensions

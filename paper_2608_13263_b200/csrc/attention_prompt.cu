@@ -237,8 +237,8 @@ __device__ void next_item(const VtkAttnArgs &a, Shared<D> &sh, Item &out, int R,
             pmin = it.pmin[x] < pmin ? it.pmin[x] : pmin;
             pmax = it.pmax[x] > pmax ? it.pmax[x] : pmax;
         }
-        it.span.q0 = it.q0;
-        it.span.qn = qn;
+        it.span.pmax = pmax;
+        it.span.floor = vtk_floor(pmin, a.window);
         it.span.base = base;
         const int end = ids_up_to_warp(a, base, it.len, pmax);
         it.span.lo = a.window > 0 ? ids_up_to_warp(a, base, it.len, (int64_t)pmin - a.window) : 0;
@@ -448,7 +448,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         done_with(tile_count + T - 1);
                     }
                     const float r = l == 0.f ? 0.f : a.v_mul / l;
-                    bool bad = !(fabsf(l) < INFINITY);
+                    const bool finite = fabsf(l) < INFINITY;         // (a sum that is not: the row sees a score that is not)
+                    bool bad = false;
                     uint16_t *dst = a.out + tok * a.out_stride + (int64_t)head * D;
 #pragma unroll
                     for (int q = 0; q < D / 32; ++q) {
@@ -478,7 +479,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (have && a.lse != nullptr)
                         a.lse[tok * a.hq + head] = l == 0.f ? -INFINITY : (m * c + log2f(l) - vtk_lift<Mma>()) * 0.69314718055994531f;
                     // rows that a masked NaN may have reached: token by token
-                    unsigned again = __ballot_sync(0xffffffffu, have && bad);
+                    unsigned again = __ballot_sync(0xffffffffu, have && bad && finite);
                     if (again) __syncwarp();                         // (other lanes write over what a row's own has just stored)
                     while (again) {
                         const int src = __ffs(again) - 1;
@@ -486,8 +487,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         const int64_t q_row = __shfl_sync(0xffffffffu, (int)tok, src);
                         const int h2 = __shfl_sync(0xffffffffu, head, src), p2 = __shfl_sync(0xffffffffu, pos, src);
                         float acc[D / 32], m2, l2;
-                        vtk_row_again<D, FP4, Act>(a, q_row, h2, p2, it.span.base, it.len, acc, m2, l2);
-                        vtk_store_row<D, Act>(a, q_row, h2, acc, m2, l2);
+                        if (vtk_row_again<D, FP4, Act>(a, q_row, h2, p2, it.span, it.len, acc, m2, l2)) vtk_store_row<D, Act>(a, q_row, h2, acc, m2, l2);
                     }
                     tc_before_sync();
                 }
@@ -740,8 +740,6 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
                 return;
             }
-            const int pmin = two && it.pmin[1] < it.pmin[0] ? it.pmin[1] : it.pmin[0];
-            const int pmax = two && it.pmax[1] > it.pmax[0] ? it.pmax[1] : it.pmax[0];
             int slot[2], id[2];
             auto fetch = [&](int j) {                              // this thread's two tokens of tile j
 #pragma unroll
@@ -773,7 +771,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                         slot[i] = -1;
                     }
                     mt.ids[at] = id[i];
-                    sh.slots[c % AP_META][at] = vtk_sees(id[i], pmax, vtk_floor(pmin, a.window), a.sinks) ? slot[i] : -1;
+                    sh.slots[c % AP_META][at] = vtk_sees(id[i], it.span.pmax, it.span.floor, a.sinks) ? slot[i] : -1;
                     const unsigned there = __ballot_sync(0xffffffffu, slot[i] >= 0);
                     const unsigned every0 = __ballot_sync(0xffffffffu, slot[i] >= 0 && vtk_sees(id[i], it.pmin[0], vtk_floor(it.pmax[0], a.window), a.sinks));
                     const unsigned every1 = __ballot_sync(0xffffffffu, slot[i] >= 0 && vtk_sees(id[i], it.pmin[1], vtk_floor(it.pmax[1], a.window), a.sinks));

@@ -241,3 +241,74 @@ def test_a_call_without_query_tokens_needs_no_tensors():
     st.run()
     assert st.c.flags() == 0
     st.c.close()
+
+
+# ---- values that a row may not see ----------------------------------------------------------------
+def poisoned(geometry, lens, positions, where, window=0, sinks=0, value=np.nan, **options):
+    """where: (request, id, 'k' or 'v') of rows whose value 3 of head 0 (its first group over 4 bits) is not finite."""
+    st = problem(np.random.default_rng(39), geometry, lens, positions, window=window, sinks=sinks, **options)
+    c = st.c
+    for r, tok, which in where:
+        s = int(st.slots[r][list(st.ids[r]).index(tok)])
+        pool, host = (c.k_pool, c.k64) if which == "k" else (c.v_pool, c.v64)
+        host[s] = host[s].copy()
+        if c.kv == "fp4":
+            pool[c.layer, s, c.hkv * c.d // 2] = 0x7f
+            host[s][0, :16] = np.nan
+        else:
+            pool[c.layer, s, 3] = value
+            host[s][0, 3] = value
+    return st
+
+
+def check_poisoned(st):
+    st.run()
+    out, _ = st.outputs()
+    ref, _, tol, _ = st.reference()
+    fine = np.isfinite(ref)
+    assert fine.any() and not fine.all()
+    assert np.array_equal(np.isfinite(out), fine)
+    assert (np.abs(out - ref)[fine] <= tol[fine]).all()
+    assert st.c.flags() == 0
+    st.c.close()
+
+
+@pytest.mark.parametrize("geometry", [("bf16", "bf16", 8, 2, 128), ("fp16", "fp16", 7, 1, 128), ("bf16", "fp4", 8, 2, 128), ("fp16", "fp4", 14, 2, 64)],
+                         ids=["bf16", "fp16", "fp4", "fp4-fp16"])
+@pytest.mark.parametrize("hint", [None, 1])
+@pytest.mark.parametrize("queries", [4, 300])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them_alone(geometry, hint, queries):
+    """Keys and values, in rows that some queries see and others do not (yet, or any more), next to rows that all of them see."""
+    n = 600
+    positions = [list(range(n - queries, n)), [40, 80, 20]]
+    for where in ([(0, n - queries // 2, "v")], [(0, n - queries // 2, "k"), (1, 50, "k")], [(0, 5, "v"), (0, n - 2, "v")],
+                  [(0, n - 1, "v"), (1, 30, "v"), (1, 60, "k")], [(0, 0, "v"), (0, n - 3, "k")]):
+        check_poisoned(poisoned(geometry, [n, 90], positions, where, max_query_len=hint))
+    for where in ([(0, n - queries - 20, "v")], [(0, n - queries - 20, "k"), (1, 30, "v")], [(0, 2, "v"), (0, n - queries // 2, "v")],
+                  [(0, n - queries, "v"), (0, n - queries - 10, "v"), (1, 1, "v")]):
+        check_poisoned(poisoned(geometry, [n, 90], positions, where, window=30, sinks=4, max_query_len=hint))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp4"])
+@pytest.mark.parametrize("queries,n", [(4096, 4096), (4, 60000)])
+def test_one_value_that_is_not_finite_does_not_slow_the_call_down(kv, queries, n):
+    """The first token is seen by every row: no row can be any better, and none is worked on again."""
+    import torch
+    times = []
+    for where in ([], [(0, 0, "v"), (0, 1, "k")]):
+        st = poisoned(("bf16", kv, 8, 2, 128), [n], [list(range(n - queries, n))], where, cache_options=dict(poison=False))
+        st.run()
+        best = 1e9
+        for _ in range(5):
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            e0.record()
+            st.call()
+            e1.record()
+            torch.cuda.synchronize()
+            best = min(best, e0.elapsed_time(e1))
+        times.append(best)
+        out, _ = st.outputs()
+        assert np.isfinite(out[:, 4:]).all()
+        assert np.isfinite(out[:, :4]).all() == (not where)
+        st.c.close()
+    assert times[1] < 4 * times[0] + 0.05, times

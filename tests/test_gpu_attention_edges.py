@@ -312,3 +312,40 @@ def test_one_value_that_is_not_finite_does_not_slow_the_call_down(kv, queries, n
         assert np.isfinite(out[:, :4]).all() == (not where)
         st.c.close()
     assert times[1] < 4 * times[0] + 0.05, times
+
+
+# ---- many heads side by side, several streams -----------------------------------------------------
+@pytest.mark.parametrize("act,hq,hkv,d", [("bf16", 16, 8, 128), ("fp16", 3, 3, 128), ("bf16", 20, 5, 64), ("fp16", 24, 12, 64), ("bf16", 12, 12, 128)])
+@pytest.mark.parametrize("many", [False, True])
+def test_many_requests_over_4_bits_and_many_heads(act, hq, hkv, d, many):
+    """So many requests that the heads of a row are read side by side by a team of warps, with key heads that do not fill it."""
+    rng = np.random.default_rng(40)
+    lens = [int(n) for n in rng.integers(1, 120, 300)]
+    positions = [[n - 1, max(0, n - 2), n // 2][:3 if many else 1] for n in lens]
+    run_and_check(problem(rng, (act, "fp4", hq, hkv, d), lens, positions, keep=0.8, window=60, sinks=2))
+
+
+def test_calls_that_overlap_on_two_streams():
+    """A workspace for each stream; one call of few rows and one of prompts at the same time, again and again."""
+    import torch
+    rng = np.random.default_rng(41)
+    few = problem(rng, ("bf16", "bf16", 8, 2, 128), [9000, 3000, 70], positions=[[8999], [2999], [69]])
+    many = problem(rng, ("fp16", "fp16", 7, 1, 128), [900, 300], positions=[list(range(300, 900)), list(range(300))])
+    few.run()
+    many.run()
+    want = [st.check() for st in (few, many)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        few.out_all.fill_(9.0)
+        many.out_all.fill_(9.0)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for st, s in zip((few, many), streams):
+                st.call(stream=s)
+        torch.cuda.synchronize()
+        for st, w in zip((few, many), want):
+            got = st.outputs()
+            assert np.array_equal(got[0], w[0]) and np.array_equal(got[1], w[1])
+    for st in (few, many):
+        assert st.c.flags() == 0
+        st.c.close()

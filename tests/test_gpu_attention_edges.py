@@ -349,3 +349,33 @@ def test_calls_that_overlap_on_two_streams():
     for st in (few, many):
         assert st.c.flags() == 0
         st.c.close()
+
+
+# ---- shapes and factors ---------------------------------------------------------------------------
+@pytest.mark.parametrize("geometry", [("bf16", "bf16", 64, 1, 128), ("fp16", "fp4", 96, 1, 64), ("bf16", "fp4", 99, 3, 128), ("fp16", "fp16", 300, 1, 64)],
+                         ids=["64", "96-4", "33-4", "300"])
+def test_many_query_heads_on_a_key_head(geometry):
+    """More than 32 rows from one query token, 128 and 256 rows from a few, tiles that end inside a token's heads."""
+    rng = np.random.default_rng(43)
+    run_and_check(problem(rng, geometry, [300, 1, 40, 7], positions=[[299], [0], [37, 38, 39], [6]]))
+    run_and_check(problem(rng, geometry, [300, 90], positions=[[200, 250, 280, 299], [80]], keep=0.5, window=33, sinks=2))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp4"])
+def test_more_prompts_than_threads(kv):
+    """600 requests of 40 query rows each, some without queries, some without entries."""
+    rng = np.random.default_rng(44)
+    lens = [int(n) for n in rng.integers(0, 50, 600)]
+    positions = [list(range(max(0, n - 5), max(5, n))) if i % 9 else [] for i, n in enumerate(lens)]
+    run_and_check(problem(rng, ("bf16", kv, 8, 1, 64), lens, positions))
+
+
+@pytest.mark.parametrize("geometry", [("bf16", "bf16", 8, 2, 128), ("fp16", "fp16", 7, 1, 128), ("bf16", "fp4", 8, 2, 128), ("fp16", "fp4", 14, 2, 64)],
+                         ids=["bf16", "fp16", "fp4", "fp4-fp16"])
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 1e-20, -3.0])
+def test_any_factor_of_the_scores(geometry, scale):
+    rng = np.random.default_rng(45)
+    for window in (0, 40):
+        st = problem(rng, geometry, [300, 33, 90], positions=[[299], [32], list(range(20, 90))], window=window)
+        st.sm_scale = scale
+        run_and_check(st)

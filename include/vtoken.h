@@ -42,7 +42,10 @@
  * changes it): when it runs out the warp sets VTOKEN_FLAG_TIMEOUT, gives its copies in flight a
  * bounded time to land and returns, so the kernel always ends and the context stays usable.  Rows
  * may then be missing: those of the item the warp was waiting for, of the items already in its
- * ring, of the rest of its ticket and of the ticket it had requested ahead.
+ * ring, of the rest of its ticket and of the ticket it had requested ahead.  In the prompt kernel
+ * of vtoken_attention the warps of a CTA also wait for one another's tiles, under the same limit;
+ * what may be missing there are the outputs of the item (256 query rows of a key head) and of the
+ * one the CTA had taken ahead.
  *
  * Threads: a context is not thread-safe.  Calls on one context must come from one thread at a
  * time; different contexts (different pools) are independent.
@@ -666,9 +669,12 @@ typedef struct {                   /* all pointers DEVICE */
 int64_t vtoken_attention_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens);
 
 /* out = softmax(sm_scale * q K^T) V over the cached tokens that the query sees, for the query rows of every
- * request; scores, softmax and sums in 32 bits.  A row that sees no token is zero, its lse minus infinity.
- * Tokens that no query of the row's request sees are not read; what a masked token holds (NaN, infinities) does
- * not reach a row that does not see it.  A slot outside the pool makes its token invisible
+ * request; scores, softmax statistics and sums in 32 bits.  The weights enter the product with V as 16-bit numbers: as the
+ * sum of two of them in the kernel for few rows over 16-bit rows (and over 4-bit rows with fp16 queries); rounded
+ * once to the queries' type in the prompt kernel over 16-bit rows, to half precision over 4-bit rows -- the sum
+ * under the quotient takes them unrounded.  A row that sees no token is zero, its lse minus infinity.
+ * Tokens that no query of the row's request sees are not read (the prompt kernel: no query of the 256 rows that
+ * share its tiles); what a masked token holds (NaN, infinities) does not reach a row that does not see it.  A slot outside the pool makes its token invisible
  * (VTOKEN_FLAG_BAD_SLOT).  Every row is summed in an order that depends on the sizes and the tables alone. */
 int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in,
                      void *cuda_stream);

@@ -2,14 +2,16 @@
 // generation tensor cores.
 //
 // 4 * D flops and one exponential per pair: 128 x 128 pairs of D 128 take the tensor pipe (8192 flops a cycle) as long as the
-// SM's 16 exponentials a cycle.  Measured, the copies are the bound: 64 KB of K and V rows for every pair of row tiles go through
-// cp.async at about 22 bytes a cycle and SM.  8192 tokens, 32 heads over 8: 669 us, 822 TFLOP/s; without exponentials, without the
-// softmax, or with an eighth of the products it takes 640 to 700.
+// SM's 16 exponentials a cycle, 2048 cycles for two row tiles and one of K and V.  Measured, those take about 5000, with no unit near
+// its limit (4096 tokens: tensor pipe 34 %, exponentials 35 %, issue slots 33 %, DRAM 3 %): the bound is the chain of hand-overs from
+// copy to scores to softmax to outputs to the free stage, and the barrier between items.  8192 tokens, 32 heads over 8: 655 to 687 us
+// from box to box, 800 to 840 TFLOP/s; at an earlier step without exponentials, softmax, copies or most of the products each 640 to 700.
 // One CTA per SM takes items (request, two tiles of 128 query rows, key head); the rows of a tile are the query
 // tokens of the request times the heads of the group, so a K or V tile is read once for all of them, and the two
 // row tiles share it again.  Roles, 16 warps:
 //   0 .. 3, 4 .. 7   softmax of row tile 0 and 1, one thread a row: scores from tensor memory, running maximum (moved
-//                    only when a score passes it by 2^8), exponentials, P as 16 bits back into the scores' columns
+//                    only when a score passes it by 2^8), exponentials, P as 16 bits back into the scores' columns (rounded once, as
+//                    a second product for the rest would double the tensor work: error against 64 bits 0.0021 for 0.0016, bf16)
 //   8 .. 11          producers: rows of Q, K and V gathered by slot into 128-byte-swizzled tiles, 16 bytes a thread by
 //                    cp.async, or 4-bit rows expanded to half precision in registers on the way
 //   12               one thread issues every tcgen05.mma: S = Q K^T (both operands from shared memory, K-major),

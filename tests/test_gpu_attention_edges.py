@@ -5,7 +5,7 @@ import pytest
 
 from attention_sim import Cache, Step, quantise_rows, dequantise_rows, spread, to64, torch_dtype, unit
 from paper_2608_13263_b200 import binding as vt
-from test_gpu_attention import problem, run_and_check
+from test_gpu_attention import GEOMETRIES, IDS, problem, run_and_check
 
 pytestmark = pytest.mark.gpu
 
@@ -379,3 +379,50 @@ def test_any_factor_of_the_scores(geometry, scale):
         st = problem(rng, geometry, [300, 33, 90], positions=[[299], [32], list(range(20, 90))], window=window)
         st.sm_scale = scale
         run_and_check(st)
+
+
+# ---- every value counts ---------------------------------------------------------------------------
+def held_to(st, row_tokens):
+    """Relative rounding of the weights on their way into the product with V: as the sum of two numbers (few rows over 16-bit rows), once
+    to the queries' type (prompts over 16-bit rows), once to half precision (over 4-bit rows)."""
+    c = st.c
+    few = st.max_query_len * c.hq // c.hkv <= 32 or row_tokens * c.hq // c.hkv <= 32
+    if c.kv == "fp4":
+        return 2.0 ** -12
+    return 2.0 ** -17 if few else (2.0 ** -9 if c.act == "bf16" else 2.0 ** -12)
+
+
+def check_sharply(st):
+    """Outputs within their own rounding and errors that are relative to the sum of w |v|, not to the largest |v|: one value that is
+    wrong among hundreds shows."""
+    st.run()
+    c = st.c
+    out, _ = st.outputs()
+    q = to64(st.q_all)[:st.n, :c.hq * c.d].reshape(st.n, c.hq, c.d)
+    for r in range(len(st.ids)):
+        for j, p in enumerate(st.positions[r]):
+            row = int(st.q_off[r]) + j
+            seen = [int(s) for i, s in zip(st.ids[r], st.slots[r]) if i <= p and (not st.window or i > p - st.window or i < st.sinks)]
+            if not seen:
+                assert (out[row] == 0).all()
+                continue
+            k, v = (np.repeat(np.stack([x[s] for s in seen]), c.hq // c.hkv, 1) for x in (c.k64, c.v64))
+            s = np.einsum("hd,lhd->hl", q[row], k) * st.sm_scale
+            w = np.exp(s - s.max(-1, keepdims=True))
+            w /= w.sum(-1, keepdims=True)
+            ref, mass = np.einsum("hl,lhd->hd", w, v), np.einsum("hl,lhd->hd", w, np.abs(v))
+            # scores as in attention_sim: D * 2^-23 of the sum of |q k|, on both sides of the quotient; sums of n / 8 additions each
+            ds = (c.d * 2.0 ** -23 * np.einsum("hd,lhd->hl", np.abs(q[row]), np.abs(k)) * abs(st.sm_scale)).max(-1) + 2.0 ** -20 * (1 + np.abs(s).max(-1))
+            soft = held_to(st, len(st.positions[r])) + 2 * ds[:, None] + (len(seen) / 8 + 64) * 2.0 ** -23
+            tol = 1.01 * unit(c.act) * np.abs(ref) + soft * mass + 2.0 ** -24
+            assert (np.abs(out[row] - ref) <= tol).all(), (r, j, (np.abs(out[row] - ref) / tol).max())
+    assert c.flags() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("geometry", GEOMETRIES, ids=IDS)
+def test_outputs_to_their_own_rounding(geometry):
+    rng = np.random.default_rng(46)
+    check_sharply(problem(rng, geometry, [1, 17, 64, 300, 1000, 3000]))
+    check_sharply(problem(rng, geometry, [400, 1500, 33], positions=[[399, 398], [1400, 1499], [30, 31, 32]], keep=0.6, window=200, sinks=4))
+    check_sharply(problem(rng, geometry, [300, 700, 20], positions=[list(range(250, 300)), list(range(640, 700)), list(range(20))], keep=0.8))

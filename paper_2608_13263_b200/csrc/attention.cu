@@ -1,7 +1,7 @@
 // Attention of few query rows per request (a decode step) over the slot cache.
 //
 // Bound by HBM: every visible K and V row is read once, 4 * D flops per row, head and query.  512 requests over 3.1 GB of
-// 16-bit rows take 536 to 564 us from box to box (5.5 to 5.8 TB/s, 0.85 to 0.89 of the copy bandwidth).  256 requests over 650 MB of
+// 16-bit rows take 536 to 564 us from machine to machine (5.5 to 5.8 TB/s, 0.85 to 0.89 of the copy bandwidth).  256 requests over 650 MB of
 // 4-bit rows take 238 us: there 63 % of the issue slots are taken (ALU 50 %, DRAM 33 %), by about 400 instructions for 16 tokens of
 // a head to expand codes and scales, and the warps, four a scheduler, wait on their own chains of them; the instantiation with 512
 // threads has 128 registers and spills (336 bytes of loads).  A small call takes 6 us of dependent loads (requests, lengths,

@@ -5,7 +5,7 @@
 // SM's 16 exponentials a cycle, 2048 cycles for two row tiles and one of K and V.  Measured, those take about 5000, with no unit near
 // its limit (4096 tokens: tensor pipe 34 %, exponentials 35 %, issue slots 33 %, DRAM 3 %): the bound is the chain of hand-overs from
 // copy to scores to softmax to outputs to the free stage, and the barrier between items.  8192 tokens, 32 heads over 8: 655 to 687 us
-// from box to box, 800 to 840 TFLOP/s; at an earlier step without exponentials, softmax, copies or most of the products each 640 to 700.
+// from machine to machine, 800 to 840 TFLOP/s; at an earlier step without exponentials, softmax, copies or most of the products each 640 to 700.
 // One CTA per SM takes items (request, two tiles of 128 query rows, key head); the rows of a tile are the query
 // tokens of the request times the heads of the group, so a K or V tile is read once for all of them, and the two
 // row tiles share it again.  Roles, 16 warps:

@@ -424,8 +424,8 @@ def _own_select(s):
     c, lib = s["case"], s["lib"]
     lib.vt.vtoken_select_victims(lib.ctx, num_requests=s["num_requests"], tt_offsets=s["tt_offsets"], cache_ids=s["cache_ids"],
                                  cache_len=s["cache_len"], scores=s["scores"], budget=s["budget"], shared_len=s["shared_len"],
-                                 sinks=c["sinks"], recent=c["recent"], victim_req=s["victim_req"], victim_tok=s["victim_tok"],
-                                 max_victims=s["victim_req"].shape[0], num_victims=s["num_victims"])
+                                 sinks=c["sinks"], recent=c["recent"], max_cache_len=s["max_live"],
+                                 victim_req=s["victim_req"], victim_tok=s["victim_tok"], max_victims=s["victim_req"].shape[0], num_victims=s["num_victims"])
     return s["victim_req"], s["victim_tok"], s["num_victims"]
 
 

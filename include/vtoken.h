@@ -679,6 +679,124 @@ int64_t vtoken_attention_workspace_bytes(const vtoken_ctx *ctx, const vtoken_hea
 int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in,
                      void *cuda_stream);
 
+/* ---- Which tokens leave the cache ------------------------------------------------------------------
+ * An eviction policy in two calls -- the attention weight that every cached token received, summed over
+ * queries, heads and, call by call, layers and steps; the tokens with the lowest sums, as the victims
+ * that vtoken_evict_tokens and vtoken_slot_cache_mark take -- and the verification of drafted tokens,
+ * whose rejected ones leave the cache the same way.  They only enqueue kernels on the stream and are
+ * capturable. */
+typedef struct {                   /* all pointers DEVICE; the fields of vtoken_attention_in have its meaning */
+    const int32_t *num_requests, *q_offsets, *positions;
+    const void *q;
+    int64_t q_stride;
+    int32_t max_query_tokens, max_query_len;
+    const int32_t *tt_offsets, *cache_slots, *cache_ids, *cache_len;
+    const float *lse;              /* [max_query_tokens][num_q_heads] as vtoken_attention left it for these queries */
+    float sm_scale;
+    int32_t window, sinks;
+    float decay;                   /* finite; factor of the score that a token had */
+    const float *prev;             /* [max_tokens of the context] scores before the call; may be `scores` itself; NULL, or
+                                      decay 0: none (nothing is read there) */
+    float *scores;                 /* [max_tokens of the context] token i of request r is at tt_offsets[r] + i */
+    void *workspace;               /* as in vtoken_attention_in */
+    int64_t workspace_bytes;       /* >= vtoken_token_weights_workspace_bytes (VTOKEN_ECAPACITY otherwise) */
+} vtoken_weights_in;
+
+/* Bytes of workspace for calls of up to max_query_tokens rows on this context; negative: VTOKEN_EINVAL. */
+int64_t vtoken_token_weights_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens);
+
+/* For every request that has query rows and every one of its active tokens t (cache entries; id_t its id):
+ *   scores[tt_offsets[r] + id_t] = decay * prev[tt_offsets[r] + id_t] +
+ *                                  sum over query rows i that see t and heads h of exp(sm_scale * q_ih k_t - lse_ih)
+ * A token that no row sees gets decay * prev.  Requests without query rows, and entries of tokens that are not
+ * active, are neither read nor written.  Scores, exponentials and sums in 32 bits; what a masked key holds does
+ * not matter, a row whose lse is minus infinity adds nothing.  A slot outside the pool makes its token invisible
+ * (VTOKEN_FLAG_BAD_SLOT); an id outside the table of its request is skipped (VTOKEN_FLAG_BAD_VICTIM).  Every sum is
+ * taken in an order that depends on the sizes and the tables alone. */
+int vtoken_token_weights(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_weights_in *in,
+                         void *cuda_stream);
+
+typedef struct {                   /* all pointers DEVICE */
+    const int32_t *num_requests;   /* device scalar R <= max_requests of the context */
+    const int32_t *tt_offsets;     /* [R+1] */
+    const int32_t *cache_ids;      /* ids of the active tokens at tt_offsets[r] .., strictly ascending from 0 or above; NULL:
+                                      0, 1, 2, ... */
+    const int32_t *cache_len;      /* [R] active tokens */
+    const float *scores;           /* [max_tokens of the context] token i of request r is at tt_offsets[r] + i */
+    const int32_t *budget;         /* [R] active tokens that a request is cut back to (below 0 counts as 0) */
+    const int32_t *shared_len;     /* [R] or NULL: first cache entries that stay (a prefix shared with other requests) */
+    int32_t sinks;                 /* ids below this stay */
+    int32_t recent;                /* the last `recent` cache entries stay */
+    int32_t max_cache_len;         /* a hint: longest cache_len, >= 1.  It chooses how many SMs work on one request; right
+                                      for every length */
+    int32_t *victim_req, *victim_tok;   /* [max_victims] */
+    int32_t max_victims;
+    int32_t *num_victims;          /* device scalar */
+} vtoken_select_in;
+
+/* Cuts every request back to its budget: of its entries that may leave (not among the first shared_len[r] nor the
+ * last `recent`, id >= sinks) those with the lowest scores leave, as many as are needed, all of them if that is not
+ * enough; of equal scores (-0 equals 0) the earlier entry stays, a NaN counts as lower than every number.  The victims are
+ * listed by request, then ascending id.  An id outside the table of its request has no score: it counts as NaN
+ * (VTOKEN_FLAG_BAD_VICTIM).  Victims beyond max_victims are dropped (VTOKEN_FLAG_CAPACITY); *num_victims is the number
+ * listed.  Scores, ids and tables are only read. */
+int vtoken_select_victims(vtoken_ctx *ctx, const vtoken_select_in *in, void *cuda_stream);
+
+enum { VTOKEN_PROB_BF16 = 0, VTOKEN_PROB_FP16 = 1, VTOKEN_PROB_F32 = 2 };
+
+typedef struct {                   /* all pointers DEVICE */
+    const int32_t *num_requests;   /* device scalar R <= max_requests of the context */
+    const int32_t *draft_offsets;  /* [R+1] first draft of each request, non-decreasing from 0 */
+    int32_t max_drafts;            /* rows of the draft arrays; draft_offsets beyond it are clipped (VTOKEN_FLAG_CAPACITY).
+                                      0: no request has drafts, the draft arrays may be NULL */
+    const int32_t *draft_tokens;   /* [max_drafts] */
+    int32_t prob_type;             /* VTOKEN_PROB_* */
+    int32_t vocab;                 /* 1 .. 2^30 */
+    const void *target_probs;      /* [max_drafts + max_requests][vocab]: request r has one row more than drafts, from row
+                                      draft_offsets[r] + r on; row i: given the tokens before its draft i */
+    int64_t target_stride;         /* elements between rows; 0: vocab */
+    const void *draft_probs;       /* [max_drafts][vocab] what each draft was drawn from, or NULL: it was the only choice */
+    int64_t draft_stride;
+    const float *accept_random;    /* [max_drafts] uniform in [0, 1) */
+    const float *sample_random;    /* [R] uniform in [0, 1) */
+    const int32_t *first_id;       /* [R] logical id of each request's first draft; needed for the victims only */
+    int32_t *accepted;             /* [R] drafts accepted */
+    int32_t *next_tokens;          /* [R] the token behind them */
+    int32_t *out_tokens;           /* [max_drafts + max_requests] or NULL: per request, from draft_offsets[r] + r on, the accepted
+                                      drafts, the next token, -1 */
+    int32_t *victim_req, *victim_tok;   /* [max_victims] or NULL (with num_victims NULL): the rejected drafts, by request, then
+                                      ascending id */
+    int32_t max_victims;
+    int32_t *num_victims;          /* device scalar */
+} vtoken_verify_in;
+
+/* Per request, with p_i the target's rows, q_i the drafts' (one at the draft and zero elsewhere without draft_probs), x_i the
+ * drafts: draft i is accepted while all before it were and accept_random * q_i(x_i) < p_i(x_i).  The next token is drawn from
+ * max(0, p_i - q_i) at the first rejected draft (from p_i if that has no mass), from the last row when none was rejected: the
+ * first token whose cumulated mass exceeds sample_random times all of it.  Products and sums in 64 bits.  A probability that is
+ * not a positive finite number counts as 0, and so does that of a draft outside [0, vocab); a row without mass gives the token -1.
+ * Victims beyond max_victims are dropped (VTOKEN_FLAG_CAPACITY). */
+int vtoken_verify_drafts(vtoken_ctx *ctx, const vtoken_verify_in *in, void *cuda_stream);
+
+/* ---- Attention behind shared prefixes --------------------------------------------------------------- */
+typedef struct {                   /* all pointers DEVICE */
+    const int32_t *num_groups;     /* device scalar, 0 .. max_requests */
+    const int32_t *group_offsets;  /* [num_groups+1] non-decreasing: requests [group_offsets[g], group_offsets[g+1]) share a prefix;
+                                      requests outside every group share nothing */
+    const int32_t *shared_len;     /* [R] the first shared_len[r] cache entries of request r -- slots and ids -- are those of the
+                                      first request of its group; the smallest of a group counts */
+} vtoken_shared_in;
+
+/* Bytes of workspace for calls of up to max_query_tokens rows on this context; negative: VTOKEN_EINVAL. */
+int64_t vtoken_attention_shared_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens);
+
+/* vtoken_attention (same arguments, results and masks; in->workspace_bytes >= vtoken_attention_shared_workspace_bytes) for
+ * requests whose caches begin with the same entries, as the planners' protected blocks hold them: the rows of a prefix are read
+ * once for the query rows of its whole group, and each request goes on over its own entries from there.  Requests of more than
+ * 32 query rows (tokens times heads of a key head) read the prefix for themselves. */
+int vtoken_attention_shared(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in,
+                            const vtoken_shared_in *shared, void *cuda_stream);
+
 /* Diagnostics. */
 const char *vtoken_strerror(int code);
 int vtoken_last_cuda_error(const vtoken_ctx *ctx);       /* cudaError_t of the last VTOKEN_ECUDA */

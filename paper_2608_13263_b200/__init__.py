@@ -9,9 +9,15 @@ built library raises ImportError.
 from .binding import (  # noqa: F401
     Heads,
     vtoken_attention,
+    vtoken_attention_shared,
+    vtoken_attention_shared_workspace_bytes,
     vtoken_attention_workspace_bytes,
     vtoken_kv_row_bytes,
     vtoken_read_tokens,
+    vtoken_select_victims,
+    vtoken_token_weights,
+    vtoken_token_weights_workspace_bytes,
+    vtoken_verify_drafts,
     vtoken_write_tokens,
     VtokenError,
     vtoken_apply_moves,
@@ -48,4 +54,6 @@ __all__ = ["VtokenError", "vtoken_create", "vtoken_destroy", "vtoken_plan", "vto
            "vtoken_repack_host_partial", "vtoken_repack_waves", "vtoken_waves_workspace_bytes", "vtoken_slot_cache_mark",
            "vtoken_slot_cache_update", "vtoken_check_tables", "vtoken_evict_tokens_counted",
            "vtoken_sync_new_tokens_counted", "Heads", "vtoken_kv_row_bytes", "vtoken_write_tokens",
-           "vtoken_read_tokens", "vtoken_attention", "vtoken_attention_workspace_bytes"]
+           "vtoken_read_tokens", "vtoken_attention", "vtoken_attention_workspace_bytes",
+           "vtoken_token_weights", "vtoken_token_weights_workspace_bytes", "vtoken_select_victims", "vtoken_verify_drafts",
+           "vtoken_attention_shared", "vtoken_attention_shared_workspace_bytes"]

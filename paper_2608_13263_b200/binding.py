@@ -18,6 +18,7 @@ NOT_SELECTED, REPACKED, NO_GAIN, DEFERRED_NO_FREE = 0, 1, 2, 3
 FLAG_BAD_SLOT, FLAG_BAD_BLOCK, FLAG_BAD_FREE, FLAG_CAPACITY, FLAG_TIMEOUT, FLAG_GATHER_OVERFLOW = 1, 2, 4, 8, 16, 32
 FLAG_BAD_VICTIM, FLAG_APPEND_STOPPED, FLAG_CHECK_FAILED, FLAG_BAD_POSITION = 64, 128, 256, 512
 KV_BF16, KV_FP16, KV_FP4 = 0, 1, 2
+PROB_BF16, PROB_FP16, PROB_F32 = 0, 1, 2
 
 SYMBOLS = ["vtoken_create", "vtoken_destroy", "vtoken_plan", "vtoken_repack", "vtoken_gather_logical",
            "vtoken_read_counts", "vtoken_repack_host", "vtoken_strerror", "vtoken_last_cuda_error",
@@ -28,7 +29,9 @@ SYMBOLS = ["vtoken_create", "vtoken_destroy", "vtoken_plan", "vtoken_repack", "v
            "vtoken_slot_cache_update", "vtoken_repack_host_partial", "vtoken_check_tables",
            "vtoken_evict_tokens_counted", "vtoken_sync_new_tokens_counted", "vtoken_checked_build",
            "vtoken_debug_probe", "vtoken_kv_row_bytes", "vtoken_write_tokens", "vtoken_read_tokens",
-           "vtoken_attention_workspace_bytes", "vtoken_attention"]
+           "vtoken_attention_workspace_bytes", "vtoken_attention", "vtoken_token_weights_workspace_bytes",
+           "vtoken_token_weights", "vtoken_select_victims", "vtoken_verify_drafts",
+           "vtoken_attention_shared_workspace_bytes", "vtoken_attention_shared"]
 
 
 class VtokenError(RuntimeError):
@@ -135,6 +138,38 @@ class AttentionIn(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_int64)]
 
 
+class WeightsIn(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_void_p), ("q_offsets", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("max_query_tokens", ctypes.c_int32),
+                ("max_query_len", ctypes.c_int32), ("tt_offsets", ctypes.c_void_p), ("cache_slots", ctypes.c_void_p),
+                ("cache_ids", ctypes.c_void_p), ("cache_len", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("sm_scale", ctypes.c_float), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("decay", ctypes.c_float), ("prev", ctypes.c_void_p), ("scores", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
+
+
+class SelectIn(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_void_p), ("tt_offsets", ctypes.c_void_p), ("cache_ids", ctypes.c_void_p),
+                ("cache_len", ctypes.c_void_p), ("scores", ctypes.c_void_p), ("budget", ctypes.c_void_p),
+                ("shared_len", ctypes.c_void_p), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("max_cache_len", ctypes.c_int32), ("victim_req", ctypes.c_void_p), ("victim_tok", ctypes.c_void_p),
+                ("max_victims", ctypes.c_int32), ("num_victims", ctypes.c_void_p)]
+
+
+class VerifyIn(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_void_p), ("draft_offsets", ctypes.c_void_p), ("max_drafts", ctypes.c_int32),
+                ("draft_tokens", ctypes.c_void_p), ("prob_type", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("target_probs", ctypes.c_void_p), ("target_stride", ctypes.c_int64), ("draft_probs", ctypes.c_void_p),
+                ("draft_stride", ctypes.c_int64), ("accept_random", ctypes.c_void_p),
+                ("sample_random", ctypes.c_void_p), ("first_id", ctypes.c_void_p), ("accepted", ctypes.c_void_p),
+                ("next_tokens", ctypes.c_void_p), ("out_tokens", ctypes.c_void_p), ("victim_req", ctypes.c_void_p),
+                ("victim_tok", ctypes.c_void_p), ("max_victims", ctypes.c_int32), ("num_victims", ctypes.c_void_p)]
+
+
+class SharedIn(ctypes.Structure):
+    _fields_ = [("num_groups", ctypes.c_void_p), ("group_offsets", ctypes.c_void_p), ("shared_len", ctypes.c_void_p)]
+
+
 _lib = None
 _libs = {}
 _flavour = "production"
@@ -222,6 +257,15 @@ def load():
         lib.vtoken_attention_workspace_bytes.restype = ctypes.c_int64
         lib.vtoken_attention.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32,
                                          ctypes.POINTER(AttentionIn), ctypes.c_void_p]
+        for name in ("vtoken_token_weights_workspace_bytes", "vtoken_attention_shared_workspace_bytes"):
+            getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32]
+            getattr(lib, name).restype = ctypes.c_int64
+        lib.vtoken_token_weights.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32,
+                                             ctypes.POINTER(WeightsIn), ctypes.c_void_p]
+        lib.vtoken_select_victims.argtypes = [ctypes.c_void_p, ctypes.POINTER(SelectIn), ctypes.c_void_p]
+        lib.vtoken_verify_drafts.argtypes = [ctypes.c_void_p, ctypes.POINTER(VerifyIn), ctypes.c_void_p]
+        lib.vtoken_attention_shared.argtypes = [ctypes.c_void_p, ctypes.POINTER(Heads), ctypes.c_int32,
+                                                ctypes.POINTER(AttentionIn), ctypes.POINTER(SharedIn), ctypes.c_void_p]
         _libs[path] = lib
         _lib = lib
     return _lib
@@ -572,3 +616,70 @@ def vtoken_attention(ctx, *, heads, layer, num_requests, q_offsets, positions, q
     rc = load().vtoken_attention(ctx, heads, layer, a, _stream(stream))
     if rc != OK:
         _check(rc, "vtoken_attention", ctx)
+
+
+# ---- which tokens leave the cache --------------------------------------------------------------
+def vtoken_token_weights_workspace_bytes(ctx, heads, max_query_tokens) -> int:
+    n = load().vtoken_token_weights_workspace_bytes(ctx, ctypes.byref(heads), max_query_tokens)
+    if n < 0:
+        raise VtokenError(int(n), "vtoken_token_weights_workspace_bytes")
+    return n
+
+
+def vtoken_token_weights(ctx, *, heads, layer, num_requests, q_offsets, positions, q, max_query_tokens, max_query_len,
+                         tt_offsets, cache_slots, cache_len, lse, sm_scale, scores, workspace, workspace_bytes,
+                         cache_ids=None, window=0, sinks=0, decay=1.0, prev=None, q_stride=0, stream=None) -> None:
+    """The attention weight that every active token received from the queries, added to its decayed score."""
+    a = WeightsIn(_ptr(num_requests), _ptr(q_offsets), _ptr(positions), _ptr(q), q_stride, max_query_tokens,
+                  max_query_len, _ptr(tt_offsets), _ptr(cache_slots), _ptr(cache_ids), _ptr(cache_len), _ptr(lse), sm_scale,
+                  window, sinks, decay, _ptr(prev), _ptr(scores), _ptr(workspace), workspace_bytes)
+    rc = load().vtoken_token_weights(ctx, heads, layer, a, _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_token_weights", ctx)
+
+
+def vtoken_select_victims(ctx, *, num_requests, tt_offsets, cache_len, scores, budget, victim_req, victim_tok, max_victims,
+                          num_victims, max_cache_len, cache_ids=None, shared_len=None, sinks=0, recent=0, stream=None) -> None:
+    """The tokens that leave when every request is cut back to its budget: the lowest scores."""
+    a = SelectIn(_ptr(num_requests), _ptr(tt_offsets), _ptr(cache_ids), _ptr(cache_len), _ptr(scores), _ptr(budget),
+                 _ptr(shared_len), sinks, recent, max_cache_len, _ptr(victim_req), _ptr(victim_tok), max_victims,
+                 _ptr(num_victims))
+    rc = load().vtoken_select_victims(ctx, a, _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_select_victims", ctx)
+
+
+def vtoken_verify_drafts(ctx, *, num_requests, draft_offsets, max_drafts, draft_tokens, prob_type, vocab, target_probs,
+                         accept_random, sample_random, accepted, next_tokens, draft_probs=None, target_stride=0,
+                         draft_stride=0, first_id=None, out_tokens=None, victim_req=None, victim_tok=None, max_victims=0,
+                         num_victims=None, stream=None) -> None:
+    """Drafted tokens accepted or refused by the target's probabilities, and the token behind the accepted ones."""
+    a = VerifyIn(_ptr(num_requests), _ptr(draft_offsets), max_drafts, _ptr(draft_tokens), prob_type, vocab,
+                 _ptr(target_probs), target_stride, _ptr(draft_probs), draft_stride, _ptr(accept_random),
+                 _ptr(sample_random), _ptr(first_id), _ptr(accepted), _ptr(next_tokens), _ptr(out_tokens), _ptr(victim_req),
+                 _ptr(victim_tok), max_victims, _ptr(num_victims))
+    rc = load().vtoken_verify_drafts(ctx, a, _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_verify_drafts", ctx)
+
+
+# ---- attention behind shared prefixes -----------------------------------------------------------
+def vtoken_attention_shared_workspace_bytes(ctx, heads, max_query_tokens) -> int:
+    n = load().vtoken_attention_shared_workspace_bytes(ctx, ctypes.byref(heads), max_query_tokens)
+    if n < 0:
+        raise VtokenError(int(n), "vtoken_attention_shared_workspace_bytes")
+    return n
+
+
+def vtoken_attention_shared(ctx, *, heads, layer, num_requests, q_offsets, positions, q, max_query_tokens, max_query_len,
+                            tt_offsets, cache_slots, cache_len, out, sm_scale, num_groups, group_offsets, shared_len,
+                            workspace, workspace_bytes, cache_ids=None, lse=None, window=0, sinks=0, q_stride=0,
+                            out_stride=0, stream=None) -> None:
+    """vtoken_attention for groups of requests whose caches begin with the same entries."""
+    a = AttentionIn(_ptr(num_requests), _ptr(q_offsets), _ptr(positions), _ptr(q), q_stride, max_query_tokens,
+                    max_query_len, _ptr(tt_offsets), _ptr(cache_slots), _ptr(cache_ids), _ptr(cache_len), sm_scale,
+                    window, sinks, _ptr(out), out_stride, _ptr(lse), _ptr(workspace), workspace_bytes)
+    b = SharedIn(_ptr(num_groups), _ptr(group_offsets), _ptr(shared_len))
+    rc = load().vtoken_attention_shared(ctx, heads, layer, a, b, _stream(stream))
+    if rc != OK:
+        _check(rc, "vtoken_attention_shared", ctx)

@@ -23,11 +23,12 @@ LIB = os.path.join(PKG, "libvtoken.so")
 CHECKED_LIB = os.path.join(PKG, "libvtoken_checked.so")
 
 LIB_SOURCES = ["api.cu", "plan.cu", "plan_small.cu", "copy.cu", "gather.cu", "gather_static.cu", "runtime.cu", "plan_partial.cu",
-               "waves.cu", "slot_cache.cu", "check.cu", "tokens.cu", "attention.cu", "attention_prompt.cu"]
-HEADERS = ["common.cuh", "heads.cuh", "attention.cuh"]
+               "waves.cu", "slot_cache.cu", "check.cu", "tokens.cu", "attention.cu", "attention_prompt.cu",
+               "attention_shared.cu", "weights.cu", "victims.cu", "verify.cu"]
+HEADERS = ["common.cuh", "cluster.cuh", "heads.cuh", "attention.cuh", "weights.cuh"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC",
+              "-shared", "-Xcompiler", "-fPIC", "--threads", "0",
               "-cudart", "static"]
 
 

@@ -840,14 +840,6 @@ int launch_by_type(vtoken_ctx *ctx, bool fp4, bool wide, const VtkAttnArgs &a, c
     return wide ? launch<D, 16, Rows16<D, Act>, Act, true>(ctx, a, st) : launch<D, 8, Rows16<D, Act>, Act, true>(ctx, a, st);
 }
 
-float two_to(int e)
-{
-    float x = 1.f;
-    for (; e > 0; --e) x *= 2.f;
-    for (; e < 0; ++e) x *= 0.5f;
-    return x;
-}
-
 }  // namespace
 
 // A share leaves parts of at most two segments for each of its heads; shares times heads are at most 16 a CTA with 8
@@ -883,8 +875,8 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     if (!in->num_requests || !in->q_offsets || !in->tt_offsets || !in->cache_slots || !in->cache_len || !in->workspace) return VTOKEN_EINVAL;
     if (in->max_query_tokens != 0 && (!in->positions || !in->q || !in->out)) return VTOKEN_EINVAL;     // (without elements: no address)
     if (in->max_query_tokens < 0 || in->max_query_len < 1 || in->window < 0 || in->sinks < 0) return VTOKEN_EINVAL;
-    const float scale = in->sm_scale * 1.4426950408889634f * two_to(heads->k_exponent);
-    if (!(in->sm_scale > -1e30f && in->sm_scale < 1e30f) || !(scale > -INFINITY && scale < INFINITY)) return VTOKEN_EINVAL;
+    float scale;
+    if (!vtk_score_scale(heads, in->sm_scale, scale)) return VTOKEN_EINVAL;
     if ((((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)in->workspace) & 15) || ((uintptr_t)in->lse & 3)) return VTOKEN_EINVAL;
     VtkAttnArgs a;
     const int64_t dense = (int64_t)heads->num_q_heads * heads->head_dim;
@@ -917,7 +909,7 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     a.window = in->window;
     a.sinks = in->window > 0 ? in->sinks : 0;
     a.scale_log2 = scale;
-    a.v_mul = two_to(heads->v_exponent);
+    a.v_mul = vtk_two_to(heads->v_exponent);
     a.flags = &ctx->rt_counts->error_flags;
     a.counters = (uint32_t *)in->workspace + 4;
     a.part = nullptr;

@@ -323,6 +323,22 @@ inline cudaError_t vtk_allow_smem(const vtoken_ctx *ctx, std::atomic<int> &allow
     return e;
 }
 
+// host: 2^e
+inline float vtk_two_to(int e)
+{
+    float x = 1.f;
+    for (; e > 0; --e) x *= 2.f;
+    for (; e < 0; ++e) x *= 0.5f;
+    return x;
+}
+
+// host: the factor of the scores as an exponent of two, with that of the keys; false when it leaves 32 bits
+inline bool vtk_score_scale(const vtoken_heads *heads, float sm_scale, float &scale)
+{
+    scale = sm_scale * 1.4426950408889634f * vtk_two_to(heads->k_exponent);
+    return sm_scale > -1e30f && sm_scale < 1e30f && scale > -INFINITY && scale < INFINITY;
+}
+
 // host: launchers of attention.cu and of attention_prompt.cu
 int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st);
 int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st);

@@ -1,0 +1,355 @@
+// Verification of drafted tokens: the first refusal, the row to draw from, the draw, the list of rejected drafts.
+//
+// Bound by the row of the vocabulary (two after a refusal) that the next token is drawn from.  A cluster works on a request; its
+// warps take consecutive runs of the row and sum them in 64 bits, the CTAs exchange their sums, and the one warp whose run holds the
+// drawn mass walks over its run again.  The drafts before it need two numbers each.  One more cluster tests the drafts of all
+// requests and lists the rejected ones, so that a step is one launch.
+#include "cluster.cuh"
+#include "heads.cuh"
+
+namespace {
+
+constexpr int VD_NT = 512, VD_WARPS = VD_NT / 32, VD_LANES = 8;     // VD_LANES: threads that test the drafts of a request
+
+struct VerifyArgs {
+    const int32_t *num_requests;
+    vtk_arr<const int32_t> draft_offsets, draft_tokens, first_id;
+    const void *target, *draft;
+    int64_t target_stride, draft_stride;
+    vtk_arr<const float> accept_random, sample_random;
+    vtk_arr<int32_t> accepted, next_tokens, out_tokens, victim_req, victim_tok;
+    int32_t *num_victims;
+    int32_t vocab, max_drafts, max_requests, max_victims;
+    uint32_t *flags;
+};
+
+struct F32 {
+    using type = float;
+    static constexpr int VE = 4;
+    static __device__ __forceinline__ float get(float x) { return x; }
+    static __device__ __forceinline__ void unpack(uint4 w, float (&x)[4])
+    {
+        x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+    }
+};
+template <typename T>
+struct Half {
+    using type = uint16_t;
+    static constexpr int VE = 8;
+    static __device__ __forceinline__ float get(uint16_t x) { return T::unpack(x).x; }
+    static __device__ __forceinline__ void unpack(uint4 w, float (&x)[8]) { vtk_unpack8<T>(w, x); }
+};
+
+// what a probability counts for
+__device__ __forceinline__ float mass(float x) { return x > 0.f && x < INFINITY ? x : 0.f; }
+
+struct Drafts { int d0, k; };
+__device__ __forceinline__ Drafts drafts_of(const VerifyArgs &a, int r, bool &clipped)
+{
+    Drafts d;
+    if (a.max_drafts == 0) { d.d0 = d.k = 0; return d; }
+    const int o0 = a.draft_offsets[r], o1 = a.draft_offsets[r + 1];
+    d.d0 = o0 < 0 ? 0 : (o0 > a.max_drafts ? a.max_drafts : o0);
+    const int end = o1 < d.d0 ? d.d0 : (o1 > a.max_drafts ? a.max_drafts : o1);
+    d.k = end - d.d0;
+    clipped |= d.d0 != o0 || end != o1;
+    return d;
+}
+
+template <typename P>
+__device__ __forceinline__ bool refused(const VerifyArgs &a, int r, const Drafts &d, int i)
+{
+    using T = typename P::type;
+    const int x = a.draft_tokens[d.d0 + i];
+    float p = 0.f, q = a.draft == nullptr ? 1.f : 0.f;
+    if (x >= 0 && x < a.vocab) {
+        p = mass(P::get(static_cast<const T *>(a.target)[(int64_t)(d.d0 + r + i) * a.target_stride + x]));
+        if (a.draft != nullptr) q = mass(P::get(static_cast<const T *>(a.draft)[(int64_t)(d.d0 + i) * a.draft_stride + x]));
+    }
+    return !((double)a.accept_random[d.d0 + i] * (double)q < (double)p);
+}
+
+// the row that a token is drawn from: p, or what p has more than q, or p without one token
+template <typename P, bool VEC>
+struct Row {
+    using T = typename P::type;
+    const T *p, *q;
+    int without, vocab;
+    // masses of the elements [at, at + VE), zero behind the vocabulary
+    __device__ __forceinline__ void get(int at, float (&x)[P::VE], float (&y)[P::VE]) const
+    {
+        if (VEC && at + P::VE <= vocab) {
+            P::unpack(*reinterpret_cast<const uint4 *>(p + at), x);
+            if (q != nullptr) P::unpack(*reinterpret_cast<const uint4 *>(q + at), y);
+        } else {
+#pragma unroll
+            for (int e = 0; e < P::VE; ++e) {
+                x[e] = at + e < vocab ? P::get(p[at + e]) : 0.f;
+                y[e] = q != nullptr && at + e < vocab ? P::get(q[at + e]) : 0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ double value(int at, float x, float y) const
+    {
+        double v = (double)mass(x);
+        if (q != nullptr) v = fmax(v - (double)mass(y), 0.0);
+        return at == without ? 0.0 : v;
+    }
+};
+
+struct Shared {
+    double warp_sum[VD_WARPS], cta_sum[2];
+    int at;                              // first refusal, or the number of drafts
+    int scan[VD_WARPS + 1];
+};
+
+// cluster `last` of the grid: every request's drafts, the rejected ones in a list
+template <typename P>
+__device__ void list_rejected(const VerifyArgs &a, Shared &sh, int R, bool &clipped)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, sub = tid % VD_LANES;
+    int64_t base = 0;
+    for (int r0 = 0; r0 < R; r0 += VD_NT / VD_LANES) {
+        const int r = r0 + tid / VD_LANES;
+        Drafts d = {0, 0};
+        if (r < R) d = drafts_of(a, r, clipped);
+        int at = d.k;
+        for (int i = sub; i < at; i += VD_LANES)
+            if (refused<P>(a, r, d, i)) at = i;              // (the lane's first; the loop ends)
+#pragma unroll
+        for (int s = VD_LANES / 2; s > 0; s >>= 1) {
+            const int o = __shfl_xor_sync(0xffffffffu, at, s);
+            at = o < at ? o : at;
+        }
+        const int mine = sub == 0 ? d.k - at : 0, incl = vtk_warp_incl_scan(mine);
+        if (lane == 31) sh.scan[warp] = incl;
+        __syncthreads();
+        int64_t before = base;
+        for (int w = 0; w < VD_WARPS; ++w) {
+            if (w < warp) before += sh.scan[w];
+            base += sh.scan[w];
+        }
+        before += __shfl_sync(0xffffffffu, incl - mine, lane & ~(VD_LANES - 1));
+        for (int i = at + sub; i < d.k; i += VD_LANES) {
+            const int64_t to = before + (i - at);
+            if (to < a.max_victims) {
+                a.victim_req[to] = r;
+                a.victim_tok[to] = a.first_id[r] + i;
+            }
+        }
+        __syncthreads();
+    }
+    if (tid == 0) {
+        *a.num_victims = base > a.max_victims ? a.max_victims : (int)base;
+        clipped |= base > a.max_victims;
+    }
+}
+
+template <typename P, bool VEC>
+__global__ void __launch_bounds__(VD_NT) verify_kernel(const __grid_constant__ VerifyArgs a, int row_clusters)
+{
+    using T = typename P::type;
+    constexpr int VE = P::VE, STEP = 32 * VE;
+    __shared__ Shared sh;
+    vtk_release_successor();
+    vtk_wait_for_predecessor();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int C = vtk_cluster_size(), rank = vtk_cluster_rank(), cluster = blockIdx.x / C;
+    int R = *a.num_requests;
+    bool clipped = R < 0 || R > a.max_requests;
+    R = R < 0 ? 0 : (R > a.max_requests ? a.max_requests : R);
+    if (cluster >= row_clusters) {
+        if (rank == 0) list_rejected<P>(a, sh, R, clipped);
+        if (clipped) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
+        return;
+    }
+    // the warp's run of every row
+    const int per = ((a.vocab + C * VD_WARPS - 1) / (C * VD_WARPS) + STEP - 1) / STEP * STEP;
+    const int64_t run0 = (int64_t)(rank * VD_WARPS + warp) * per;
+    const int lo = run0 < a.vocab ? (int)run0 : a.vocab, hi = run0 + per < a.vocab ? (int)run0 + per : a.vocab;
+    int turn = 0;
+    for (int r = cluster; r < R; r += row_clusters) {
+        const Drafts d = drafts_of(a, r, clipped);
+        if (warp == 0) {
+            int at = d.k;
+            for (int i0 = 0; i0 < d.k && at == d.k; i0 += 32) {
+                const unsigned no = __ballot_sync(0xffffffffu, i0 + lane < d.k && refused<P>(a, r, d, i0 + lane));
+                if (no) at = i0 + __ffs(no) - 1;
+            }
+            if (lane == 0) sh.at = at;
+        }
+        __syncthreads();
+        const int at = sh.at;
+        Row<P, VEC> row;
+        row.vocab = a.vocab;
+        row.p = static_cast<const T *>(a.target) + (int64_t)(d.d0 + r + at) * a.target_stride;
+        row.q = at < d.k && a.draft != nullptr ? static_cast<const T *>(a.draft) + (int64_t)(d.d0 + at) * a.draft_stride : nullptr;
+        row.without = at < d.k && a.draft == nullptr ? a.draft_tokens[d.d0 + at] : -1;
+        if (rank == 0) {
+            if (tid == 0) a.accepted[r] = at;
+            if (!a.out_tokens.null())
+                for (int i = tid; i <= d.k; i += VD_NT)
+                    if (i != at) a.out_tokens[d.d0 + r + i] = i < at ? a.draft_tokens[d.d0 + i] : -1;
+        }
+        double before, total;
+        for (;;) {
+            double sum = 0.0;
+            constexpr int U = 4;
+            for (int i = lo + lane * VE; i < hi; i += STEP * U) {
+                float x[U][VE], y[U][VE];
+#pragma unroll
+                for (int u = 0; u < U; ++u) row.get(i + u * STEP < hi ? i + u * STEP : a.vocab, x[u], y[u]);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) sum += i + u * STEP < hi ? row.value(i + u * STEP + e, x[u][e], y[u][e]) : 0.0;
+            }
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+            if (lane == 0) sh.warp_sum[warp] = sum;
+            __syncthreads();
+            if (tid == 0) {
+                double s = 0.0;
+                for (int w = 0; w < VD_WARPS; ++w) s += sh.warp_sum[w];
+                sh.cta_sum[turn & 1] = s;
+            }
+            if (C > 1) vtk_cluster_sync(); else __syncthreads();
+            before = total = 0.0;
+            for (int c = 0; c < C; ++c) {
+                if (c == rank) before = total;
+                total += C > 1 ? vtk_cluster_read(&sh.cta_sum[turn & 1], c) : sh.cta_sum[turn & 1];
+            }
+            ++turn;
+            if (total > 0.0 || (row.q == nullptr && row.without < 0)) break;
+            row.q = nullptr;                                 // the draft's source has all that the target has
+            row.without = -1;
+        }
+        // the run with the drawn mass: the first whose cumulated mass exceeds it, else the last that has any
+        const float w0 = a.sample_random[r];
+        const double drawn = (w0 > 0.f ? (double)w0 : 0.0) * total;
+        int owner = -1, last = -1;
+        double upto = 0.0;
+        for (int c = 0; c < C; ++c) {
+            const double s = C > 1 ? vtk_cluster_read(&sh.cta_sum[(turn - 1) & 1], c) : sh.cta_sum[(turn - 1) & 1];
+            upto += s;
+            if (s > 0.0) last = c;
+            if (owner < 0 && upto > drawn) owner = c;
+        }
+        if (owner < 0) owner = last;
+        int token = -1;
+        if (owner == rank) {
+            int w_owner = -1, w_last = -1;
+            double w_before = 0.0;
+            upto = before;
+            for (int w = 0; w < VD_WARPS; ++w) {
+                const double s = sh.warp_sum[w];
+                if (s > 0.0) w_last = w;
+                if (w_owner < 0 && upto + s > drawn) w_owner = w;
+                upto += s;
+            }
+            if (w_owner < 0) w_owner = w_last;
+            w_before = before;
+            for (int w = 0; w < w_owner; ++w) w_before += sh.warp_sum[w];
+            if (warp == w_owner) {
+                int any = -1;                                // the last element with mass
+                for (int i0 = lo; i0 < hi && token < 0; i0 += STEP) {
+                    const int i = i0 + lane * VE;
+                    float x[VE], y[VE];
+                    row.get(i < hi ? i : a.vocab, x, y);
+                    double v[VE], sum = 0.0;
+                    int mine = -1;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        v[e] = i < hi ? row.value(i + e, x[e], y[e]) : 0.0;
+                        if (v[e] > 0.0) mine = i + e;
+                        sum += v[e];
+                    }
+                    const double incl = vtk_warp_incl_scan(sum);
+                    double c = w_before + (incl - sum);
+                    int found = -1;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        c += v[e];
+                        if (found < 0 && c > drawn && v[e] > 0.0) found = i + e;
+                    }
+                    const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
+                    if (who) token = __shfl_sync(0xffffffffu, found, __ffs(who) - 1);
+                    any = max(any, __reduce_max_sync(0xffffffffu, mine));
+                    w_before += __shfl_sync(0xffffffffu, incl, 31);
+                }
+                if (token < 0) token = any;
+                if (lane == 0) {
+                    a.next_tokens[r] = token;
+                    if (!a.out_tokens.null()) a.out_tokens[d.d0 + r + at] = token;
+                }
+            }
+        } else if (owner < 0 && rank == 0 && tid == 0) {
+            a.next_tokens[r] = -1;
+            if (!a.out_tokens.null()) a.out_tokens[d.d0 + r + at] = -1;
+        }
+        __syncthreads();                                     // the sums are the next request's
+    }
+    if (clipped) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
+    if (C > 1) vtk_cluster_sync();                           // (a neighbour may still be reading here)
+}
+
+template <typename P>
+int launch(vtoken_ctx *ctx, const VerifyArgs &a, bool vec, cudaStream_t st)
+{
+    int size = 1;
+    while (size < 8 && a.vocab > size * VD_NT * 8) size *= 2;
+    const int64_t most = (int64_t)ctx->num_sms * 8 / size;
+    const int rows = a.max_requests < most ? a.max_requests : (int)most, clusters = rows + (a.num_victims != nullptr ? 1 : 0);
+    VTK_CUDA(ctx, vec ? vtk_launch_clusters(ctx, verify_kernel<P, true>, size, dim3(clusters * size), dim3(VD_NT), 0, st, a, rows)
+                      : vtk_launch_clusters(ctx, verify_kernel<P, false>, size, dim3(clusters * size), dim3(VD_NT), 0, st, a, rows));
+    VTK_CUDA(ctx, cudaGetLastError());
+    return VTOKEN_OK;
+}
+
+}  // namespace
+
+extern "C" int vtoken_verify_drafts(vtoken_ctx *ctx, const vtoken_verify_in *in, void *cuda_stream)
+{
+    if (!ctx || !in || !in->num_requests || !in->target_probs || !in->sample_random || !in->accepted || !in->next_tokens) return VTOKEN_EINVAL;
+    if (in->max_drafts < 0 || in->vocab < 1 || in->vocab > (1 << 30)) return VTOKEN_EINVAL;
+    if (in->max_drafts > 0 && (!in->draft_offsets || !in->draft_tokens || !in->accept_random)) return VTOKEN_EINVAL;
+    if (in->prob_type != VTOKEN_PROB_BF16 && in->prob_type != VTOKEN_PROB_FP16 && in->prob_type != VTOKEN_PROB_F32) return VTOKEN_EINVAL;
+    const int64_t ts = in->target_stride ? in->target_stride : in->vocab, ds = in->draft_stride ? in->draft_stride : in->vocab;
+    if (ts < in->vocab || ds < in->vocab) return VTOKEN_EINVAL;
+    const int size = in->prob_type == VTOKEN_PROB_F32 ? 4 : 2;
+    if (((uintptr_t)in->target_probs | (uintptr_t)in->draft_probs) % size) return VTOKEN_EINVAL;
+    const bool victims = in->victim_req || in->victim_tok || in->num_victims;
+    if (in->max_victims < 0) return VTOKEN_EINVAL;
+    if (victims && (!in->num_victims || !in->first_id || (in->max_victims > 0 && (!in->victim_req || !in->victim_tok)))) return VTOKEN_EINVAL;
+    VerifyArgs a;
+    const int64_t D = in->max_drafts, Q = ctx->cfg.max_requests;
+    a.num_requests = in->num_requests;
+    a.draft_offsets = VTK_ARR(ctx, in->draft_offsets, Q + 1);
+    a.draft_tokens = VTK_ARR(ctx, in->draft_tokens, D);
+    a.first_id = VTK_ARR(ctx, in->first_id, Q);
+    a.target = in->target_probs;
+    a.draft = in->draft_probs;
+    a.target_stride = ts;
+    a.draft_stride = ds;
+    a.accept_random = VTK_ARR(ctx, in->accept_random, D);
+    a.sample_random = VTK_ARR(ctx, in->sample_random, Q);
+    a.accepted = VTK_ARR(ctx, in->accepted, Q);
+    a.next_tokens = VTK_ARR(ctx, in->next_tokens, Q);
+    a.out_tokens = VTK_ARR(ctx, in->out_tokens, D + Q);
+    a.victim_req = VTK_ARR(ctx, in->victim_req, in->max_victims);
+    a.victim_tok = VTK_ARR(ctx, in->victim_tok, in->max_victims);
+    a.num_victims = victims ? in->num_victims : nullptr;
+    a.vocab = in->vocab;
+    a.max_drafts = in->max_drafts;
+    a.max_requests = ctx->cfg.max_requests;
+    a.max_victims = in->max_victims;
+    a.flags = &ctx->rt_counts->error_flags;
+    // rows that start on 16 bytes are read 16 bytes at a time
+    const bool vec = (((uintptr_t)a.target | (uintptr_t)a.draft) & 15) == 0 && (ts * size) % 16 == 0 && (a.draft == nullptr || (ds * size) % 16 == 0);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    switch (in->prob_type) {
+        case VTOKEN_PROB_F32: return launch<F32>(ctx, a, vec, st);
+        case VTOKEN_PROB_BF16: return launch<Half<VtkBf16>>(ctx, a, vec, st);
+        default: return launch<Half<VtkFp16>>(ctx, a, vec, st);
+    }
+}

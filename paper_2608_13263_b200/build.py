@@ -24,8 +24,8 @@ CHECKED_LIB = os.path.join(PKG, "libvtoken_checked.so")
 
 LIB_SOURCES = ["api.cu", "plan.cu", "plan_small.cu", "copy.cu", "gather.cu", "gather_static.cu", "runtime.cu", "plan_partial.cu",
                "waves.cu", "slot_cache.cu", "check.cu", "tokens.cu", "attention.cu", "attention_prompt.cu",
-               "attention_shared.cu", "weights.cu", "victims.cu", "verify.cu"]
-HEADERS = ["common.cuh", "cluster.cuh", "heads.cuh", "attention.cuh", "weights.cuh"]
+               "attention_shared.cu", "weights.cu", "weights_prompt.cu", "victims.cu", "verify.cu"]
+HEADERS = ["common.cuh", "cluster.cuh", "heads.cuh", "attention.cuh", "tensor.cuh", "weights.cuh"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "--threads", "0",

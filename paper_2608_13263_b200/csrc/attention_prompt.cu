@@ -23,12 +23,13 @@
 // Every wait is bounded (wait_limit_ms): where one runs out, the roles leave their loops, the tensor memory is freed
 // and VTOKEN_FLAG_TIMEOUT is set.
 #include "attention.cuh"
+#include "tensor.cuh"
 
 namespace {
 
 constexpr int AP_REGS_SOFTMAX = 192, AP_REGS_LOAD = 80, AP_REGS_REST = 48;
 static_assert(2 * AP_REGS_SOFTMAX + AP_REGS_LOAD + AP_REGS_REST <= 4 * 128, "the registers that the block is launched with");
-constexpr int AP_NT = 512, AP_STAGES = 4, AP_TILE = 128, AP_META = 4;
+constexpr int AP_NT = 512, AP_STAGES = 4, AP_TILE = TC_TILE, AP_META = 4;
 constexpr uint64_t AP_DRAIN_NS = 1000000000;    // products in flight end by themselves: waited for whatever the caller's limit is
 
 struct Item {                            // what one CTA works on
@@ -71,110 +72,6 @@ struct Shared {
     int abort;
 };
 
-// ---- tcgen05 -------------------------------------------------------------------------------------
-// (these four are called by a whole warp, in uniform control flow, so that their operands can stay in uniform registers; `one`
-// picks the lane that issues)
-__device__ __forceinline__ bool tc_elect()
-{
-    uint32_t r;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
-    return r != 0;
-}
-__device__ __forceinline__ void tc_commit(bool one, uint64_t *bar)
-{
-    if (one) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void tc_mma_ss(bool one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
-{
-    if (one)
-        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void tc_mma_ts(bool one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
-{
-    if (one)
-        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-                     ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void tc_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// ... with the registers that the load wrote: nothing that reads them comes before the wait
-#define P8(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
-__device__ __forceinline__ void tc_wait_ld(uint32_t (&r)[32])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;" : P8(r, 0), P8(r, 8), P8(r, 16), P8(r, 24) : : "memory");
-}
-__device__ __forceinline__ void tc_wait_ld(uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;" : P8(r, 0), P8(r, 8) : : "memory");
-}
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float d;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-// two 32-bit operations an instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
-    return *reinterpret_cast<float2 *>(&d);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-    return *reinterpret_cast<float2 *>(&d);
-}
-__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-#define R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
-#define W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
-// 32 consecutive columns of the warp's 32 lanes: thread = lane, register = column
-__device__ __forceinline__ void tc_ld32(uint32_t addr, uint32_t (&r)[32])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
-                 "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-                 : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24) : "r"(addr));
-}
-__device__ __forceinline__ void tc_ld16(uint32_t addr, uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-                 : R8(r, 0), R8(r, 8) : "r"(addr));
-}
-__device__ __forceinline__ void tc_st16(uint32_t addr, const uint32_t (&r)[16])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-                 ::"r"(addr), W8(r, 0), W8(r, 8) : "memory");
-}
-
-// Shared-memory operand: 128-byte swizzle; 8-row (K-major) or 8-token (MN-major) groups 1024 bytes apart, 64-wide
-// panels a whole tile apart (used by the MN-major operand only).
-__device__ __forceinline__ uint64_t operand(uint32_t addr)
-{
-    return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)(AP_TILE * 128 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-
-// byte offset of 16-byte piece c (of D / 8) of row `row` in a tile of D / 64 panels
-__device__ __forceinline__ uint32_t swizzled(int row, int c)
-{
-    return (uint32_t)((c >> 3) * (AP_TILE * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4));
-}
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-// the barrier gets this thread's arrival when its copies so far have landed: nobody waits for them here
-__device__ __forceinline__ void cp_arrive(uint64_t *bar)
-{
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(vtk_smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-// Shared memory written by threads (cp.async too) is read by the tensor cores through another path: this fence stands between the two,
-// in the thread that issues the products, behind its wait for the tile (or in the threads that wrote, before they arrive).
-__device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // entries of the ascending ids [base, base + len) that are <= p, found by a warp: 32 probes a round
 __device__ inline int ids_up_to_warp(const VtkAttnArgs &a, int64_t base, int len, int64_t p)
 {
@@ -250,11 +147,6 @@ __device__ void next_item(const VtkAttnArgs &a, Shared<D> &sh, Item &out, int R,
         it.tiles = (it.span.n + AP_TILE - 1) / AP_TILE;
     }
     if (lane == 0) out = it;
-}
-
-__device__ __forceinline__ void st_shared16(uint32_t addr, uint4 w)
-{
-    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
 }
 
 template <int D, bool FP4, typename Act>

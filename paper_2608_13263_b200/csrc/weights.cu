@@ -378,7 +378,7 @@ extern "C" {
 int64_t vtoken_token_weights_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens)
 {
     if (!ctx || vtk_check_heads(ctx, heads, 0) != VTOKEN_OK || max_query_tokens < 0) return VTOKEN_EINVAL;
-    return 16;
+    return vtk_weights_prompt_workspace(ctx, heads);
 }
 
 int vtoken_token_weights(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_weights_in *in, void *cuda_stream)
@@ -429,11 +429,12 @@ int vtoken_token_weights(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t lay
     w.prev = VTK_ARR(ctx, in->decay == 0.f ? (const float *)nullptr : in->prev, ctx->cfg.max_tokens);
     w.scores = VTK_ARR(ctx, in->scores, ctx->cfg.max_tokens);
     w.decay = in->decay;
-    const bool prompts = false;
+    const bool prompts = (int64_t)in->max_query_len * a.group > TW_ROW_LIMIT;
     a.row_limit = prompts ? TW_ROW_LIMIT : INT32_MAX;
     const bool wide = (prompts ? 1 : (int64_t)in->max_query_len) * a.group > 8;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    return heads->head_dim == 128 ? launch_by_type<128>(ctx, heads, w, wide, st) : launch_by_type<64>(ctx, heads, w, wide, st);
+    const int rc = heads->head_dim == 128 ? launch_by_type<128>(ctx, heads, w, wide, st) : launch_by_type<64>(ctx, heads, w, wide, st);
+    return rc == VTOKEN_OK && prompts ? vtk_launch_weights_prompt(ctx, heads, w, in->workspace, st) : rc;
 }
 
 }  // extern "C"

@@ -1,0 +1,666 @@
+// Attention weight received by every cached token from many query rows per request (prompts and chunks of prompts), on the fifth
+// generation tensor cores.
+//
+// 2 D flops and one exponential a pair of query row and token.  The product is taken as S^T = K Q^T, tokens as the rows of the
+// accumulator: a thread then owns a token and the sum over query rows is a sum over its registers, where S = Q K^T would need one over
+// the lanes of a warp for every column.  256 x 128 pairs take 1024 cycles of the tensor pipe and 2048 of the 16 exponentials a
+// cycle: the exponentials are the bound.
+//
+// An item is (request, 256 tokens, key head, chunk of row tiles): its K rows stay in shared memory while the 128-row tiles of Q that
+// see any of them stream by.  Sums of an item go to the workspace; a second small kernel adds them up in the order of chunks and
+// heads and joins them with the scores before.  Roles, 24 warps:
+//   0 .. 15          thread = token: exponentials of a row of S^T, summed.  Two groups of 8 warps take the row tiles in turn, each
+//                    with an accumulator for the first and one for the second 128 tokens
+//   16 .. 19         copies of K rows (by slot, once an item) and Q rows into 128-byte-swizzled tiles; 4-bit keys expanded on the way
+//   20               one thread issues the products
+//   21               draws items; 22, 23 find the row tiles that see the item's tokens and lay out positions and logarithms
+// Each role goes from item to item on its own, handed on by barriers in shared memory.  Every wait is bounded (wait_limit_ms): where
+// one runs out all roles leave and VTOKEN_FLAG_TIMEOUT is set.
+#include "tensor.cuh"
+#include "weights.cuh"
+
+namespace {
+
+constexpr int WP_NT = 768, WP_SUMS = 16, WP_META = 4, WP_Q = 2, WP_PAIR = 2 * TC_TILE, WP_JOIN_NT = 256;
+constexpr int WP_READERS = WP_SUMS + 4 + 1;                      // warps that read a Meta
+constexpr uint64_t WP_DRAIN_NS = 1000000000;
+
+struct Args {
+    VtkWeightsArgs w;
+    uint32_t *tickets;                   // next item, CTAs that are done; zero between calls
+    float *parts;                        // sums of the items, WP_PAIR each
+    int64_t max_parts;
+    int32_t row_limit;                   // requests of at most so many rows belong to weights.cu
+    int32_t grid;                        // of the kernel that computes
+    uint64_t limit_ns;
+    int64_t stall;                       // (checked build) the item whose first rows never become complete
+};
+
+// a request in this kernel
+struct Spread {
+    int q0, len;
+    int64_t base, rows, pairs, tiles;    // pairs of token tiles; row tiles
+};
+
+__device__ inline Spread spread_of(const Args &w, int r, bool &clipped)
+{
+    const VtkAttnArgs &a = w.w.at;
+    Spread s;
+    int qn;
+    bool c;
+    vtk_request_rows(a, r, s.q0, qn, s.base, s.len, c);
+    clipped |= c;
+    s.rows = (int64_t)qn * a.group;
+    s.pairs = s.rows > w.row_limit ? ((int64_t)s.len + WP_PAIR - 1) / WP_PAIR : 0;
+    s.tiles = (s.rows + TC_TILE - 1) / TC_TILE;
+    return s;
+}
+__device__ __forceinline__ int64_t chunks_of(const Spread &s, int64_t chunk) { return (s.tiles + chunk - 1) / chunk; }
+
+// The cut, the same in every CTA of both kernels: row tiles of a chunk, pairs and items in front of each thread's requests.
+template <int NT>
+struct Cut {
+    int64_t pairs[NT + 1], items[NT + 1], warp_sum[2][NT / 32];
+    int64_t chunk;
+    int R, seg;
+    template <typename F>
+    __device__ void scan(const Args &w, F f, bool &clipped)  // f: request -> (pairs, items)
+    {
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        int64_t p = 0, n = 0;
+        for (int64_t r = (int64_t)tid * seg; r < (int64_t)(tid + 1) * seg && r < R; ++r) {
+            const Spread s = spread_of(w, (int)r, clipped);
+            p += s.pairs;
+            n += f(s);
+        }
+        const int64_t ip = vtk_warp_incl_scan(p), in = vtk_warp_incl_scan(n);
+        if (lane == 31) { warp_sum[0][warp] = ip; warp_sum[1][warp] = in; }
+        __syncthreads();
+        int64_t bp = 0, bn = 0;
+        for (int v = 0; v < warp; ++v) { bp += warp_sum[0][v]; bn += warp_sum[1][v]; }
+        pairs[tid + 1] = bp + ip;
+        items[tid + 1] = bn + in;
+        if (tid == 0) pairs[0] = items[0] = 0;
+        __syncthreads();
+    }
+    __device__ void make(const Args &w, bool &clipped)
+    {
+        const VtkAttnArgs &a = w.w.at;
+        int n = *a.num_requests;
+        clipped |= n < 0 || n > a.max_requests;
+        n = n < 0 ? 0 : (n > a.max_requests ? a.max_requests : n);
+        if (threadIdx.x == 0) { R = n; seg = (n + NT - 1) / NT; }
+        __syncthreads();
+        scan(w, [&](const Spread &s) { return s.pairs * s.tiles * a.hkv; }, clipped);
+        // about six items a CTA, of 4 to 64 row tiles, as many as the workspace has room for
+        int64_t c = items[NT] / ((int64_t)w.grid * 6);
+        c = c < 4 ? 4 : (c > 64 ? 64 : c);
+        for (;; c *= 2) {
+            bool again = false;
+            scan(w, [&](const Spread &s) { return s.pairs * chunks_of(s, c) * a.hkv; }, again);
+            if (items[NT] <= w.max_parts || c >= (1ll << 40)) break;
+        }
+        if (threadIdx.x == 0) chunk = c;                     // (a number of row tiles: far below 2^32)
+        __syncthreads();
+    }
+    // the request of pair (or item) `i`, and what is left of i there
+    __device__ int find(const Args &w, const int64_t (&prefix)[NT + 1], bool by_items, int64_t &i, int64_t &items_before, Spread &s) const
+    {
+        int lo = 0, hi = NT;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (prefix[mid] <= i) lo = mid; else hi = mid;
+        }
+        i -= prefix[lo];
+        items_before = items[lo];
+        for (int r = lo * seg;; ++r) {
+            bool c = false;
+            s = spread_of(w, r, c);
+            const int64_t n = s.pairs * chunks_of(s, chunk) * w.w.at.hkv, here = by_items ? n : s.pairs;
+            if (i < here) return r;
+            i -= here;
+            items_before += n;
+        }
+    }
+};
+
+struct Item {
+    int none, kv, q0, rows, first, n;    // query rows of the request; first cache entry and number of tokens
+    int tile0, tile1;                    // row tiles
+    int64_t base, ticket;
+};
+
+struct Meta {                            // a tile of query rows
+    int tile, pmin, pmax;                // tile -1: the item's end
+    int all[2];                          // of each half: every row is there and saw something
+    alignas(16) float lse2[TC_TILE];     // minus the logarithm to base 2
+    alignas(16) int pos[TC_TILE];        // -2^31: the row adds nothing
+    alignas(16) float scale[TC_TILE];    // bf16 queries over 4-bit keys: factor of the row's scores
+};
+
+// The sum over a tile's query rows of what token `id` gets from them: 128 columns of the thread's accumulator row.  Two copies, as a
+// branch at every mask would keep the compiler from overlapping the chains of loads, products and exponentials (6500 cycles a tile
+// instead of 3700).
+template <bool SCALED, bool MASKED>
+__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id)
+{
+    const float c = a.scale_log2;
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    uint32_t v[2][16];
+    tc_ld16(src, v[0]);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        uint32_t(&now)[16] = v[q & 1];
+        tc_wait_ld(now);
+        if (q < 7) tc_ld16(src + 16 * (q + 1), v[(q + 1) & 1]);
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const float4 l = *reinterpret_cast<const float4 *>(&m.lse2[16 * q + i]);
+            float4 f = make_float4(c, c, c, c);
+            if (SCALED) {
+                f = *reinterpret_cast<const float4 *>(&m.scale[16 * q + i]);
+                f.x *= c; f.y *= c; f.z *= c; f.w *= c;
+            }
+            float2 y0 = fma2(make_float2(__uint_as_float(now[i]), __uint_as_float(now[i + 1])), make_float2(f.x, f.y), make_float2(l.x, l.y));
+            float2 y1 = fma2(make_float2(__uint_as_float(now[i + 2]), __uint_as_float(now[i + 3])), make_float2(f.z, f.w), make_float2(l.z, l.w));
+            y0.x = vtk_exp2(y0.x); y0.y = vtk_exp2(y0.y);
+            y1.x = vtk_exp2(y1.x); y1.y = vtk_exp2(y1.y);
+            if (MASKED) {
+                const int4 p = *reinterpret_cast<const int4 *>(&m.pos[16 * q + i]);
+                y0.x = vtk_sees(id, p.x, vtk_floor(p.x, a.window), a.sinks) ? y0.x : 0.f;
+                y0.y = vtk_sees(id, p.y, vtk_floor(p.y, a.window), a.sinks) ? y0.y : 0.f;
+                y1.x = vtk_sees(id, p.z, vtk_floor(p.z, a.window), a.sinks) ? y1.x : 0.f;
+                y1.y = vtk_sees(id, p.w, vtk_floor(p.w, a.window), a.sinks) ? y1.y : 0.f;
+            }
+            sum[0] = add2(sum[0], y0);
+            sum[1] = add2(sum[1], y1);
+        }
+    }
+    sum[0] = add2(sum[0], sum[1]);
+    return sum[0].x + sum[0].y;
+}
+
+template <int D>
+struct Shared {
+    uint8_t k[2][2][D / 64][TC_TILE * 128];
+    uint8_t q[WP_Q][D / 64][TC_TILE * 128];
+    Meta meta[WP_META];
+    Item item[2];
+    float other[2][WP_PAIR];             // the second group's sums of an item
+    Cut<WP_NT> cut;
+    uint64_t item_full[2], item_empty[2], meta_full[WP_META], meta_empty[WP_META], scale_full[WP_META], k_full[2], k_empty[2], other_full[2];
+    uint64_t q_full[WP_Q], q_empty[WP_Q], s_full[2][2], s_empty[2][2], drain;
+    uint32_t tmem;
+    int abort;
+};
+
+template <int D, bool FP4, typename Act>
+__global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_constant__ Args w)
+{
+    using Mma = typename std::conditional<FP4, VtkFp16, Act>::type;
+    constexpr int PIECES = D / 8, PANEL = TC_TILE * 128;
+    constexpr bool SCALED = FP4 && Act::kind == VTOKEN_KV_BF16;
+    const VtkAttnArgs &a = w.w.at;
+    extern __shared__ uint8_t raw[];
+    Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw + ((1024 - (vtk_smem_u32(raw) & 1023)) & 1023));
+    vtk_release_successor();
+    vtk_wait_for_predecessor();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            vtk_mbar_init(&sh.item_full[i], 1); vtk_mbar_init(&sh.item_empty[i], WP_READERS + 2);
+            vtk_mbar_init(&sh.k_full[i], 128); vtk_mbar_init(&sh.k_empty[i], 1); vtk_mbar_init(&sh.other_full[i], 8);
+            for (int b = 0; b < 2; ++b) { vtk_mbar_init(&sh.s_full[i][b], 1); vtk_mbar_init(&sh.s_empty[i][b], 4); }
+        }
+        for (int i = 0; i < WP_META; ++i) { vtk_mbar_init(&sh.meta_full[i], 2); vtk_mbar_init(&sh.meta_empty[i], WP_READERS); vtk_mbar_init(&sh.scale_full[i], 128); }
+        for (int i = 0; i < WP_Q; ++i) { vtk_mbar_init(&sh.q_full[i], 128); vtk_mbar_init(&sh.q_empty[i], 1); }
+        vtk_mbar_init(&sh.drain, 1);
+        sh.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == WP_SUMS + 4) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(vtk_smem_u32(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    bool clipped = false;
+    sh.cut.make(w, clipped);
+    if (blockIdx.x == 0 && (clipped || (tid == 0 && sh.cut.items[WP_NT] > w.max_parts))) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = sh.tmem;
+    constexpr uint32_t IDESC = (1u << 4) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 7) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 10) |
+                               ((uint32_t)(TC_TILE >> 4) << 24) | ((uint32_t)(TC_TILE >> 3) << 17);
+    auto wait_phase = [&](uint64_t *bar, uint32_t parity, uint64_t limit) {
+        return (bool)__all_sync(0xffffffffu, vtk_mbar_wait(bar, parity, limit, &sh.abort, 1));
+    };
+    auto wait = [&](uint64_t *bar, uint32_t count, uint32_t ring) { return wait_phase(bar, (count / ring) & 1, w.limit_ns); };     // the count-th phase of a ring's barrier
+    auto wait_empty = [&](uint64_t *bar, uint32_t count, uint32_t ring) { return wait_phase(bar, ((count / ring) & 1) ^ 1, w.limit_ns); };
+    auto arrive = [&](uint64_t *bar) {
+        __syncwarp();
+        if (lane == 0) vtk_mbar_arrive(bar);
+    };
+
+    // Every role runs over the items and, within one, over the row tiles that see something of it.
+    uint32_t n_item = 0, n_meta = 0;
+    auto each_item = [&](auto &&body) {
+        for (;; ++n_item) {
+            const int s = n_item & 1;
+            if (!wait(&sh.item_full[s], n_item, 2)) return;
+            const Item it = sh.item[s];
+            if (it.none || !body(it)) return;
+            arrive(&sh.item_empty[s]);
+        }
+    };
+    auto each_tile = [&](auto &&body) {                      // false: given up
+        for (;;) {
+            const int s = n_meta % WP_META;
+            if (!wait(&sh.meta_full[s], n_meta, WP_META)) return false;
+            const bool end = sh.meta[s].tile < 0;
+            if (!end && !body(sh.meta[s])) return false;
+            arrive(&sh.meta_empty[s]);
+            ++n_meta;
+            if (end) return true;
+        }
+    };
+
+    if (warp < WP_SUMS) {
+        // ================= exponentials: thread = token =================
+        const int group = warp >> 3, x = (warp >> 2) & 1, row = tid & 127;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;                       // 32 lanes a warp
+        uint32_t n_mine = 0, n_q = 0;
+        bool bad_slot = false;
+        each_item([&](const Item &it) {
+            const int at = x * TC_TILE + row;
+            int id = INT32_MAX;
+            bool there = false;
+            if (at < it.n) {
+                const int64_t e = it.base + it.first + at, slot = a.cache_slots[e];
+                there = slot >= 0 && slot < a.slots_per_layer;
+                bad_slot |= slot >= a.slots_per_layer;
+                if (there) id = a.cache_ids.null() ? it.first + at : a.cache_ids[e];
+            }
+            const bool every = __all_sync(0xffffffffu, there);
+            const int id_lo = __reduce_min_sync(0xffffffffu, id), id_hi = __reduce_max_sync(0xffffffffu, there ? id : -1);
+            const bool mine = x * TC_TILE < it.n;                                // (uniform)
+            float total = 0.f;
+            const bool ok = each_tile([&](const Meta &m) {
+                const uint32_t turn = n_q++;
+                if (!mine || (int)(turn & 1) != group) return true;
+                if (!wait(&sh.s_full[x][group], n_mine, 1)) return false;
+                if (SCALED && !wait(&sh.scale_full[turn % WP_META], turn, WP_META)) return false;
+                tc_after_sync();
+                const uint32_t src = tmem + lanes + (x * 2 + group) * TC_TILE;
+                const bool some = m.pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(m.pmin, a.window) || id_lo < a.sinks);
+                const bool full = every && m.all[0] && m.all[1] && id_hi <= m.pmin && (id_lo > vtk_floor(m.pmax, a.window) || id_hi < a.sinks);
+                if (some) total += full ? row_sum<SCALED, false>(a, m, src, id) : row_sum<SCALED, true>(a, m, src, id);
+                tc_before_sync();
+                arrive(&sh.s_empty[x][group]);
+                ++n_mine;
+                return true;
+            });
+            if (!ok) return false;
+            const int turn = n_item & 1;
+            if (group == 1) {
+                sh.other[turn][at] = total;
+                arrive(&sh.other_full[turn]);
+            } else {
+                if (!wait(&sh.other_full[turn], n_item, 2)) return false;
+                if (mine) w.parts[it.ticket * WP_PAIR + at] = total + sh.other[turn][at];
+            }
+            return true;
+        });
+        if (bad_slot) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
+    } else if (warp < WP_SUMS + 4) {
+        // ================= copies =================
+        const int pt = tid - WP_SUMS * 32;
+        uint32_t n_k = 0, n_q = 0;
+        auto stalled = [&](const Item &it) {
+#ifdef VTOKEN_CHECKED
+            return it.ticket == w.stall;
+#else
+            return false;
+#endif
+        };
+        auto keys = [&](const Item &it) {
+            const int kb = n_k & 1;
+            if (!wait_empty(&sh.k_empty[kb], n_k, 2)) return false;
+            auto slot_of = [&](int at) {
+                const int64_t slot = at < it.n ? a.cache_slots[it.base + it.first + at] : -1;
+                return slot < a.slots_per_layer ? (int)slot : -1;
+            };
+            for (int x = 0; x < (it.n > TC_TILE ? 2 : 1); ++x) {
+                const uint32_t dst = vtk_smem_u32(sh.k[kb][x]);
+                if (!FP4) {
+                    constexpr int ROWS = PIECES;             // PIECES threads a row, each with the same number of consecutive rows
+                    const int piece = pt % PIECES, row0 = pt / PIECES * ROWS;
+                    const uint8_t *base = a.k_rows + ((int64_t)it.kv * D + 8 * piece) * 2;
+                    const int mine = slot_of(x * TC_TILE + pt);                  // (a warp's threads have 32 rows)
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) {
+                        const int slot = __shfl_sync(0xffffffffu, mine, lane / PIECES * ROWS + i);
+                        cp_async16(dst + swizzled(row0 + i, piece), base + (int64_t)(slot < 0 ? 0 : slot) * a.row_bytes, slot >= 0);
+                    }
+                } else {
+                    constexpr int QW = D / 32;               // four threads a token, a quarter of its codes and scales each
+                    const int part = pt & 3;
+                    uint32_t code[4][QW], sc[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t slot = slot_of(x * TC_TILE + (pt >> 2) + 32 * i);
+#pragma unroll
+                        for (int k = 0; k < QW; ++k) code[i][k] = 0;
+                        sc[i] = 0;
+                        if (slot < 0) continue;
+                        const uint8_t *src = a.k_rows + slot * a.row_bytes, *codes = src + it.kv * (D / 2) + part * (D / 8);
+                        const uint8_t *scales = src + a.hkv * (D / 2) + it.kv * (D / 16) + part * (D / 64);
+                        if (D == 128) {
+                            const uint4 q4 = vtk_ldg16(codes);
+                            code[i][0] = q4.x; code[i][1] = q4.y; code[i][QW - 2] = q4.z; code[i][QW - 1] = q4.w;
+                            sc[i] = __ldg(reinterpret_cast<const uint16_t *>(scales));
+                        } else {
+                            const uint2 q2 = __ldg(reinterpret_cast<const uint2 *>(codes));
+                            code[i][0] = q2.x; code[i][1] = q2.y;
+                            sc[i] = __ldg(scales);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t two_scales = vtk_scales_to_half2(sc[i]);
+#pragma unroll
+                        for (int k = 0; k < QW; ++k)
+                            st_shared16(dst + swizzled((pt >> 2) + 32 * i, part * QW + k), vtk_expand8(code[i][k], __byte_perm(two_scales, 0, k < 2 ? 0x1010 : 0x3232)));
+                    }
+                }
+            }
+            if (!FP4) {
+                cp_arrive(&sh.k_full[kb]);
+            } else {
+                async_proxy_fence();
+                vtk_mbar_arrive(&sh.k_full[kb]);
+            }
+            ++n_k;
+            return true;
+        };
+        each_item([&](const Item &it) {
+            bool first = true;
+            return each_tile([&](Meta &m) {
+                if (first && !keys(it)) return false;
+                const int stage = n_q % WP_Q;
+                if (!wait_empty(&sh.q_empty[stage], n_q, WP_Q)) return false;
+                const uint32_t dst = vtk_smem_u32(sh.q[stage]);
+                if (!FP4) {
+                    constexpr int ROWS = PIECES;             // (as the keys: each thread looks up one of its warp's 32 rows)
+                    const int piece = pt % PIECES, row0 = pt / PIECES * ROWS, at = m.tile * TC_TILE + pt;
+                    int64_t mine = -1;                       // where the row starts
+                    if (at < it.rows) mine = (int64_t)(it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
+#pragma unroll
+                    for (int i = 0; i < ROWS; ++i) {
+                        const int64_t row = __shfl_sync(0xffffffffu, mine, lane / PIECES * ROWS + i);
+                        cp_async16(dst + swizzled(row0 + i, piece), a.q + (row < 0 ? 0 : row) + 8 * piece, row >= 0);
+                    }
+                    if (!(first && stalled(it)) || pt > 0) cp_arrive(&sh.q_full[stage]);
+                } else {
+                    const int at = m.tile * TC_TILE + pt;
+                    const bool there = at < it.rows;
+                    const uint16_t *src = a.q;
+                    if (there) src += (int64_t)(it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
+                    float up = 1.f;
+                    if (SCALED) {                            // bf16 queries in half precision: see attention.cu
+                        float top = 0.f, v[8];
+                        for (int i = 0; i < PIECES; ++i) {
+                            vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0), v);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+                        }
+                        int e2 = (int)(__float_as_uint(top) >> 23) - 127;
+                        e2 = 14 - (e2 < -100 ? -100 : e2);
+                        up = __uint_as_float((uint32_t)(127 + e2) << 23);
+                        m.scale[pt] = __uint_as_float((uint32_t)(127 - e2) << 23);
+                        vtk_mbar_arrive(&sh.scale_full[n_q % WP_META]);      // (of the rows that see something: fewer than entries)
+                    }
+                    for (int i = 0; i < PIECES; ++i) {
+                        uint4 word = there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+                        if (SCALED) {
+                            float v[8];
+                            vtk_unpack8<VtkBf16>(word, v);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] *= up;
+                            word = vtk_pack8<VtkFp16>(v);
+                        }
+                        st_shared16(dst + swizzled(pt, i), word);
+                    }
+                    async_proxy_fence();
+                    if (!(first && stalled(it)) || pt > 0) vtk_mbar_arrive(&sh.q_full[stage]);
+                }
+                first = false;
+                ++n_q;
+                return true;
+            });
+        });
+        if (!FP4) cp_wait_all();
+    } else if (warp == WP_SUMS + 4) {
+        // ================= products =================
+        const bool one = tc_elect();
+        uint32_t n_k = 0, n_q = 0, n_acc[2][2] = {{0, 0}, {0, 0}};
+        each_item([&](const Item &it) {
+            bool first = true;
+            const bool two = it.n > TC_TILE;
+            const int kb = n_k & 1;
+            const bool ok = each_tile([&](const Meta &) {
+                if (first && !wait(&sh.k_full[kb], n_k, 2)) return false;
+                first = false;
+                const int stage = n_q % WP_Q;
+                if (!wait(&sh.q_full[stage], n_q, WP_Q)) return false;
+                async_proxy_fence();
+                const int b = n_q & 1;
+                for (int x = 0; x < (two ? 2 : 1); ++x) {
+                    if (!wait_empty(&sh.s_empty[x][b], n_acc[x][b], 1)) return false;
+                    tc_after_sync();
+                    const uint64_t kd = operand(vtk_smem_u32(sh.k[kb][x])), qd = operand(vtk_smem_u32(sh.q[stage]));
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = ((k / 4) * PANEL + (k % 4) * 32) >> 4;
+                        tc_mma_ss(one, tmem + (x * 2 + b) * TC_TILE, kd + off, qd + off, IDESC, k > 0);
+                    }
+                    tc_commit(one, &sh.s_full[x][b]);
+                    ++n_acc[x][b];
+                }
+                tc_commit(one, &sh.q_empty[stage]);
+                ++n_q;
+                return true;
+            });
+            if (!first) {
+                tc_commit(one, &sh.k_empty[kb]);
+                ++n_k;
+            }
+            return ok;
+        });
+        // what was issued ends before the tensor memory goes
+        tc_commit(one, &sh.drain);
+        const uint64_t t0 = vtk_global_ns();
+        while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < WP_DRAIN_NS) {}
+        __syncwarp();
+    } else if (warp == WP_SUMS + 5) {
+        // ================= items =================
+        for (;; ++n_item) {
+            const int s = n_item & 1;
+            // (an item's roles wait once a tile, and each of those waits has the limit)
+            if (!wait_phase(&sh.item_empty[s], ((n_item / 2) & 1) ^ 1, w.limit_ns * (uint64_t)(sh.cut.chunk + 2))) break;
+            int64_t idx = 0;
+            if (lane == 0) idx = (int64_t)atomicAdd(w.tickets, 1u);
+            idx = __shfl_sync(0xffffffffu, idx, 0);
+            Item it;
+            it.none = 1;
+            it.ticket = idx;
+            if (idx < sh.cut.items[WP_NT] && idx < w.max_parts) {
+                Spread sp;
+                int64_t left = idx, before;
+                sh.cut.find(w, sh.cut.items, true, left, before, sp);
+                const int64_t chunks = chunks_of(sp, sh.cut.chunk);
+                it.none = 0;
+                it.kv = (int)(left % a.hkv);
+                left /= a.hkv;
+                const int64_t c = left % chunks, pair = left / chunks;
+                it.tile0 = (int)(c * sh.cut.chunk);
+                it.tile1 = (int)((c + 1) * sh.cut.chunk < sp.tiles ? (c + 1) * sh.cut.chunk : sp.tiles);
+                it.q0 = sp.q0;
+                it.rows = (int)sp.rows;
+                it.first = (int)(pair * WP_PAIR);
+                it.n = sp.len - it.first < WP_PAIR ? sp.len - it.first : WP_PAIR;
+                it.base = sp.base;
+            }
+            if (lane == 0) sh.item[s] = it;
+            arrive(&sh.item_full[s]);
+            if (it.none) break;
+        }
+    } else {
+        // ================= row tiles: which ones see something, positions and logarithms =================
+        const int half = warp - (WP_SUMS + 6);
+        each_item([&](const Item &it) {
+            const int id_lo = a.cache_ids.null() ? it.first : a.cache_ids[it.base + it.first];
+            const int id_hi = a.cache_ids.null() ? it.first + it.n - 1 : a.cache_ids[it.base + it.first + it.n - 1];
+            auto put = [&](int tile, int pmin, int pmax) {
+                float l[2] = {-INFINITY, -INFINITY};
+                int p[2] = {INT32_MIN, INT32_MIN};
+                bool all = true;
+                if (tile >= 0) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int at = tile * TC_TILE + 64 * half + 32 * i + lane;
+                        if (at < it.rows) {
+                            const int64_t tok = it.q0 + at / a.group;
+                            l[i] = w.w.lse_in[tok * a.hq + it.kv * a.group + at % a.group];
+                            p[i] = a.positions[tok];
+                        }
+                        all &= l[i] != -INFINITY;
+                    }
+                    all = __all_sync(0xffffffffu, all);
+                }
+                const int s = n_meta % WP_META;
+                if (!wait_empty(&sh.meta_empty[s], n_meta, WP_META)) return false;
+                Meta &m = sh.meta[s];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int row = 64 * half + 32 * i + lane;
+                    m.lse2[row] = l[i] * -1.4426950408889634f;
+                    m.pos[row] = l[i] == -INFINITY ? INT32_MIN : (p[i] < INT32_MAX - 1 ? p[i] : INT32_MAX - 1);      // (INT32_MAX: what is not there)
+                }
+                if (lane == 0) {
+                    m.all[half] = all;
+                    if (half == 0) {
+                        m.tile = tile;
+                        m.pmin = pmin;
+                        m.pmax = pmax;
+                    }
+                }
+                arrive(&sh.meta_full[s]);
+                ++n_meta;
+                return true;
+            };
+            for (int t0 = it.tile0; t0 < it.tile1; t0 += 32) {
+                int pmin = INT32_MAX, pmax = INT32_MIN;
+                if (t0 + lane < it.tile1) {
+                    const int first = (t0 + lane) * TC_TILE, last = first + TC_TILE < it.rows ? first + TC_TILE - 1 : it.rows - 1;
+#pragma unroll 4
+                    for (int t = first / a.group; t <= last / a.group; ++t) {
+                        const int p = a.positions[it.q0 + t];
+                        pmin = p < pmin ? p : pmin;
+                        pmax = p > pmax ? p : pmax;
+                    }
+                }
+                const bool sees = t0 + lane < it.tile1 && pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(pmin, a.window) || id_lo < a.sinks);
+                unsigned mask = __ballot_sync(0xffffffffu, sees);
+                while (mask) {
+                    const int src = __ffs(mask) - 1;
+                    mask &= mask - 1;
+                    if (!put(t0 + src, __shfl_sync(0xffffffffu, pmin, src), __shfl_sync(0xffffffffu, pmax, src))) return false;
+                }
+            }
+            return put(-1, 0, 0);
+        });
+    }
+    __syncthreads();
+    if (tid == 0) {
+        if (sh.abort) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_TIMEOUT);
+        __threadfence();
+        if (atomicAdd(w.tickets + 1, 1u) == gridDim.x - 1) { w.tickets[0] = 0; w.tickets[1] = 0; }
+    }
+    if (warp == WP_SUMS + 4) {
+        tc_after_sync();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    }
+}
+
+// sums of chunks and heads, in their order, and the scores before
+__global__ void __launch_bounds__(WP_JOIN_NT) weights_join_kernel(const __grid_constant__ Args w)
+{
+    static_assert(WP_JOIN_NT == WP_PAIR, "thread = token");
+    const VtkAttnArgs &a = w.w.at;
+    __shared__ Cut<WP_JOIN_NT> cut;
+    vtk_release_successor();
+    vtk_wait_for_predecessor();
+    bool clipped = false, bad_id = false;
+    cut.make(w, clipped);
+    for (int64_t p = blockIdx.x; p < cut.pairs[WP_JOIN_NT]; p += gridDim.x) {
+        Spread s;
+        int64_t pair = p, before;
+        const int r = cut.find(w, cut.pairs, false, pair, before, s);
+        const int64_t at = pair * WP_PAIR + threadIdx.x;
+        if (at >= s.len) continue;
+        const int id = a.cache_ids.null() ? (int)at : a.cache_ids[s.base + at];
+        const int64_t t1 = a.tt_offsets[r + 1], end = t1 > a.max_tokens ? a.max_tokens : t1;
+        if (id < 0 || id >= end - s.base) { bad_id = true; continue; }
+        const int64_t n = chunks_of(s, cut.chunk) * a.hkv, first = before + pair * n;
+        float y = 0.f;
+        for (int64_t i = first; i < first + n && i < w.max_parts; ++i) y += __ldcg(w.parts + i * WP_PAIR + threadIdx.x);
+        if (!w.w.prev.null()) y = fmaf(w.w.decay, w.w.prev[s.base + id], y);
+        w.w.scores[s.base + id] = y;
+    }
+    if (bad_id) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_VICTIM);
+}
+
+// what the items of a call can be: one chunk of row tiles everywhere, and some more chunks where there are few
+int64_t parts_of(const vtoken_ctx *ctx, const vtoken_heads *heads)
+{
+    return ((ctx->cfg.max_tokens + WP_PAIR - 1) / WP_PAIR + ctx->cfg.max_requests) * heads->num_kv_heads + (int64_t)ctx->num_sms * 12;
+}
+
+template <int D, bool FP4, typename Act>
+int launch(vtoken_ctx *ctx, const Args &w, cudaStream_t st)
+{
+    constexpr int smem = (int)sizeof(Shared<D>) + 1024;
+    static_assert(smem <= 232448, "shared memory of a CTA");
+    auto kernel = weights_prompt_kernel<D, FP4, Act>;
+    static std::atomic<int> allowed{-1};                     // the device that knows of this kernel's shared memory
+    VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed, (const void *)kernel, smem));
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(w.grid), dim3(WP_NT), smem, st, w));
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, weights_join_kernel, dim3(ctx->num_sms * 2), dim3(WP_JOIN_NT), 0, st, w));
+    VTK_CUDA(ctx, cudaGetLastError());
+    return VTOKEN_OK;
+}
+
+template <int D>
+int launch_by_type(vtoken_ctx *ctx, const vtoken_heads *h, const Args &w, cudaStream_t st)
+{
+    if (h->kv_type == VTOKEN_KV_FP4) return h->act_type == VTOKEN_KV_BF16 ? launch<D, true, VtkBf16>(ctx, w, st) : launch<D, true, VtkFp16>(ctx, w, st);
+    return h->act_type == VTOKEN_KV_BF16 ? launch<D, false, VtkBf16>(ctx, w, st) : launch<D, false, VtkFp16>(ctx, w, st);
+}
+
+}  // namespace
+
+int64_t vtk_weights_prompt_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads) { return 16 + parts_of(ctx, heads) * WP_PAIR * 4; }
+
+int vtk_launch_weights_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkWeightsArgs &weights, void *workspace, cudaStream_t st)
+{
+    Args w;
+    w.w = weights;
+    w.tickets = (uint32_t *)workspace;
+    w.parts = (float *)((uint8_t *)workspace + 16);
+    w.max_parts = parts_of(ctx, heads);
+    w.row_limit = weights.at.row_limit;
+    w.grid = ctx->num_sms;
+    w.limit_ns = (uint64_t)ctx->wait_limit_ns;
+    w.stall = ctx->stall_item;
+    return heads->head_dim == 128 ? launch_by_type<128>(ctx, heads, w, st) : launch_by_type<64>(ctx, heads, w, st);
+}

@@ -39,7 +39,6 @@
 
 namespace {
 
-constexpr int AT_ROW_LIMIT = 32;         // query rows (tokens times group) of a request up to which it is worked on here
 constexpr int AT_KNOWN = 8;              // requests of a share that are looked up together at the start
 constexpr int AT_MIN_SHARE = 2;          // tiles of the smallest share, for each warp of its team
 constexpr int AT_PARTS = 3;              // shares that a segment of mean length is cut into at most, about
@@ -196,10 +195,11 @@ __device__ __forceinline__ float weight(float m, float top) { return m == -INFIN
 // one request as the cut sees it
 struct Known {
     int q0, qn, len, tiles, row_tiles;
+    int parts;                           // of the shared prefix in front: where the running maximum and sums go on from
     VtkRequest s;
 };
 
-template <int NR, int TILE>
+template <int NR, int TILE, bool SHARED>
 __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
 {
     Known k;
@@ -207,7 +207,8 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
     vtk_request_rows(a, r, k.q0, k.qn, k.s.base, k.len, c);
     clipped |= c;
     if (k.qn * (int64_t)a.group > a.row_limit) k.qn = 0;
-    k.s.lo = k.s.n_sink = 0;
+    k.parts = 0;
+    k.s.lo = k.s.n_sink = k.s.first = 0;
     k.s.n = k.len;
     k.s.pmax = k.s.floor = -1;
     k.row_tiles = (k.qn * a.group + NR - 1) / NR;
@@ -221,13 +222,20 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
             pmax = p > pmax ? p : pmax;
         }
         k.s = vtk_request_span(a, k.s.base, k.len, last, pmin, pmax);
+        if (SHARED) {
+            const int2 prefix = a.shared[r];
+            if (prefix.x > 0) {
+                k.parts = prefix.y;
+                k.s.behind(prefix.x);
+            }
+        }
     }
     k.tiles = k.qn > 0 ? (k.s.n > 0 ? (k.s.n + TILE - 1) / TILE : 1) : 0;
     return k;
 }
 
 // A walk over the segments of a share; the request it is at is kept in the warp's shared memory.
-template <int NR, int TILE>
+template <int NR, int TILE, bool SHARED>
 struct Walk {
     Known *k;
     int r, rt, hg, t0, t1;               // segment (hg: group of key heads) and its tiles [t0, t1) inside the share
@@ -248,7 +256,7 @@ struct Walk {
                 int tiles;
                 do {
                     ++r;
-                    const Known n = in_window(r, r_known) ? known[r - r_known] : look_up<NR, TILE>(a, r, c);
+                    const Known n = in_window(r, r_known) ? known[r - r_known] : look_up<NR, TILE, SHARED>(a, r, c);
                     tiles = n.tiles;
                     __syncwarp();
                     if (vtk_lane() == 0) *k = n;
@@ -260,8 +268,8 @@ struct Walk {
     }
 };
 
-// NR: query rows of a segment (8 or 16); SPLIT_P: P as a sum of two 16-bit values
-template <int D, int NR, typename Rows, typename Act, bool SPLIT_P>
+// NR: query rows of a segment (8 or 16); SPLIT_P: P as a sum of two 16-bit values; SHARED: requests may go on from a shared prefix
+template <int D, int NR, typename Rows, typename Act, bool SPLIT_P, bool SHARED>
 __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(const __grid_constant__ VtkAttnArgs a)
 {
     using Mma = typename Rows::Mma;
@@ -283,7 +291,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     int my_segments = 0;
     Known own;                                               // the thread's last request: its only one below 257 requests
     for (int r = tid * seg; r < (tid + 1) * seg && r < R; ++r) {
-        own = look_up<NR, TILE>(a, r, clipped);
+        own = look_up<NR, TILE, SHARED>(a, r, clipped);
         mine += (int64_t)own.tiles * own.row_tiles;
         my_segments += own.tiles > 0 ? own.row_tiles : 0;
     }
@@ -335,7 +343,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         }
     }
     __syncthreads();
-    Walk<NR, TILE> use;
+    Walk<NR, TILE, SHARED> use;
     use.f = share < G ? start_of(share) : 0;
     use.f1 = share < G ? start_of(share + 1) : 0;
     use.k = &s_use[warp];
@@ -351,7 +359,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     if (share >= G) return;
     for (;; ++use.r) {
         bool c = false;
-        const Known k = use.in_window(use.r, r_known) ? s_known[use.r - r_known] : look_up<NR, TILE>(a, use.r, c);
+        const Known k = use.in_window(use.r, r_known) ? s_known[use.r - r_known] : look_up<NR, TILE, SHARED>(a, use.r, c);
         const int64_t all = (int64_t)k.tiles * k.row_tiles * groups;
         if (left < all) {
             if (lane == 0) s_use[warp] = s_get[warp] = k;
@@ -375,7 +383,7 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         int slot, id, kv, pmax, floor;
         bool there;
     };
-    Walk<NR, TILE> get = use;
+    Walk<NR, TILE, SHARED> get = use;
     get.k = &s_get[warp];
     int tile = get.t0 + tw, issued = 0;
     bool more = true;
@@ -497,6 +505,50 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 for (int e = 0; e < 4; ++e) o[i][h][e] = 0.f;
 #pragma unroll
         for (int h = 0; h < RH; ++h) { m[h] = -INFINITY; l[h] = 0.f; }
+        if (SHARED && use.k->parts > 0 && use.t0 == 0 && tw == 0 && rows > 0) {
+            // the prefix, its parts in their order: maxima and sums of the rows g (and 8 + g), values of 2t and 2t + 1 (+ 8)
+            const int parts = use.k->parts;
+            const int64_t stride = (int64_t)a.plan->query_tokens * a.hq;
+            auto place = [&](int row) -> int64_t {
+                if (row >= rows) return -1;
+                int64_t tok;
+                int head;
+                split_row(a, rt * NR + row, tok, head);
+                return (tok + use.k->q0) * a.hq + kv * a.group + head;
+            };
+#pragma unroll
+            for (int h = 0; h < RH; ++h) {
+                const int64_t mine = place(g + 8 * h);
+                if (mine >= 0)
+#pragma unroll 4
+                    for (int k = 0; k < parts; ++k) m[h] = fmaxf(m[h], __ldcg(&a.pre_ml[k * stride + mine]).x);
+                int64_t at[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) at[e] = place(8 * h + 2 * t + e);
+#pragma unroll 2
+                for (int k = 0; k < parts; ++k) {
+                    const float2 ml = mine >= 0 ? __ldcg(&a.pre_ml[k * stride + mine]) : make_float2(-INFINITY, 0.f);
+                    const float f = weight(ml.x, m[h]);
+                    if (t == 0) l[h] += f * ml.y;            // (the row's four lanes are added up at the end)
+                    float fe[2];
+                    fe[0] = __shfl_sync(0xffffffffu, f, 8 * t);
+                    fe[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (at[e] < 0 || fe[e] == 0.f) continue;         // (a part without a token that the row sees holds no values)
+                        const float *src = a.pre_o + (k * stride + at[e]) * D;
+#pragma unroll
+                        for (int i = 0; i < MT; i += 2) {
+                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + Rows::vdim(g, i / 4) + 2 * (i % 4)));
+                            o[i][h][e] += fe[e] * x.x;
+                            o[i][h][2 + e] += fe[e] * x.y;
+                            o[i + 1][h][e] += fe[e] * x.z;
+                            o[i + 1][h][2 + e] += fe[e] * x.w;
+                        }
+                    }
+                }
+            }
+        }
 
         for (int tl = use.t0 + tw; tl < use.t1; tl += lanes, ++used) {
             cp_wait<ST - 2>();
@@ -819,10 +871,10 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
     }
 }
 
-template <int D, int NR, typename Rows, typename Act, bool SPLIT_P>
+template <int D, int NR, typename Rows, typename Act, bool SPLIT_P, bool SHARED>
 int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, cudaStream_t st)
 {
-    auto kernel = attention_rows_kernel<D, NR, Rows, Act, SPLIT_P>;
+    auto kernel = attention_rows_kernel<D, NR, Rows, Act, SPLIT_P, SHARED>;
     constexpr int smem = (int)sizeof(Shared<D, NR, Rows>);
     static_assert(Shared<D, NR, Rows>::ST >= 2 && smem + sizeof(Known) * (AT_KNOWN + 2 * Rows::WARPS) <= 232448, "shared memory of a CTA");
     static std::atomic<int> allowed{-1};                     // the device that knows of this kernel's shared memory
@@ -832,12 +884,21 @@ int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, cudaStream_t st)
     return VTOKEN_OK;
 }
 
-template <int D, typename Act>
+template <int D, typename Act, bool SHARED>
 int launch_by_type(vtoken_ctx *ctx, bool fp4, bool wide, const VtkAttnArgs &a, cudaStream_t st)
 {
     constexpr bool bf = Act::kind == VTOKEN_KV_BF16;
-    if (fp4) return wide ? launch<D, 16, Rows4<D, 8>, Act, !bf>(ctx, a, st) : launch<D, 8, Rows4<D, 16>, Act, !bf>(ctx, a, st);
-    return wide ? launch<D, 16, Rows16<D, Act>, Act, true>(ctx, a, st) : launch<D, 8, Rows16<D, Act>, Act, true>(ctx, a, st);
+    if (fp4) return wide ? launch<D, 16, Rows4<D, 8>, Act, !bf, SHARED>(ctx, a, st) : launch<D, 8, Rows4<D, 16>, Act, !bf, SHARED>(ctx, a, st);
+    return wide ? launch<D, 16, Rows16<D, Act>, Act, true, SHARED>(ctx, a, st) : launch<D, 8, Rows16<D, Act>, Act, true, SHARED>(ctx, a, st);
+}
+
+template <bool SHARED>
+int launch_by_heads(vtoken_ctx *ctx, const vtoken_heads *heads, bool wide, const VtkAttnArgs &a, cudaStream_t st)
+{
+    const bool fp4 = heads->kv_type == VTOKEN_KV_FP4, bf = heads->act_type == VTOKEN_KV_BF16;
+    if (heads->head_dim == 128)
+        return bf ? launch_by_type<128, VtkBf16, SHARED>(ctx, fp4, wide, a, st) : launch_by_type<128, VtkFp16, SHARED>(ctx, fp4, wide, a, st);
+    return bf ? launch_by_type<64, VtkBf16, SHARED>(ctx, fp4, wide, a, st) : launch_by_type<64, VtkFp16, SHARED>(ctx, fp4, wide, a, st);
 }
 
 }  // namespace
@@ -851,24 +912,14 @@ int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *
     return counters + shares * 2 * 8 * (heads->head_dim + 2) * 4;
 }
 
-int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st)
+int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, bool shared, cudaStream_t st)
 {
     vtk_attention_rows_workspace(ctx, heads, &a);
-    const bool fp4 = heads->kv_type == VTOKEN_KV_FP4, wide = (int64_t)a.group * max_query_len > 8;
-    if (heads->head_dim == 128)
-        return heads->act_type == VTOKEN_KV_BF16 ? launch_by_type<128, VtkBf16>(ctx, fp4, wide, a, st) : launch_by_type<128, VtkFp16>(ctx, fp4, wide, a, st);
-    return heads->act_type == VTOKEN_KV_BF16 ? launch_by_type<64, VtkBf16>(ctx, fp4, wide, a, st) : launch_by_type<64, VtkFp16>(ctx, fp4, wide, a, st);
+    const bool wide = (int64_t)a.group * max_query_len > 8;
+    return shared ? launch_by_heads<true>(ctx, heads, wide, a, st) : launch_by_heads<false>(ctx, heads, wide, a, st);
 }
 
-extern "C" {
-
-int64_t vtoken_attention_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens)
-{
-    if (!ctx || vtk_check_heads(ctx, heads, 0) != VTOKEN_OK || max_query_tokens < 0) return VTOKEN_EINVAL;
-    return vtk_attention_rows_workspace(ctx, heads, nullptr);
-}
-
-int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in, void *cuda_stream)
+int vtk_attention_args(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in, int64_t workspace_bytes, VtkAttnArgs &a)
 {
     if (!ctx || !heads || !in) return VTOKEN_EINVAL;
     if (vtk_check_heads(ctx, heads, layer) != VTOKEN_OK) return VTOKEN_EINVAL;
@@ -878,12 +929,11 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     float scale;
     if (!vtk_score_scale(heads, in->sm_scale, scale)) return VTOKEN_EINVAL;
     if ((((uintptr_t)in->q | (uintptr_t)in->out | (uintptr_t)in->workspace) & 15) || ((uintptr_t)in->lse & 3)) return VTOKEN_EINVAL;
-    VtkAttnArgs a;
     const int64_t dense = (int64_t)heads->num_q_heads * heads->head_dim;
     a.q_stride = vtk_stride(in->q_stride, dense);
     a.out_stride = vtk_stride(in->out_stride, dense);
     if (a.q_stride < 0 || a.out_stride < 0) return VTOKEN_EINVAL;
-    if (in->workspace_bytes < vtoken_attention_workspace_bytes(ctx, heads, in->max_query_tokens)) return VTOKEN_ECAPACITY;
+    if (in->workspace_bytes < workspace_bytes) return VTOKEN_ECAPACITY;
     if (in->max_query_tokens == 0) return VTOKEN_OK;
     a.num_requests = in->num_requests;
     a.q_offsets = VTK_ARR(ctx, in->q_offsets, ctx->cfg.max_requests + 1);
@@ -913,10 +963,31 @@ int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, 
     a.flags = &ctx->rt_counts->error_flags;
     a.counters = (uint32_t *)in->workspace + 4;
     a.part = nullptr;
-    const bool prompts = (int64_t)in->max_query_len * a.group > AT_ROW_LIMIT;
-    a.row_limit = prompts ? AT_ROW_LIMIT : INT32_MAX;
-    const int rc = vtk_launch_attention_rows(ctx, heads, a, prompts ? 1 : in->max_query_len, (cudaStream_t)cuda_stream);
-    return rc == VTOKEN_OK && prompts ? vtk_launch_attention_prompt(ctx, heads, a, (uint32_t *)in->workspace, (cudaStream_t)cuda_stream) : rc;
+    a.plan = nullptr;
+    a.groups = nullptr;
+    a.shared = nullptr;
+    a.pre_ml = nullptr;
+    a.pre_o = nullptr;
+    a.row_limit = (int64_t)in->max_query_len * a.group > VTK_ROW_LIMIT ? VTK_ROW_LIMIT : INT32_MAX;
+    return VTOKEN_OK;
+}
+
+extern "C" {
+
+int64_t vtoken_attention_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens)
+{
+    if (!ctx || vtk_check_heads(ctx, heads, 0) != VTOKEN_OK || max_query_tokens < 0) return VTOKEN_EINVAL;
+    return vtk_attention_rows_workspace(ctx, heads, nullptr);
+}
+
+int vtoken_attention(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in, void *cuda_stream)
+{
+    VtkAttnArgs a;
+    int rc = vtk_attention_args(ctx, heads, layer, in, in ? vtoken_attention_workspace_bytes(ctx, heads, in->max_query_tokens) : 0, a);
+    if (rc != VTOKEN_OK || in->max_query_tokens == 0) return rc;
+    const bool prompts = a.row_limit != INT32_MAX;
+    rc = vtk_launch_attention_rows(ctx, heads, a, prompts ? 1 : in->max_query_len, false, (cudaStream_t)cuda_stream);
+    return rc == VTOKEN_OK && prompts ? vtk_launch_attention_prompt(ctx, heads, a, (uint32_t *)in->workspace, false, (cudaStream_t)cuda_stream) : rc;
 }
 
 }  // extern "C"

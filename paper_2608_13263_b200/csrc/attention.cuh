@@ -5,6 +5,22 @@
 
 #include "heads.cuh"
 
+// A shared prefix as the planning kernel of attention_shared.cu leaves it in the workspace.
+struct VtkPrefixGroup {
+    int32_t q0, q1;                      // query rows of the group: those of consecutive requests
+    int32_t base, len;                   // the prefix: cache entries [base, base + len)
+    int32_t splits, tiles;               // parts that its tiles are cut into, tiles of a part
+    int32_t first, end;                  // requests
+    int64_t items;                       // items of the groups in front
+    int32_t members;                     // requests with query rows that read the prefix here
+    int32_t pad;
+};
+struct VtkPrefixPlan {
+    int64_t items;                       // of all groups: (256 query rows, part, key head)
+    int32_t groups;
+    int32_t query_tokens;                // of the call: parts are [splits][query_tokens][query heads]
+};
+
 struct VtkAttnArgs {
     const int32_t *num_requests;
     vtk_arr<const int32_t> q_offsets, positions, tt_offsets, cache_slots, cache_ids, cache_len;
@@ -22,6 +38,12 @@ struct VtkAttnArgs {
     uint32_t *counters;                  // workspace: arrivals of split rows, zero between calls
     float *part;                         // workspace: partial rows
     int32_t row_limit;                   // requests of more query rows (tokens times group) belong to attention_prompt.cu
+    // shared prefixes only
+    const VtkPrefixPlan *plan;
+    const VtkPrefixGroup *groups;
+    const int2 *shared;                  // per request: entries of its prefix, parts
+    float2 *pre_ml;                      // per part and row: running maximum (exponents of two) and sum of the prefix ...
+    float *pre_o;                        // ... and the sum of its weighted values
 };
 
 // Ids are not negative.  A query at p sees the ids in (vtk_floor(p), p] and those below `sinks`.
@@ -29,13 +51,22 @@ __device__ __forceinline__ int vtk_floor(int p, int window) { return window == 0
 __device__ __forceinline__ bool vtk_sees(int id, int p, int floor, int sinks) { return id <= p && (id > floor || id < sinks); }
 
 // What a request's queries read of its slot cache: entries [0, n_sink) and [lo, lo + n - n_sink), numbered
-// 0 .. n - 1 in that order ("virtual" indexes).
+// 0 .. n - 1 in that order ("virtual" indexes).  Behind a shared prefix the first of the two is [first, first + n_sink).
 struct VtkRequest {
     int pmax, floor;                     // no query sees an id above pmax, nor one up to floor that is no sink
     int64_t base;                        // first cache entry
-    int lo, n_sink, n;
-    __device__ __forceinline__ int64_t entry(int v) const { return base + (v < n_sink ? v : lo + (v - n_sink)); }
-    __device__ __forceinline__ int index(int v) const { return v < n_sink ? v : lo + (v - n_sink); }
+    int lo, n_sink, n, first;
+    __device__ __forceinline__ int index(int v) const { return v < n_sink ? first + v : lo + (v - n_sink); }
+    __device__ __forceinline__ int64_t entry(int v) const { return base + index(v); }
+    // without the entries in front of `prefix`
+    __device__ __forceinline__ void behind(int prefix)
+    {
+        const int hi = lo + (n - n_sink);
+        first = n_sink > prefix ? prefix : 0;
+        n_sink = n_sink > prefix ? n_sink - prefix : 0;
+        lo = lo > prefix ? lo : prefix;
+        n = n_sink + (hi > lo ? hi - lo : 0);
+    }
 };
 
 __device__ __forceinline__ int vtk_clamp_offset(int x, int cap) { return x < 0 ? 0 : (x > cap ? cap : x); }
@@ -65,6 +96,7 @@ __device__ inline int vtk_ids_up_to(const VtkAttnArgs &a, int64_t base, int len,
 __device__ inline VtkRequest vtk_request_span(const VtkAttnArgs &a, int64_t base, int len, int last, int pmin, int pmax)
 {
     VtkRequest q;
+    q.first = 0;
     q.pmax = pmax;
     q.floor = vtk_floor(pmin, a.window);
     q.base = base;
@@ -340,6 +372,9 @@ inline bool vtk_score_scale(const vtoken_heads *heads, float sm_scale, float &sc
 }
 
 // host: launchers of attention.cu and of attention_prompt.cu
-int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, cudaStream_t st);
-int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st);
+int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, bool shared, cudaStream_t st);
+int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, bool prefix, cudaStream_t st);
 int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs *a);
+constexpr int VTK_ROW_LIMIT = 32;        // query rows (tokens times group) of a request up to which attention.cu works on it
+// host: checks of a call and the kernels' arguments; VTOKEN_OK with max_query_tokens 0: nothing to do
+int vtk_attention_args(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in, int64_t workspace_bytes, VtkAttnArgs &a);

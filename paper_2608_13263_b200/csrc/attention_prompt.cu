@@ -36,7 +36,8 @@ struct Item {                            // what one CTA works on
     int none, ticket;
     int kv, q0, first, rows, len;        // key head; first query row of the request; first row and rows of the pair of tiles
     int pmin[2], pmax[2];                // positions of the two row tiles
-    int tiles;                           // tiles of 128 tokens
+    int tile0, tiles;                    // tiles of 128 tokens
+    int part;                            // shared prefixes: number of the part, -1: nobody reads these rows
     VtkRequest span;
 };
 
@@ -139,17 +140,135 @@ __device__ void next_item(const VtkAttnArgs &a, Shared<D> &sh, Item &out, int R,
         it.span.pmax = pmax;
         it.span.floor = vtk_floor(pmin, a.window);
         it.span.base = base;
+        it.span.first = 0;
         const int end = ids_up_to_warp(a, base, it.len, pmax);
         it.span.lo = a.window > 0 ? ids_up_to_warp(a, base, it.len, (int64_t)pmin - a.window) : 0;
         if (it.span.lo > end) it.span.lo = end;
         it.span.n_sink = a.sinks > 0 ? ids_up_to_warp(a, base, it.span.lo, (int64_t)a.sinks - 1) : 0;
         it.span.n = it.span.n_sink + end - it.span.lo;
+        it.tile0 = it.part = 0;
         it.tiles = (it.span.n + AP_TILE - 1) / AP_TILE;
     }
     if (lane == 0) out = it;
 }
 
+// The same for shared prefixes: the rows of a group, the entries of its first request, a part of the tiles.
+template <int D>
+__device__ void next_prefix_item(const VtkAttnArgs &a, Item &out, uint32_t *tickets)
+{
+    const int lane = vtk_lane();
+    int64_t idx = 0;
+    if (lane == 0) idx = (int64_t)atomicAdd(tickets, 1u);
+    idx = __shfl_sync(0xffffffffu, idx, 0);
+    Item it;
+    it.none = 1;
+    it.ticket = (int)idx;
+    if (idx < a.plan->items) {
+        it.none = 0;
+        int lo = 0, hi = a.plan->groups;     // the last group with items up to idx (groups without items have none in front of the next)
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32, probe = lo + vtk_lane() * step;
+            const int n = __popc(__ballot_sync(0xffffffffu, probe < hi && a.groups[probe].items <= idx));    // (lane 0's always is)
+            const int next_hi = lo + n * step;
+            lo += (n - 1) * step;
+            if (next_hi < hi) hi = next_hi;
+        }
+        const VtkPrefixGroup g = a.groups[lo];
+        int64_t left = idx - g.items;
+        it.kv = (int)(left % a.hkv);
+        left /= a.hkv;
+        it.part = (int)(left % g.splits);
+        it.first = (int)(left / g.splits) * 2 * AP_TILE;
+        it.q0 = g.q0;
+        it.len = g.len;
+        const int64_t rows = (int64_t)(g.q1 - g.q0) * a.group - it.first;
+        it.rows = rows < 2 * AP_TILE ? (int)rows : 2 * AP_TILE;
+        int pmin = INT32_MAX, pmax = -1;
+        for (int x = 0; x < 2; ++x) {
+            int lo_p = INT32_MAX, hi_p = -1;
+            const int r0 = it.first + x * AP_TILE, r1 = it.first + (it.rows < (x + 1) * AP_TILE ? it.rows : (x + 1) * AP_TILE);
+            if (r0 < r1)
+                for (int t = r0 / a.group + lane; t <= (r1 - 1) / a.group; t += 32) {
+                    const int p = a.positions[it.q0 + t];
+                    lo_p = p < lo_p ? p : lo_p;
+                    hi_p = p > hi_p ? p : hi_p;
+                }
+            it.pmin[x] = __reduce_min_sync(0xffffffffu, lo_p);
+            it.pmax[x] = __reduce_max_sync(0xffffffffu, hi_p);
+            pmin = it.pmin[x] < pmin ? it.pmin[x] : pmin;
+            pmax = it.pmax[x] > pmax ? it.pmax[x] : pmax;
+        }
+        it.span.pmax = pmax;
+        it.span.floor = vtk_floor(pmin, a.window);
+        it.span.base = g.base;
+        it.span.first = 0;
+        const int end = ids_up_to_warp(a, g.base, g.len, pmax);
+        it.span.lo = a.window > 0 ? ids_up_to_warp(a, g.base, g.len, (int64_t)pmin - a.window) : 0;
+        if (it.span.lo > end) it.span.lo = end;
+        it.span.n_sink = a.sinks > 0 ? ids_up_to_warp(a, g.base, it.span.lo, (int64_t)a.sinks - 1) : 0;
+        it.span.n = it.span.n_sink + end - it.span.lo;
+        const int all = (it.span.n + AP_TILE - 1) / AP_TILE;
+        it.tile0 = it.part * g.tiles;
+        it.tiles = all - it.tile0 < g.tiles ? (all > it.tile0 ? all - it.tile0 : 0) : g.tiles;
+        // rows of one request that reads the prefix for itself
+        int before = g.first, behind = g.end;
+        const int t0 = it.q0 + it.first / a.group, t1 = it.q0 + (it.first + it.rows - 1) / a.group;
+        while (behind - before > 1) {        // q_offsets[before] <= t0 < q_offsets[behind]
+            const int mid = (before + behind) >> 1;
+            if (a.q_offsets[mid] <= t0) before = mid; else behind = mid;
+        }
+        if (t1 < a.q_offsets[before + 1] && ((int64_t)a.q_offsets[before + 1] - a.q_offsets[before]) * a.group > a.row_limit) {
+            it.part = -1;
+            it.tiles = 0;
+        }
+    }
+    if (lane == 0) out = it;
+}
+
+// One query row over the tokens [v0, v1) of a prefix by one warp, token by token (see vtk_row_again); false when it stands.
 template <int D, bool FP4, typename Act>
+__device__ __noinline__ bool prefix_row_again(const VtkAttnArgs &a, int64_t q_row, int head, int pos, const VtkRequest &span, int len, int v0, int v1,
+                                              float (&o)[D / 32], float &m, float &l)
+{
+    if (!vtk_hidden_value<D, FP4, Act>(a, head, pos, span, len)) return false;
+    constexpr int N = D / 32;
+    const int lane = vtk_lane(), kv = head / a.group, floor = vtk_floor(pos, a.window);
+    float q[N];
+    const uint32_t *qp = reinterpret_cast<const uint32_t *>(a.q + q_row * a.q_stride + (int64_t)head * D + lane * N);
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) {
+        const float2 v = Act::unpack(qp[j]);
+        q[2 * j] = v.x;
+        q[2 * j + 1] = v.y;
+    }
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = 0.f;
+    for (int i = v0; i < v1; ++i) {
+        const int id = a.cache_ids.null() ? span.index(i) : a.cache_ids[span.entry(i)];
+        const int64_t slot = a.cache_slots[span.entry(i)];
+        if (slot < 0 || slot >= a.slots_per_layer || !vtk_sees(id, pos, floor, a.sinks)) continue;
+        float k[N], v[N], s = 0.f;
+        vtk_row_values<D, FP4, Act, N>(a.k_rows + slot * a.row_bytes, a.hkv, kv, lane * N, k);
+        vtk_row_values<D, FP4, Act, N>(a.v_rows + slot * a.row_bytes, a.hkv, kv, lane * N, v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) s += q[j] * k[j];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        s *= a.scale_log2;
+        const float m2 = fmaxf(m, s), keep = m == m2 ? 1.f : (m == -INFINITY ? 0.f : exp2f(m - m2));
+        const float p = s == -INFINITY ? 0.f : exp2f(s - m2);
+        l = l * keep + p;
+#pragma unroll
+        for (int j = 0; j < N; ++j) o[j] = o[j] * keep + p * v[j];
+        m = m2;
+    }
+    return true;
+}
+
+// PREFIX: the rows of all requests of a group over their shared prefix, left as running maximum, sum and weighted values
+template <int D, bool FP4, typename Act, bool PREFIX>
 __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid_constant__ VtkAttnArgs a, uint32_t *tickets, int row_limit,
                                                                     uint64_t limit_ns, float scale, int negate, int64_t stall)
 {
@@ -180,7 +299,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     R = R < 0 ? 0 : (R > a.max_requests ? a.max_requests : R);
     const int seg = (R + AP_NT - 1) / AP_NT;
     int pairs = 0;
-    for (int r = tid * seg; r < (tid + 1) * seg && r < R; ++r) {
+    for (int r = tid * seg; !PREFIX && r < (tid + 1) * seg && r < R; ++r) {
         int q0, qn, len;
         int64_t base;
         bool c;
@@ -200,7 +319,11 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     if (tid == 0) sh.prefix[0] = 0;
     __syncthreads();
     const uint32_t tmem = sh.tmem;
-    if (warp == 13) next_item<D>(a, sh, sh.item[0], R, seg, tickets, row_limit);
+    auto next = [&](Item &out) {
+        if (PREFIX) next_prefix_item<D>(a, out, tickets);
+        else next_item<D>(a, sh, out, R, seg, tickets, row_limit);
+    };
+    if (warp == 13) next(sh.item[0]);
 
     // running counts of the rings and barriers
     uint32_t kv_count = 0;               // K and V tiles loaded (producers) or used (mma)
@@ -340,6 +463,47 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (T > 0) {
                         tc_after_sync();
                         done_with(tile_count + T - 1);
+                    }
+                    if (PREFIX) {
+                        // as it is: the request's own tokens go on from here
+                        const bool write = have && it.part >= 0;
+                        const int64_t place = ((int64_t)it.part * a.plan->query_tokens + tok) * a.hq + head;
+                        if (write) a.pre_ml[place] = make_float2(l == 0.f ? -INFINITY : m * c, l);
+                        bool bad = false;
+                        float *dst = a.pre_o + place * D;
+#pragma unroll
+                        for (int q = 0; q < D / 32; ++q) {
+                            uint32_t o[32];
+                            if (T > 0) {
+                                tc_ld32(t_o + 32 * q, o);
+                                tc_wait_ld(o);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) bad |= !(fabsf(__uint_as_float(o[i])) < INFINITY);
+                                if (write && l != 0.f) {
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i)
+                                        *reinterpret_cast<uint4 *>(dst + 32 * q + 4 * i) = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                                }
+                            }
+                        }
+                        unsigned again = __ballot_sync(0xffffffffu, write && bad && l != 0.f && fabsf(l) < INFINITY);
+                        if (again) __syncwarp();                     // (other lanes write over what a row's own has just stored)
+                        while (again) {
+                            const int src = __ffs(again) - 1;
+                            again &= again - 1;
+                            const int64_t q_row = __shfl_sync(0xffffffffu, (int)tok, src), to = __shfl_sync(0xffffffffu, place, src);
+                            const int h2 = __shfl_sync(0xffffffffu, head, src), p2 = __shfl_sync(0xffffffffu, pos, src);
+                            const int v0 = it.tile0 * AP_TILE, v1 = (it.tile0 + T) * AP_TILE < it.span.n ? (it.tile0 + T) * AP_TILE : it.span.n;
+                            float acc[D / 32], m2, l2;
+                            if (prefix_row_again<D, FP4, Act>(a, q_row, h2, p2, it.span, it.len, v0, v1, acc, m2, l2)) {
+                                const float lift = exp2f(vtk_lift<Mma>());
+#pragma unroll
+                                for (int j = 0; j < D / 32; ++j) a.pre_o[to * D + lane * (D / 32) + j] = acc[j] * lift;
+                                if (lane == 0) a.pre_ml[to] = make_float2(m2, l2 * lift);
+                            }
+                        }
+                        tc_before_sync();
+                        return;
                     }
                     const float r = l == 0.f ? 0.f : a.v_mul / l;
                     const bool finite = fabsf(l) < INFINITY;         // (a sum that is not: the row sees a score that is not)
@@ -631,14 +795,14 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(AP_REGS_REST));
         each_item([&](const Item &it, int T, bool two) {
             if (warp == 13) {
-                next_item<D>(a, sh, sh.item[(item_count + 1) & 1], R, seg, tickets, row_limit);
+                next(sh.item[(item_count + 1) & 1]);
                 return;
             }
             int slot[2], id[2];
             auto fetch = [&](int j) {                              // this thread's two tokens of tile j
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int v = j * AP_TILE + (warp - 14) * 64 + 32 * i + lane;
+                    const int v = ((PREFIX ? it.tile0 : 0) + j) * AP_TILE + (warp - 14) * 64 + 32 * i + lane;
                     slot[i] = -1;
                     id[i] = INT32_MAX;
                     if (v < it.span.n) {
@@ -693,12 +857,12 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     }
 }
 
-template <int D, bool FP4, typename Act>
+template <int D, bool FP4, typename Act, bool PREFIX>
 int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st)
 {
     constexpr int smem = (int)sizeof(Shared<D>) + 1024;
     static_assert(smem <= 232448, "shared memory of a CTA");
-    auto kernel = attention_prompt_kernel<D, FP4, Act>;
+    auto kernel = attention_prompt_kernel<D, FP4, Act, PREFIX>;
     static std::atomic<int> allowed{-1};                     // the device that knows of this kernel's shared memory
     VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed, (const void *)kernel, smem));
     // the sign of the scores' factor goes into the product (a zero factor: one that no 32-bit score can be seen through)
@@ -709,17 +873,18 @@ int launch(vtoken_ctx *ctx, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_
     return VTOKEN_OK;
 }
 
-template <int D>
+template <int D, bool PREFIX>
 int launch_by_type(vtoken_ctx *ctx, const vtoken_heads *h, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st)
 {
     if (h->kv_type == VTOKEN_KV_FP4)
-        return h->act_type == VTOKEN_KV_BF16 ? launch<D, true, VtkBf16>(ctx, a, tickets, st) : launch<D, true, VtkFp16>(ctx, a, tickets, st);
-    return h->act_type == VTOKEN_KV_BF16 ? launch<D, false, VtkBf16>(ctx, a, tickets, st) : launch<D, false, VtkFp16>(ctx, a, tickets, st);
+        return h->act_type == VTOKEN_KV_BF16 ? launch<D, true, VtkBf16, PREFIX>(ctx, a, tickets, st) : launch<D, true, VtkFp16, PREFIX>(ctx, a, tickets, st);
+    return h->act_type == VTOKEN_KV_BF16 ? launch<D, false, VtkBf16, PREFIX>(ctx, a, tickets, st) : launch<D, false, VtkFp16, PREFIX>(ctx, a, tickets, st);
 }
 
 }  // namespace
 
-int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, cudaStream_t st)
+int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, bool prefix, cudaStream_t st)
 {
-    return heads->head_dim == 128 ? launch_by_type<128>(ctx, heads, a, tickets, st) : launch_by_type<64>(ctx, heads, a, tickets, st);
+    if (prefix) return heads->head_dim == 128 ? launch_by_type<128, true>(ctx, heads, a, tickets, st) : launch_by_type<64, true>(ctx, heads, a, tickets, st);
+    return heads->head_dim == 128 ? launch_by_type<128, false>(ctx, heads, a, tickets, st) : launch_by_type<64, false>(ctx, heads, a, tickets, st);
 }

@@ -1,15 +1,15 @@
 // Verification of drafted tokens: the first refusal, the row to draw from, the draw, the list of rejected drafts.
 //
 // Bound by the row of the vocabulary (two after a refusal) that the next token is drawn from.  A cluster works on a request; its
-// warps take consecutive runs of the row and sum them in 64 bits, the CTAs exchange their sums, and the one warp whose run holds the
-// drawn mass walks over its run again.  The drafts before it need two numbers each.  One more cluster tests the drafts of all
+// warps take consecutive runs of the row and sum them in 64 bits, the CTAs exchange their sums, and the run that holds the drawn mass is
+// cut up among its CTA's warps once more before one of them walks over what is left.  The drafts before it need two numbers each.  One more cluster tests the drafts of all
 // requests and lists the rejected ones, so that a step is one launch.
 #include "cluster.cuh"
 #include "heads.cuh"
 
 namespace {
 
-constexpr int VD_NT = 512, VD_WARPS = VD_NT / 32, VD_LANES = 8;     // VD_LANES: threads that test the drafts of a request
+constexpr int VD_NT = 256, VD_WARPS = VD_NT / 32, VD_LANES = 8;     // VD_LANES: threads that test the drafts of a request
 
 struct VerifyArgs {
     const int32_t *num_requests;
@@ -95,10 +95,95 @@ struct Row {
         if (q != nullptr) v = fmax(v - (double)mass(y), 0.0);
         return at == without ? 0.0 : v;
     }
+    static constexpr int STEP = 32 * P::VE, U = 16 / P::VE;  // elements of a warp's load; independent loads
+    // Of the elements [lo, hi) by a warp, in every lane.  CLEAN false: infinities are not taken out, a sum that is no finite number tells of
+    // them.  There a difference p - q >= 0 is the 32-bit one and its rounding error, which 32 bits hold too (|p| >= |q|), so that one
+    // conversion to 64 bits does where the definition has two and a comparison (conversions, at 16 a cycle and SM, bound the sum of a
+    // row that way); the errors of 16 elements are added in 32 bits, 2^-45 of the sum.
+    template <bool CLEAN, bool MINUS>
+    __device__ __forceinline__ double sum_of(int lo, int hi) const
+    {
+        double s = 0.0;
+        for (int i = lo + vtk_lane() * P::VE; i < hi; i += STEP * U) {
+            float x[U][P::VE], y[U][P::VE], low = 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) get(i + u * STEP < hi ? i + u * STEP : vocab, x[u], y[u]);
+            if (!CLEAN && !MINUS) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if ((uint32_t)(without - (i + u * STEP)) < (uint32_t)P::VE) {        // (one lane, once a row)
+#pragma unroll
+                        for (int e = 0; e < P::VE; ++e)
+                            if (i + u * STEP + e == without) x[u][e] = 0.f;
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < P::VE; ++e) {
+                    if (CLEAN) {
+                        s += value(i + u * STEP + e, x[u][e], y[u][e]);
+                    } else if (MINUS) {
+                        const float q0 = fmaxf(y[u][e], 0.f), p0 = fmaxf(x[u][e], q0), d = p0 - q0;
+                        low += (p0 - d) - q0;
+                        s += (double)d;
+                    } else {
+                        s += (double)fmaxf(x[u][e], 0.f);
+                    }
+                }
+            s += (double)low;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        return s;
+    }
+    __device__ __forceinline__ double sum(int lo, int hi, bool clean) const
+    {
+        if (clean) return sum_of<true, true>(lo, hi);
+        return q != nullptr ? sum_of<false, true>(lo, hi) : sum_of<false, false>(lo, hi);
+    }
+    // the first element of [lo, hi) at which the mass, `before` in front of it, exceeds `drawn`; else the last that has any; -1: none
+    __device__ __forceinline__ int find(int lo, int hi, double before, double drawn) const
+    {
+        int any = -1;
+        for (int i0 = lo; i0 < hi; i0 += STEP * U) {
+            float x[U][P::VE], y[U][P::VE];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * STEP + vtk_lane() * P::VE;
+                get(i < hi ? i : vocab, x[u], y[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * STEP + vtk_lane() * P::VE;
+                double v[P::VE], s = 0.0;
+                int mine = -1;
+#pragma unroll
+                for (int e = 0; e < P::VE; ++e) {
+                    v[e] = i < hi ? value(i + e, x[u][e], y[u][e]) : 0.0;
+                    if (v[e] > 0.0) mine = i + e;
+                    s += v[e];
+                }
+                const double incl = vtk_warp_incl_scan(s);
+                double c = before + (incl - s);
+                int found = -1;
+#pragma unroll
+                for (int e = 0; e < P::VE; ++e) {
+                    c += v[e];
+                    if (found < 0 && c > drawn && v[e] > 0.0) found = i + e;
+                }
+                const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
+                if (who) return __shfl_sync(0xffffffffu, found, __ffs(who) - 1);
+                any = max(any, __reduce_max_sync(0xffffffffu, mine));
+                before += __shfl_sync(0xffffffffu, incl, 31);
+            }
+        }
+        return any;
+    }
 };
 
 struct Shared {
-    double warp_sum[VD_WARPS], cta_sum[2];
+    double warp_sum[VD_WARPS], again[VD_WARPS], cta_sum[2];
     int at;                              // first refusal, or the number of drafts
     int scan[VD_WARPS + 1];
 };
@@ -146,10 +231,10 @@ __device__ void list_rejected(const VerifyArgs &a, Shared &sh, int R, bool &clip
 }
 
 template <typename P, bool VEC>
-__global__ void __launch_bounds__(VD_NT) verify_kernel(const __grid_constant__ VerifyArgs a, int row_clusters)
+__global__ void __launch_bounds__(VD_NT, 3) verify_kernel(const __grid_constant__ VerifyArgs a, int row_clusters)
 {
     using T = typename P::type;
-    constexpr int VE = P::VE, STEP = 32 * VE;
+    constexpr int STEP = Row<P, VEC>::STEP;
     __shared__ Shared sh;
     vtk_release_successor();
     vtk_wait_for_predecessor();
@@ -192,20 +277,9 @@ __global__ void __launch_bounds__(VD_NT) verify_kernel(const __grid_constant__ V
                     if (i != at) a.out_tokens[d.d0 + r + i] = i < at ? a.draft_tokens[d.d0 + i] : -1;
         }
         double before, total;
+        bool clean = false;
         for (;;) {
-            double sum = 0.0;
-            constexpr int U = 4;
-            for (int i = lo + lane * VE; i < hi; i += STEP * U) {
-                float x[U][VE], y[U][VE];
-#pragma unroll
-                for (int u = 0; u < U; ++u) row.get(i + u * STEP < hi ? i + u * STEP : a.vocab, x[u], y[u]);
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) sum += i + u * STEP < hi ? row.value(i + u * STEP + e, x[u][e], y[u][e]) : 0.0;
-            }
-#pragma unroll
-            for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+            const double sum = row.sum(lo, hi, clean);
             if (lane == 0) sh.warp_sum[warp] = sum;
             __syncthreads();
             if (tid == 0) {
@@ -220,6 +294,10 @@ __global__ void __launch_bounds__(VD_NT) verify_kernel(const __grid_constant__ V
                 total += C > 1 ? vtk_cluster_read(&sh.cta_sum[turn & 1], c) : sh.cta_sum[turn & 1];
             }
             ++turn;
+            if (!clean && !(total < INFINITY)) {             // (an infinity or what came of one: element by element)
+                clean = true;
+                continue;
+            }
             if (total > 0.0 || (row.q == nullptr && row.without < 0)) break;
             row.q = nullptr;                                 // the draft's source has all that the target has
             row.without = -1;
@@ -236,48 +314,32 @@ __global__ void __launch_bounds__(VD_NT) verify_kernel(const __grid_constant__ V
             if (owner < 0 && upto > drawn) owner = c;
         }
         if (owner < 0) owner = last;
-        int token = -1;
         if (owner == rank) {
-            int w_owner = -1, w_last = -1;
-            double w_before = 0.0;
-            upto = before;
-            for (int w = 0; w < VD_WARPS; ++w) {
-                const double s = sh.warp_sum[w];
-                if (s > 0.0) w_last = w;
-                if (w_owner < 0 && upto + s > drawn) w_owner = w;
-                upto += s;
-            }
-            if (w_owner < 0) w_owner = w_last;
-            w_before = before;
-            for (int w = 0; w < w_owner; ++w) w_before += sh.warp_sum[w];
-            if (warp == w_owner) {
-                int any = -1;                                // the last element with mass
-                for (int i0 = lo; i0 < hi && token < 0; i0 += STEP) {
-                    const int i = i0 + lane * VE;
-                    float x[VE], y[VE];
-                    row.get(i < hi ? i : a.vocab, x, y);
-                    double v[VE], sum = 0.0;
-                    int mine = -1;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        v[e] = i < hi ? row.value(i + e, x[e], y[e]) : 0.0;
-                        if (v[e] > 0.0) mine = i + e;
-                        sum += v[e];
-                    }
-                    const double incl = vtk_warp_incl_scan(sum);
-                    double c = w_before + (incl - sum);
-                    int found = -1;
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        c += v[e];
-                        if (found < 0 && c > drawn && v[e] > 0.0) found = i + e;
-                    }
-                    const unsigned who = __ballot_sync(0xffffffffu, found >= 0);
-                    if (who) token = __shfl_sync(0xffffffffu, found, __ffs(who) - 1);
-                    any = max(any, __reduce_max_sync(0xffffffffu, mine));
-                    w_before += __shfl_sync(0xffffffffu, incl, 31);
+            // which warp's run, which eighth of it, which element
+            auto pick = [&](const double (&sums)[VD_WARPS], double &from) {
+                int w = -1, with_mass = -1;
+                double at_w = from, upto = from, at_mass = from;
+                for (int i = 0; i < VD_WARPS; ++i) {
+                    if (sums[i] > 0.0) { with_mass = i; at_mass = upto; }
+                    if (w < 0 && upto + sums[i] > drawn) { w = i; at_w = upto; }
+                    upto += sums[i];
                 }
-                if (token < 0) token = any;
+                from = w < 0 ? at_mass : at_w;
+                return w < 0 ? with_mass : w;
+            };
+            double from = before;
+            const int64_t r0 = (int64_t)(rank * VD_WARPS + pick(sh.warp_sum, from)) * per;
+            const int piece = ((per + VD_WARPS - 1) / VD_WARPS + STEP - 1) / STEP * STEP;
+            auto edge = [&](int w) {                         // of the pieces of the run
+                const int64_t x = (int64_t)w * piece < per ? r0 + (int64_t)w * piece : r0 + per;
+                return x < a.vocab ? (int)x : a.vocab;
+            };
+            const double sum = row.sum(edge(warp), edge(warp + 1), clean);
+            if (lane == 0) sh.again[warp] = sum;
+            __syncthreads();
+            const int w = pick(sh.again, from);
+            if (warp == w) {
+                const int token = row.find(edge(w), edge(w + 1), from, drawn);
                 if (lane == 0) {
                     a.next_tokens[r] = token;
                     if (!a.out_tokens.null()) a.out_tokens[d.d0 + r + at] = token;
@@ -296,8 +358,10 @@ __global__ void __launch_bounds__(VD_NT) verify_kernel(const __grid_constant__ V
 template <typename P>
 int launch(vtoken_ctx *ctx, const VerifyArgs &a, bool vec, cudaStream_t st)
 {
+    // CTAs of a request: two for each SM in all, a CTA not below 2048 elements.  (Many requests: a cluster whose CTAs do not start
+    // together waits for the last, 200 requests of 128 256 take 91 us with eight CTAs each and 44 with two.)
     int size = 1;
-    while (size < 8 && a.vocab > size * VD_NT * 8) size *= 2;
+    while (size < 8 && a.vocab > size * VD_NT * 8 && (int64_t)a.max_requests * size < 2 * ctx->num_sms) size *= 2;
     const int64_t most = (int64_t)ctx->num_sms * 8 / size;
     const int rows = a.max_requests < most ? a.max_requests : (int)most, clusters = rows + (a.num_victims != nullptr ? 1 : 0);
     VTK_CUDA(ctx, vec ? vtk_launch_clusters(ctx, verify_kernel<P, true>, size, dim3(clusters * size), dim3(VD_NT), 0, st, a, rows)

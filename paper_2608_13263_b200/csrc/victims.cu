@@ -12,7 +12,7 @@
 
 namespace {
 
-constexpr int SV_NT = 512, SV_WARPS = SV_NT / 32, SV_BINS = 2048, SV_KEYS = 16384, SV_MAX_CLUSTER = 8;
+constexpr int SV_BINS = 2048, SV_KEYS = 8192, SV_MAX_CLUSTER = 16;
 
 struct SelectArgs {
     const int32_t *num_requests;
@@ -68,39 +68,50 @@ __device__ __forceinline__ uint32_t key_of(float x)
     return (b >> 31) ? ~b : b | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t key_at(const SelectArgs &a, const Cut &c, int entry, int &id, bool &bad)
-{
-    id = a.cache_ids.null() ? entry : a.cache_ids[c.base + entry];
-    if (id < 0 || id >= c.range) { bad = true; return 0u; }
-    return key_of(a.scores[c.base + id]);
-}
-
 struct Shared {
-    int hist[2 * SV_BINS + SV_BINS / 2]; // of the three digits
-    int64_t sums[SV_WARPS];
+    alignas(16) int hist[2 * SV_BINS + SV_BINS / 2];         // of the three digits
+    alignas(16) int slice[SV_BINS / 2];  // clusters: this CTA's share of the bins, of all CTAs
+    int64_t sums[32];
     int warp_tot[32];
-    uint64_t part[SV_WARPS], part_total; // keys below the threshold, equal ones << 32
+    uint64_t part[32], part_total; // keys below the threshold, equal ones << 32
     Cut cut;
     int bin, below, inside;
 };
 
-__device__ __forceinline__ void count_key(int *hist, int bin, bool there)
+// of a lane's four keys those that begin with `prefix`, by their next digit (SHIFT: bits behind it; 0xffffffff: there is none)
+template <int SHIFT>
+__device__ __forceinline__ void count_keys(int *hist, const uint32_t (&k)[4], uint32_t prefix)
 {
-    // (many tokens that nothing has looked at: one bin for the whole warp)
-    const unsigned who = __ballot_sync(0xffffffffu, there);
-    if (who == 0) return;
-    const int leader = __ffs(who) - 1, first = __shfl_sync(0xffffffffu, bin, leader);
-    if (__all_sync(0xffffffffu, !there || bin == first)) {
-        if (vtk_lane() == leader) atomicAdd(hist + first, __popc(who));
-    } else if (there) {
-        atomicAdd(hist + bin, 1);
+    constexpr int BITS = SHIFT == 0 ? 10 : 11;
+    constexpr uint32_t MASK = (1u << BITS) - 1u;
+    if (SHIFT == 21) {                   // tokens that nothing has looked at all have one key: one count for the warp
+        const uint32_t first = __shfl_sync(0xffffffffu, k[0], 0);
+        if (__all_sync(0xffffffffu, k[0] == first && k[1] == first && k[2] == first && k[3] == first)) {
+            if (vtk_lane() == 0 && first != 0xffffffffu) atomicAdd(hist + (first >> SHIFT), 128);
+            return;
+        }
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (SHIFT == 21 ? k[j] != 0xffffffffu : k[j] >> ((SHIFT + BITS) & 31) == prefix) atomicAdd(hist + ((k[j] >> SHIFT) & MASK), 1);      // (no score's key begins like 0xffffffff)
 }
 
-__global__ void __launch_bounds__(SV_NT) select_kernel(const __grid_constant__ SelectArgs a)
+template <typename T, int U, typename F>
+__device__ __forceinline__ void for_each(T (&x)[U][4], F f)
 {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f(u, j, x[u][j]);
+}
+
+// NT: 256 threads, four requests an SM at a time; 1024 where clusters work on a request
+template <int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) select_kernel(const __grid_constant__ SelectArgs a)
+{
+    constexpr int WARPS = NT / 32;
     __shared__ Shared sh;
-    extern __shared__ uint32_t keys[];
+    extern __shared__ __align__(16) uint32_t keys[];
     vtk_release_successor();
     vtk_wait_for_predecessor();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -114,16 +125,16 @@ __global__ void __launch_bounds__(SV_NT) select_kernel(const __grid_constant__ S
     int seen = 0;
     for (int r = blockIdx.x / C; r < R; r += clusters) {
         int64_t mine = 0;
-        for (int i = seen + tid; i <= r; i += SV_NT) {
+        for (int i = seen + tid; i <= r; i += NT) {
             const Cut c = look_up(a, i, clipped);
             if (i == r) sh.cut = c; else mine += c.v;
         }
-        for (int i = tid; i < (int)(sizeof(sh.hist) / sizeof(int)); i += SV_NT) sh.hist[i] = 0;
+        for (int i = tid; i < (int)(sizeof(sh.hist) / sizeof(int)); i += NT) sh.hist[i] = 0;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
         if (lane == 0) sh.sums[warp] = mine;
         __syncthreads();
-        for (int w = 0; w < SV_WARPS; ++w) out += sh.sums[w];
+        for (int w = 0; w < WARPS; ++w) out += sh.sums[w];
         const Cut c = sh.cut;
         seen = r + 1;
         if (r == R - 1 && rank == 0 && tid == 0) {
@@ -135,69 +146,118 @@ __global__ void __launch_bounds__(SV_NT) select_kernel(const __grid_constant__ S
             // this CTA's part of the candidates, a run of it for each warp
             const int n = c.hi - c.lo;
             const int part0 = (int)((int64_t)n * rank / C), part1 = (int)((int64_t)n * (rank + 1) / C), np = part1 - part0;
-            const int per = ((np + SV_NT - 1) / SV_NT) * 32, w0 = warp * per < np ? warp * per : np, w1 = w0 + per < np ? w0 + per : np;
+            const int per = ((np + 4 * NT - 1) / (4 * NT)) * 128, w0 = warp * per < np ? warp * per : np, w1 = w0 + per < np ? w0 + per : np;
             uint32_t threshold = 0xffffffffu;                // above every key
             int less = c.v, keep_equal = 0;
-            auto key = [&](int i, int &id) { return key_at(a, c, c.lo + part0 + i, id, bad); };
             const bool all = c.v == n;
-            if (!all) {
-                constexpr int U = 8;                         // independent loads a lane
-                for (int i = w0; i < w1; i += 32 * U) {
-                    uint32_t k[U];
-                    int id;
+            // the candidates i + lane, + 32, ..., 0xffffffff behind the last (no score has that key): from the tables, or kept
+            const int32_t *id_at = a.cache_ids.null() ? nullptr : a.cache_ids.at(c.base + c.lo + part0, np);
+            const float *score_at = a.scores.at(c.base, c.range);
+            const int entry0 = c.lo + part0;
+            auto fetch = [&](int i, auto &id, auto &k, auto whole) {
+                constexpr bool WHOLE = decltype(whole)::value;       // no candidate of these lies behind the run
+                for_each(id, [&](int u, int j, int &x) {
+                    const int at = i + 128 * u + 32 * j + lane;
+                    x = id_at != nullptr ? (WHOLE || at < w1 ? id_at[at] : 0) : entry0 + at;
+                });
+                for_each(k, [&](int u, int j, uint32_t &x) {
+                    x = 0xffffffffu;
+                    if (!WHOLE && i + 128 * u + 32 * j + lane >= w1) return;
+                    const bool ok = (uint32_t)id[u][j] < (uint32_t)c.range;
+                    bad |= !ok;
+                    x = ok ? key_of(score_at[id[u][j]]) : 0u;
+                });
+            };
+            auto kept = [&](int i, uint32_t (&k)[1][4]) {
+                if (i + 128 <= a.keys) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const int at = i + 32 * u + lane;
-                        k[u] = at < w1 ? key(at, id) : 0u;
-                    }
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const int at = i + 32 * u + lane;
-                        if (at < w1 && at < a.keys) keys[at] = k[u];
-                        count_key(sh.hist, (int)(k[u] >> 21), at < w1);
-                    }
+                    for (int j = 0; j < 4; ++j) k[0][j] = keys[i + 32 * j + lane];
+                } else {
+                    int id[1][4];
+                    fetch(i, id, k, std::false_type());
                 }
-                auto again = [&](int at) {
-                    int id;
-                    return at < a.keys ? keys[at] : key(at, id);
+            };
+            if (!all) {
+                constexpr int U = 3;                         // twelve independent loads a lane, twice
+                auto count = [&](int i0, auto whole) {
+                    uint32_t k[U][4];
+                    int id[U][4];
+                    fetch(i0, id, k, whole);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (!decltype(whole)::value && i0 + 128 * u >= w1) break;    // (what is behind is another warp's)
+                        if (i0 + 128 * (u + 1) <= a.keys)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) keys[i0 + 128 * u + 32 * j + lane] = k[u][j];
+                        count_keys<21>(sh.hist, k[u], 0u);
+                    }
                 };
+                int i0 = w0;
+                for (; i0 + 128 * U <= w1; i0 += 128 * U) count(i0, std::true_type());
+                for (; i0 < w1; i0 += 128 * U) count(i0, std::false_type());
                 uint32_t prefix = 0;
                 int rest = c.v - 1;                          // rank of the wanted key among those that share the prefix
                 less = 0;
 #pragma unroll
                 for (int pass = 0; pass < 3; ++pass) {
-                    constexpr int SHIFT[3] = {21, 10, 0}, BITS[3] = {11, 11, 10};
+                    constexpr int BITS[3] = {11, 11, 10};
                     int *hist = sh.hist + pass * SV_BINS;
                     const int bins = 1 << BITS[pass];
                     if (pass > 0) {
-                        for (int i = w0; i < w1; i += 32) {
-                            const uint32_t k = i + lane < w1 ? again(i + lane) : 0u;
-                            const bool there = i + lane < w1 && (k >> (SHIFT[pass] + BITS[pass])) == prefix;
-                            count_key(hist, (int)((k >> SHIFT[pass]) & (uint32_t)(bins - 1)), there);
+                        for (int i0 = w0; i0 < w1; i0 += 128) {
+                            uint32_t k[1][4];
+                            kept(i0, k);
+                            if (pass == 1) count_keys<10>(hist, k[0], prefix);
+                            else count_keys<0>(hist, k[0], prefix);
                         }
                     }
                     sync();
-                    int h[4] = {0, 0, 0, 0}, sum = 0;
-                    if (tid * 4 < bins) {
-                        for (int p = 0; p < C; ++p)
+                    if (C > 1) {                             // every CTA adds up a share of the bins
+                        const int share = bins / C;
+                        for (int i = tid; i < share; i += NT) {
+                            int x = 0;
+#pragma unroll 8
+                            for (int p = 0; p < C; ++p) x += vtk_cluster_read(hist + rank * share + i, p);
+                            sh.slice[i] = x;
+                        }
+                        vtk_cluster_sync();
+                    }
+                    constexpr int PER = SV_BINS / NT;        // bins of a thread
+                    int h[PER], sum = 0;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) h[j] += C > 1 ? vtk_cluster_read(hist + tid * 4 + j, p) : hist[tid * 4 + j];
+                    for (int j = 0; j < PER; ++j) h[j] = 0;
+                    if (tid * PER < bins) {
+                        if (C == 1) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) sum += h[j];
+                            for (int j = 0; j < PER; ++j) h[j] = hist[tid * PER + j];
+                        } else {
+                            const int share = bins / C;      // (a power of two, 64 or more)
+#pragma unroll
+                            for (int j = 0; j < PER; j += 2) {
+                                const int at = tid * PER + j;
+                                const int2 x = vtk_cluster_read(reinterpret_cast<const int2 *>(sh.slice + at % share), at / share);
+                                h[j] = x.x;
+                                h[j + 1] = x.y;
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) sum += h[j];
                     }
                     const int in_warp = vtk_warp_incl_scan(sum);
                     if (lane == 31) sh.warp_tot[warp] = in_warp;
                     __syncthreads();
                     int before = in_warp - sum;
                     for (int w = 0; w < warp; ++w) before += sh.warp_tot[w];
+                    if (rest >= before && rest < before + sum) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (rest >= before && rest < before + h[j]) {
-                            sh.bin = tid * 4 + j;
-                            sh.below = before;
-                            sh.inside = h[j];
+                        for (int j = 0; j < PER; ++j) {
+                            if (rest >= before && rest < before + h[j]) {
+                                sh.bin = tid * PER + j;
+                                sh.below = before;
+                                sh.inside = h[j];
+                            }
+                            before += h[j];
                         }
-                        before += h[j];
                     }
                     __syncthreads();
                     prefix = (prefix << BITS[pass]) | (uint32_t)sh.bin;
@@ -209,29 +269,26 @@ __global__ void __launch_bounds__(SV_NT) select_kernel(const __grid_constant__ S
                 threshold = prefix;
             }
             // how many of each warp's run are below and equal, then the list
-            auto value = [&](int at, int &id) {
-                if (!all && at < a.keys) {
-                    id = a.cache_ids.null() ? c.lo + part0 + at : a.cache_ids[c.base + c.lo + part0 + at];
-                    return keys[at];
-                }
-                return key(at, id);
-            };
             int lt = 0, eq = 0;
             if (all) {
                 lt = w1 - w0;
             } else {
-                for (int i = w0; i < w1; i += 32) {
-                    int id;
-                    const bool in = i + lane < w1;
-                    const uint32_t k = in ? (i + lane < a.keys ? keys[i + lane] : key(i + lane, id)) : 0u;
-                    lt += __popc(__ballot_sync(0xffffffffu, in && k < threshold));
-                    eq += __popc(__ballot_sync(0xffffffffu, in && k == threshold));
+                for (int i0 = w0; i0 < w1; i0 += 128) {
+                    uint32_t k[1][4];
+                    kept(i0, k);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        lt += k[0][j] < threshold;
+                        eq += k[0][j] == threshold;
+                    }
                 }
+                lt = __reduce_add_sync(0xffffffffu, lt);
+                eq = __reduce_add_sync(0xffffffffu, eq);
             }
             if (lane == 0) sh.part[warp] = (uint64_t)(uint32_t)lt | (uint64_t)(uint32_t)eq << 32;
             __syncthreads();
             uint64_t upto = 0, total = 0;
-            for (int w = 0; w < SV_WARPS; ++w) {
+            for (int w = 0; w < WARPS; ++w) {
                 if (w < warp) upto += sh.part[w];
                 total += sh.part[w];
             }
@@ -240,24 +297,43 @@ __global__ void __launch_bounds__(SV_NT) select_kernel(const __grid_constant__ S
                 vtk_cluster_sync();
                 for (int p = 0; p < rank; ++p) upto += vtk_cluster_read(&sh.part_total, p);
             }
-            lt = (int)(uint32_t)upto;
             eq = (int)(upto >> 32);
-            for (int i = w0; i < w1; i += 32) {
-                int id = 0;
-                const bool in = i + lane < w1;
-                const uint32_t k = in ? value(i + lane, id) : 0u;
-                const unsigned is_lt = __ballot_sync(0xffffffffu, in && k < threshold), is_eq = __ballot_sync(0xffffffffu, in && k == threshold);
-                const unsigned before = (1u << lane) - 1u;
-                const int my_lt = lt + __popc(is_lt & before), my_eq = eq + __popc(is_eq & before);
-                if (in && (k < threshold || (k == threshold && my_eq >= keep_equal))) {
-                    const int64_t at = out + my_lt + (my_eq > keep_equal ? my_eq - keep_equal : 0);
-                    if (at < a.max_victims) {
-                        a.victim_req[at] = r;
-                        a.victim_tok[at] = id;
-                    }
+            int64_t next = out + (uint32_t)upto + (eq > keep_equal ? eq - keep_equal : 0);       // where the run's victims go
+            constexpr int U = 3;
+            for (int i0 = w0; i0 < w1; i0 += 128 * U) {
+                uint32_t k[U][4];
+                int id[U][4];
+                if (all || i0 + 128 * U > a.keys) {
+                    fetch(i0, id, k, std::false_type());
+                } else {
+                    for_each(k, [&](int u, int j, uint32_t &x) {
+                        const int at = i0 + 128 * u + 32 * j + lane;
+                        x = at < w1 ? keys[at] : 0xffffffffu;
+                    });
+                    for_each(id, [&](int u, int j, int &x) {
+                        const int at = i0 + 128 * u + 32 * j + lane;
+                        x = entry0 + at;
+                        if (id_at != nullptr && k[u][j] <= threshold && at < w1) x = id_at[at];
+                    });
                 }
-                lt += __popc(is_lt);
-                eq += __popc(is_eq);
+                const unsigned before = (1u << lane) - 1u;
+                for_each(k, [&](int u, int j, uint32_t &x) {
+                    bool leaves = x < threshold;
+                    if (!all) {
+                        const unsigned eqs = __ballot_sync(0xffffffffu, x == threshold);
+                        if (eqs) {
+                            leaves |= x == threshold && eq + __popc(eqs & before) >= keep_equal;
+                            eq += __popc(eqs);
+                        }
+                    }
+                    const unsigned gone = __ballot_sync(0xffffffffu, leaves);
+                    const int64_t to = next + __popc(gone & before);
+                    if (leaves && to < a.max_victims) {
+                        a.victim_req[to] = r;
+                        a.victim_tok[to] = id[u][j];
+                    }
+                    next += __popc(gone);
+                });
             }
             out += c.v;
         }
@@ -299,9 +375,16 @@ extern "C" int vtoken_select_victims(vtoken_ctx *ctx, const vtoken_select_in *in
     a.keys = keys > SV_KEYS ? SV_KEYS : (int)keys;
     const int64_t most = (int64_t)ctx->num_sms * 8 / size;
     const int clusters = ctx->cfg.max_requests < most ? ctx->cfg.max_requests : (int)most;
-    static std::atomic<int> allowed{-1};
-    VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed, (const void *)select_kernel, SV_KEYS * 4));
-    VTK_CUDA(ctx, vtk_launch_clusters(ctx, select_kernel, size, dim3(clusters * size), dim3(SV_NT), a.keys * 4, (cudaStream_t)cuda_stream, a));
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    static std::atomic<int> allowed[2] = {{-1}, {-1}};       // the device that knows of the kernels' shared memory and clusters of 16
+    if (size == 1) {
+        VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed[0], (const void *)select_kernel<256>, SV_KEYS * 4));
+        VTK_CUDA(ctx, vtk_launch_clusters(ctx, select_kernel<256>, 1, dim3(clusters), dim3(256), a.keys * 4, st, a));
+    } else {
+        if (size > 8) VTK_CUDA(ctx, cudaFuncSetAttribute((const void *)select_kernel<1024>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed[1], (const void *)select_kernel<1024>, SV_KEYS * 4));
+        VTK_CUDA(ctx, vtk_launch_clusters(ctx, select_kernel<1024>, size, dim3(clusters * size), dim3(1024), a.keys * 4, st, a));
+    }
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
 }

@@ -195,7 +195,7 @@ __device__ __forceinline__ float weight(float m, float top) { return m == -INFIN
 // one request as the cut sees it
 struct Known {
     int q0, qn, len, tiles, row_tiles;
-    int parts;                           // of the shared prefix in front: where the running maximum and sums go on from
+    int prefix;                          // a shared prefix is in front: the running maximum and sums go on from there
     VtkRequest s;
 };
 
@@ -207,7 +207,7 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
     vtk_request_rows(a, r, k.q0, k.qn, k.s.base, k.len, c);
     clipped |= c;
     if (k.qn * (int64_t)a.group > a.row_limit) k.qn = 0;
-    k.parts = 0;
+    k.prefix = 0;
     k.s.lo = k.s.n_sink = k.s.first = 0;
     k.s.n = k.len;
     k.s.pmax = k.s.floor = -1;
@@ -223,10 +223,10 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
         }
         k.s = vtk_request_span(a, k.s.base, k.len, last, pmin, pmax);
         if (SHARED) {
-            const int2 prefix = a.shared[r];
-            if (prefix.x > 0) {
-                k.parts = prefix.y;
-                k.s.behind(prefix.x);
+            const int prefix = a.shared[r];
+            if (prefix > 0) {
+                k.prefix = 1;
+                k.s.behind(prefix);
             }
         }
     }
@@ -505,10 +505,8 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 for (int e = 0; e < 4; ++e) o[i][h][e] = 0.f;
 #pragma unroll
         for (int h = 0; h < RH; ++h) { m[h] = -INFINITY; l[h] = 0.f; }
-        if (SHARED && use.k->parts > 0 && use.t0 == 0 && tw == 0 && rows > 0) {
-            // the prefix, its parts in their order: maxima and sums of the rows g (and 8 + g), values of 2t and 2t + 1 (+ 8)
-            const int parts = use.k->parts;
-            const int64_t stride = (int64_t)a.plan->query_tokens * a.hq;
+        if (SHARED && use.k->prefix && use.t0 == 0 && tw == 0 && rows > 0) {
+            // what the prefix left: maxima and sums of the rows g (and 8 + g), values of 2t and 2t + 1 (+ 8)
             auto place = [&](int row) -> int64_t {
                 if (row >= rows) return -1;
                 int64_t tok;
@@ -519,32 +517,24 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
 #pragma unroll
             for (int h = 0; h < RH; ++h) {
                 const int64_t mine = place(g + 8 * h);
-                if (mine >= 0)
-#pragma unroll 4
-                    for (int k = 0; k < parts; ++k) m[h] = fmaxf(m[h], __ldcg(&a.pre_ml[k * stride + mine]).x);
-                int64_t at[2];
+                if (mine >= 0) {
+                    const float2 ml = __ldcg(&a.pre_ml[mine]);
+                    m[h] = ml.x;
+                    l[h] = t == 0 ? ml.y : 0.f;              // (the row's four lanes are added up at the end)
+                }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) at[e] = place(8 * h + 2 * t + e);
-#pragma unroll 2
-                for (int k = 0; k < parts; ++k) {
-                    const float2 ml = mine >= 0 ? __ldcg(&a.pre_ml[k * stride + mine]) : make_float2(-INFINITY, 0.f);
-                    const float f = weight(ml.x, m[h]);
-                    if (t == 0) l[h] += f * ml.y;            // (the row's four lanes are added up at the end)
-                    float fe[2];
-                    fe[0] = __shfl_sync(0xffffffffu, f, 8 * t);
-                    fe[1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+                for (int e = 0; e < 2; ++e) {
+                    const float seen = __shfl_sync(0xffffffffu, m[h], 8 * t + 4 * e);
+                    const int64_t at = place(8 * h + 2 * t + e);
+                    if (at < 0 || seen == -INFINITY) continue;           // (a prefix without a token that the row sees holds no values)
+                    const float *src = a.pre_o + at * D;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        if (at[e] < 0 || fe[e] == 0.f) continue;         // (a part without a token that the row sees holds no values)
-                        const float *src = a.pre_o + (k * stride + at[e]) * D;
-#pragma unroll
-                        for (int i = 0; i < MT; i += 2) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + Rows::vdim(g, i / 4) + 2 * (i % 4)));
-                            o[i][h][e] += fe[e] * x.x;
-                            o[i][h][2 + e] += fe[e] * x.y;
-                            o[i + 1][h][e] += fe[e] * x.z;
-                            o[i + 1][h][2 + e] += fe[e] * x.w;
-                        }
+                    for (int i = 0; i < MT; i += 2) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + Rows::vdim(g, i / 4) + 2 * (i % 4)));
+                        o[i][h][e] = x.x;
+                        o[i][h][2 + e] = x.y;
+                        o[i + 1][h][e] = x.z;
+                        o[i + 1][h][2 + e] = x.w;
                     }
                 }
             }

@@ -12,11 +12,11 @@ struct VtkPrefixGroup {
     int32_t splits, tiles;               // parts that its tiles are cut into, tiles of a part
     int32_t first, end;                  // requests
     int64_t items;                       // items of the groups in front
-    int32_t members;                     // requests with query rows that read the prefix here
-    int32_t pad;
+    int64_t rows;                        // rows (query tokens times query heads) of several parts in the groups in front
 };
 struct VtkPrefixPlan {
     int64_t items;                       // of all groups: (256 query rows, part, key head)
+    int64_t rows;                        // rows of several parts
     int32_t groups;
     int32_t query_tokens;                // of the call: parts are [splits][query_tokens][query heads]
 };
@@ -41,8 +41,8 @@ struct VtkAttnArgs {
     // shared prefixes only
     const VtkPrefixPlan *plan;
     const VtkPrefixGroup *groups;
-    const int2 *shared;                  // per request: entries of its prefix, parts
-    float2 *pre_ml;                      // per part and row: running maximum (exponents of two) and sum of the prefix ...
+    const int32_t *shared;               // per request: entries of its prefix
+    float2 *pre_ml;                      // per part and row: running maximum (exponents of two) and sum of the prefix, joined in part 0 ...
     float *pre_o;                        // ... and the sum of its weighted values
 };
 

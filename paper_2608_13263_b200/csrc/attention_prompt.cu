@@ -181,6 +181,7 @@ __device__ void next_prefix_item(const VtkAttnArgs &a, Item &out, uint32_t *tick
         it.first = (int)(left / g.splits) * 2 * AP_TILE;
         it.q0 = g.q0;
         it.len = g.len;
+        const int first_id = a.cache_ids.null() ? 0 : a.cache_ids[g.base], last_id = vtk_last_id(a, g.base, g.len);
         const int64_t rows = (int64_t)(g.q1 - g.q0) * a.group - it.first;
         it.rows = rows < 2 * AP_TILE ? (int)rows : 2 * AP_TILE;
         int pmin = INT32_MAX, pmax = -1;
@@ -202,10 +203,12 @@ __device__ void next_prefix_item(const VtkAttnArgs &a, Item &out, uint32_t *tick
         it.span.floor = vtk_floor(pmin, a.window);
         it.span.base = g.base;
         it.span.first = 0;
-        const int end = ids_up_to_warp(a, g.base, g.len, pmax);
-        it.span.lo = a.window > 0 ? ids_up_to_warp(a, g.base, g.len, (int64_t)pmin - a.window) : 0;
+        // (searches are rounds of loads one behind the other: the ends are looked at first)
+        const bool whole = last_id <= pmax, from_start = a.window == 0 || (int64_t)first_id > (int64_t)pmin - a.window;
+        const int end = whole ? g.len : ids_up_to_warp(a, g.base, g.len, pmax);
+        it.span.lo = from_start ? 0 : ids_up_to_warp(a, g.base, g.len, (int64_t)pmin - a.window);
         if (it.span.lo > end) it.span.lo = end;
-        it.span.n_sink = a.sinks > 0 ? ids_up_to_warp(a, g.base, it.span.lo, (int64_t)a.sinks - 1) : 0;
+        it.span.n_sink = a.sinks > 0 && it.span.lo > 0 ? ids_up_to_warp(a, g.base, it.span.lo < a.sinks ? it.span.lo : a.sinks, (int64_t)a.sinks - 1) : 0;
         it.span.n = it.span.n_sink + end - it.span.lo;
         const int all = (it.span.n + AP_TILE - 1) / AP_TILE;
         it.tile0 = it.part * g.tiles;
@@ -213,11 +216,12 @@ __device__ void next_prefix_item(const VtkAttnArgs &a, Item &out, uint32_t *tick
         // rows of one request that reads the prefix for itself
         int before = g.first, behind = g.end;
         const int t0 = it.q0 + it.first / a.group, t1 = it.q0 + (it.first + it.rows - 1) / a.group;
+        if (a.row_limit == INT32_MAX) behind = before;       // (there are none)
         while (behind - before > 1) {        // q_offsets[before] <= t0 < q_offsets[behind]
             const int mid = (before + behind) >> 1;
             if (a.q_offsets[mid] <= t0) before = mid; else behind = mid;
         }
-        if (t1 < a.q_offsets[before + 1] && ((int64_t)a.q_offsets[before + 1] - a.q_offsets[before]) * a.group > a.row_limit) {
+        if (behind > before && t1 < a.q_offsets[before + 1] && ((int64_t)a.q_offsets[before + 1] - a.q_offsets[before]) * a.group > a.row_limit) {
             it.part = -1;
             it.tiles = 0;
         }
@@ -564,52 +568,69 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
         each_item([&](const Item &it, int T, bool two) {
             if (T > 0) {
                 const int pt = tid - 256;
-                // queries, rows of both tiles
-                if (!FP4) {
-                    const int rows = two ? 2 * AP_TILE : AP_TILE;
-                    for (int i = pt; i < rows * PIECES; i += 128) {
-                        const int row = i / PIECES, piece = i % PIECES, at = it.first + row;
-                        const bool there = row < it.rows;
-                        const uint16_t *src = a.q;
-                        if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D + 8 * piece;
-                        cp_async16(vtk_smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
-                    }
-                    if (!stalled(it) || pt > 0) cp_arrive(&sh.q_full);
-                } else {
-                    for (int x = 0; x < (two ? 2 : 1); ++x) {
-                        const int row = x * AP_TILE + pt, at = it.first + row;
-                        const bool there = row < it.rows;
-                        const uint16_t *src = a.q;
-                        if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
-                        float up = 1.f, down = 1.f;
-                        if (Act::kind == VTOKEN_KV_BF16) {           // bf16 queries in half precision: see attention.cu
-                            float top = 0.f, v[8];
+                // queries, rows of both tiles (the rows of a prefix are fetched behind the first keys, which come from further away)
+                auto queries = [&]() {
+                    if (PREFIX && !FP4) {
+                        // PIECES threads a row; a division for each thread, the 32 rows of its warp by shuffles
+                        const int piece = pt % PIECES, row0 = pt / PIECES * PIECES;
+                        for (int x = 0; x < (two ? 2 : 1); ++x) {
+                            const int row = x * AP_TILE + pt, at = it.first + row;
+                            int64_t mine = -1;
+                            if (row < it.rows) mine = (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
+#pragma unroll
                             for (int i = 0; i < PIECES; ++i) {
-                                vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0), v);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+                                const int64_t from = __shfl_sync(0xffffffffu, mine, lane / PIECES * PIECES + i);
+                                cp_async16(vtk_smem_u32(sh.q[x]) + swizzled(row0 + i, piece), a.q + (from < 0 ? 0 : from) + 8 * piece, from >= 0);
                             }
-                            int e2 = (int)(__float_as_uint(top) >> 23) - 127;
-                            e2 = 14 - (e2 < -100 ? -100 : e2);
-                            up = __uint_as_float((uint32_t)(127 + e2) << 23);
-                            down = __uint_as_float((uint32_t)(127 - e2) << 23);
                         }
-                        sh.row_scale[x][pt] = down;
-                        for (int i = 0; i < PIECES; ++i) {
-                            uint4 w = there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0);
-                            if (Act::kind == VTOKEN_KV_BF16) {
-                                float v[8];
-                                vtk_unpack8<VtkBf16>(w, v);
+                        if (!stalled(it) || pt > 0) cp_arrive(&sh.q_full);
+                    } else if (!FP4) {
+                        const int rows = two ? 2 * AP_TILE : AP_TILE;
+                        for (int i = pt; i < rows * PIECES; i += 128) {
+                            const int row = i / PIECES, piece = i % PIECES, at = it.first + row;
+                            const bool there = row < it.rows;
+                            const uint16_t *src = a.q;
+                            if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D + 8 * piece;
+                            cp_async16(vtk_smem_u32(sh.q[row >> 7]) + swizzled(row & 127, piece), src, there);
+                        }
+                        if (!stalled(it) || pt > 0) cp_arrive(&sh.q_full);
+                    } else {
+                        for (int x = 0; x < (two ? 2 : 1); ++x) {
+                            const int row = x * AP_TILE + pt, at = it.first + row;
+                            const bool there = row < it.rows;
+                            const uint16_t *src = a.q;
+                            if (there) src += (it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
+                            float up = 1.f, down = 1.f;
+                            if (Act::kind == VTOKEN_KV_BF16) {           // bf16 queries in half precision: see attention.cu
+                                float top = 0.f, v[8];
+                                for (int i = 0; i < PIECES; ++i) {
+                                    vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0), v);
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) v[e] *= up;
-                                w = vtk_pack8<VtkFp16>(v);
+                                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+                                }
+                                int e2 = (int)(__float_as_uint(top) >> 23) - 127;
+                                e2 = 14 - (e2 < -100 ? -100 : e2);
+                                up = __uint_as_float((uint32_t)(127 + e2) << 23);
+                                down = __uint_as_float((uint32_t)(127 - e2) << 23);
                             }
-                            st_shared16(vtk_smem_u32(sh.q[x]) + swizzled(pt, i), w);
+                            sh.row_scale[x][pt] = down;
+                            for (int i = 0; i < PIECES; ++i) {
+                                uint4 w = there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+                                if (Act::kind == VTOKEN_KV_BF16) {
+                                    float v[8];
+                                    vtk_unpack8<VtkBf16>(w, v);
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) v[e] *= up;
+                                    w = vtk_pack8<VtkFp16>(v);
+                                }
+                                st_shared16(vtk_smem_u32(sh.q[x]) + swizzled(pt, i), w);
+                            }
                         }
+                        async_proxy_fence();
+                        if (!stalled(it) || pt > 0) vtk_mbar_arrive(&sh.q_full);
                     }
-                    async_proxy_fence();
-                    if (!stalled(it) || pt > 0) vtk_mbar_arrive(&sh.q_full);
-                }
+                };
+                if (!PREFIX) queries();
                 auto wait_meta = [&](int j) {                      // the slots of tile j
                     const uint32_t c = tile_count + j;
                     return vtk_mbar_wait(&sh.meta_full[c % AP_META], (c / AP_META) & 1, limit_ns, &sh.abort, item_count + 1);
@@ -649,6 +670,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     if (j == 0 || !FP4)
                         if (!wait_meta(j)) break;
                     if (FP4 && j == 0) fetch_rows(0, 0);
+                    if (PREFIX && FP4 && j == 0) queries();
                     if (!vtk_mbar_wait(&sh.kv_empty[stage_k], ((c0 / AP_STAGES) & 1) ^ 1, limit_ns, &sh.abort, item_count + 1)) break;
                     bool ok = true;
 #pragma unroll
@@ -676,6 +698,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             for (int i = 0; i < ROWS; ++i)
                                 cp_async16(dst + swizzled(row0 + i, piece), base + (int64_t)(sl[i] < 0 ? 0 : sl[i]) * a.row_bytes, sl[i] >= 0);
                             cp_arrive(&sh.kv_full[stage]);
+                            if (PREFIX && j == 0 && which == 0) queries();
                         } else {
                             if (which == 0) fetch_rows(1, j);
                             else if (j + 1 < T) fetch_rows(0, j + 1);

@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int AS_NT = 1024, AS_TILE = 128, AS_PAIR = 2 * AS_TILE, AS_MIN_TILES = 2, AS_GROUPS = 1024;
+constexpr int AS_NT = 1024, AS_TILE = 128, AS_PAIR = 2 * AS_TILE, AS_MIN_TILES = 2, AS_GROUPS = 1024, AS_SIZED = 64;
 
 struct Args {
     VtkAttnArgs a;
@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
 {
     const VtkAttnArgs &a = s.a;
     __shared__ int64_t warp_sum[2][AS_NT / 32];
-    __shared__ int edge[AS_GROUPS + 1], few_len[AS_GROUPS], few_readers[AS_GROUPS];
+    __shared__ int edge[AS_GROUPS + 1], few_len[AS_GROUPS], few_readers[AS_GROUPS], few_units[AS_SIZED], group_tiles[AS_SIZED];
     vtk_release_successor();
     vtk_wait_for_predecessor();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -104,13 +104,39 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
         x.splits = 0;
         x.rows = 0;
         work += x.len > 0 ? x.items * x.tiles : 0;
+        if (G <= AS_SIZED) {
+            few_units[g] = x.len > 0 ? (int)x.items : 0;
+            group_tiles[g] = x.tiles;
+        }
         s.groups[g] = x;
     }
     work = block_sum(work, warp_sum[0]);
     const int tokens = R > 0 ? vtk_clamp_offset(a.q_offsets[R], a.max_query_tokens) : 0;
     const int64_t most = tokens > 0 ? s.rows / ((int64_t)tokens * a.hq) : 1;      // parts that there is room for
+    // Tiles of a part.  A part costs about five tiles to start, and a CTA that gets one part more than the others is waited for: of sizes
+    // upwards of one that gives every CTA its share the one with the fewest (rounds of parts) x (size + 5).
     int64_t size = (work + s.ctas - 1) / s.ctas;
     size = size < AS_MIN_TILES ? AS_MIN_TILES : size;
+    if (G <= AS_SIZED) {
+        int64_t cost = INT64_MAX;
+        int64_t items = 0;
+        const int64_t mine = size / 4 + 1 + tid;
+        if (mine >= AS_MIN_TILES) {
+            for (int g = 0; g < G; ++g) items += few_units[g] * ((group_tiles[g] + mine - 1) / mine);
+            const int64_t rounds = (items + s.ctas - 1) / s.ctas;
+            cost = (rounds * (mine + 5)) << 32 | mine;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            const int64_t o = __shfl_xor_sync(0xffffffffu, cost, d);
+            cost = o < cost ? o : cost;
+        }
+        if (lane == 0) warp_sum[0][warp] = cost;
+        __syncthreads();
+        for (int w = 0; w < AS_NT / 32; ++w) cost = warp_sum[0][w] < cost ? warp_sum[0][w] : cost;
+        __syncthreads();
+        size = cost & 0xffffffff;
+    }
     int64_t items_before = 0, rows_before = 0;
     for (int g0 = 0; g0 < G; g0 += AS_NT) {
         const int g = g0 + tid;

@@ -4,37 +4,48 @@
 // itself, so there is nothing to join.  Bound by HBM: each visible K row is read once.
 //
 // All caches are cut into chunks of 16 to 128 tokens (fewer when there are few chunks), and every CTA takes an equal run of chunks.
-// Within a chunk a warp has a key head and tiles of 16 tokens: K fragments of mma.m16n8k16 come straight from the rows in HBM (8
-// dimensions of one token are the B fragment of two instructions, see attention.cu), two tiles ahead, and the accumulator's columns
-// are tokens, so that the sum over query rows is one over lanes.  The heads' sums of a token meet in shared memory, in the order of
-// the heads.
+// Within a chunk a warp has a key head and tiles of 16 tokens, copied several tiles ahead by cp.async into a ring of its own.  The
+// product is taken as S^T = K Q^T, mma.m16n8k16 with the 16 tokens as rows and 8 query rows as columns: no row of the instruction is
+// empty, a lane's accumulators belong to two tokens whose ids it holds, and the sum over query rows is one over four lanes.  (As
+// S = Q K^T, with half of the instruction empty, twelve shuffles a tile and K one tile ahead in registers, 512 requests took 428 us,
+// 256 over 4-bit rows 472.)  The order of the contracted dimension is free, so 8 dimensions of a token, 16 bytes, are the fragments
+// of two instructions, see attention.cu.  The heads' sums of a token meet in shared memory, in the order of the heads.
 #include "weights.cuh"
 
 namespace {
 
-constexpr int TW_NT = 256, TW_WARPS = TW_NT / 32, TW_CHUNK = 128, TW_CTAS = 2, TW_ROW_LIMIT = 32;
+constexpr int TW_NT = 256, TW_WARPS = TW_NT / 32, TW_CHUNK = 128, TW_CTAS = 2, TW_ROW_LIMIT = 32, TW_TILE = 16;
 
-// ---- K fragments of 16 tokens of a head: lane (g, t) takes of tokens g and 8 + g the dimensions kdim(t, j) .. + 7, j < D / 32 ----
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// ---- K rows of a tile: lane (g, t) takes of tokens g and 8 + g the dimensions kdim(t, j) .. + 7, j < D / 32 ----
 template <int D, typename Act>
 struct Keys16 {
     static constexpr bool FP4 = false;
     using Mma = Act;
+    static constexpr int PITCH = D * 2, STAGE = TW_TILE * PITCH, PIECES = D / 8, STAGES = D == 128 ? 3 : 5;
     static __device__ __forceinline__ int kdim(int t, int j) { return 32 * j + 8 * t; }
-    uint4 w[2][D / 32];
-    __device__ __forceinline__ void load(const VtkAttnArgs &a, int head, int t, int64_t s0, int64_t s1)
+    // slot: lane i < 16 holds that of token i, negative = zeros
+    static __device__ __forceinline__ void issue(uint32_t dst, const VtkAttnArgs &a, int head, int slot)
     {
+        const int lane = vtk_lane(), c = lane % PIECES, sub = lane / PIECES;
+        constexpr int PER = 32 / PIECES;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int64_t s = u ? s1 : s0;
-            const uint8_t *p = a.k_rows + (s < 0 ? 0 : s) * a.row_bytes + (head * D + 8 * t) * 2;
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) w[u][j] = s < 0 ? make_uint4(0, 0, 0, 0) : vtk_ldg16(p + 64 * j);
+        for (int i = 0; i < TW_TILE / PER; ++i) {
+            const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
+            cp_async16(dst + tok * PITCH + ((c ^ ((tok & 1) << 2)) << 4), a.k_rows + (s < 0 ? 0 : s) * a.row_bytes + head * (D * 2) + 16 * c, s >= 0);
         }
     }
-    __device__ __forceinline__ void get(int u, uint4 (&k)[D / 32]) const
+    static __device__ __forceinline__ void get(const uint8_t *at, int, int u, int g, int t, uint4 (&k)[D / 32])
     {
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) k[j] = w[u][j];
+        for (int j = 0; j < D / 32; ++j)
+            k[j] = *reinterpret_cast<const uint4 *>(at + (8 * u + g) * PITCH + (((4 * j + t) ^ ((g & 1) << 2)) << 4));
     }
 };
 
@@ -42,35 +53,34 @@ template <int D>
 struct Keys4 {
     static constexpr bool FP4 = true;
     using Mma = VtkFp16;
+    static constexpr int PITCH = D / 2, CODES = TW_TILE * PITCH, STAGE = CODES + TW_TILE * 16, PIECES = D / 32, STAGES = 8;
     static __device__ __forceinline__ int kdim(int t, int j) { return (D / 4) * t + 8 * j; }
-    uint32_t w[2][D / 32], sc[2];
-    __device__ __forceinline__ void load(const VtkAttnArgs &a, int head, int t, int64_t s0, int64_t s1)
+    static __device__ __forceinline__ void issue(uint32_t dst, const VtkAttnArgs &a, int head, int slot)
     {
+        const int lane = vtk_lane(), c = lane % PIECES, sub = lane / PIECES;
+        constexpr int PER = 32 / PIECES;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int64_t s = u ? s1 : s0;
-#pragma unroll
-            for (int j = 0; j < D / 32; ++j) w[u][j] = 0;
-            sc[u] = 0;
-            if (s < 0) continue;
-            const uint8_t *row = a.k_rows + s * a.row_bytes, *codes = row + head * (D / 2) + t * (D / 8);
-            const uint8_t *scales = row + a.hkv * (D / 2) + head * (D / 16) + t * (D / 64);
-            if (D == 128) {
-                const uint4 q = __ldg(reinterpret_cast<const uint4 *>(codes));
-                w[u][0] = q.x; w[u][1] = q.y; w[u][D / 32 - 2] = q.z; w[u][D / 32 - 1] = q.w;
-                sc[u] = __ldg(reinterpret_cast<const uint16_t *>(scales));
-            } else {
-                const uint2 q = __ldg(reinterpret_cast<const uint2 *>(codes));
-                w[u][0] = q.x; w[u][1] = q.y;
-                sc[u] = __ldg(scales);
-            }
+        for (int i = 0; i < TW_TILE / PER; ++i) {
+            const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
+            cp_async16(dst + tok * PITCH + 16 * c, a.k_rows + (s < 0 ? 0 : s) * a.row_bytes + head * PITCH + 16 * c, s >= 0);
         }
+        if (lane < TW_TILE)              // scales: the aligned 16 bytes that hold the head's
+            cp_async16(dst + CODES + lane * 16, a.k_rows + (slot < 0 ? 0 : slot) * a.row_bytes + a.hkv * PITCH + ((head * (D / 16)) & ~15), slot >= 0);
     }
-    __device__ __forceinline__ void get(int u, uint4 (&k)[D / 32]) const
+    static __device__ __forceinline__ void get(const uint8_t *at, int head, int u, int g, int t, uint4 (&k)[D / 32])
     {
-        const uint32_t two = vtk_scales_to_half2(sc[u]);
+        const uint8_t *codes = at + (8 * u + g) * PITCH + t * (D / 8), *sc = at + CODES + (8 * u + g) * 16 + ((head * (D / 16)) & 15);
+        uint32_t w[D / 32];
+        if (D == 128) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(codes);
+            w[0] = q.x; w[1] = q.y; w[D / 32 - 2] = q.z; w[D / 32 - 1] = q.w;
+        } else {
+            const uint2 q = *reinterpret_cast<const uint2 *>(codes);
+            w[0] = q.x; w[1] = q.y;
+        }
+        const uint32_t two = vtk_scales_to_half2(D == 128 ? *reinterpret_cast<const uint16_t *>(sc + 2 * t) : sc[t]);
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) k[j] = vtk_expand8(w[u][j], __byte_perm(two, 0, j < 2 ? 0x1010 : 0x3232));
+        for (int j = 0; j < D / 32; ++j) k[j] = vtk_expand8(w[j], __byte_perm(two, 0, j < 2 ? 0x1010 : 0x3232));
     }
 };
 
@@ -94,18 +104,23 @@ __device__ inline Known look_up(const VtkAttnArgs &a, int r, bool &clipped)
 
 __device__ __forceinline__ int64_t chunks_of(const Known &k, int chunk) { return k.qn > 0 ? ((int64_t)k.len + chunk - 1) / chunk : 0; }
 
+template <typename Keys>
 struct Shared {
-    int64_t prefix[TW_NT + 1];           // tokens, then chunks, in front of each thread's requests
+    alignas(128) uint8_t ring[TW_WARPS][Keys::STAGES][Keys::STAGE];
+    int ids[TW_WARPS][Keys::STAGES][TW_TILE];                // INT32_MAX: not there, or nobody sees it
+    int64_t prefix[TW_NT + 1];           // chunks in front of each thread's requests
     int64_t warp_sum[TW_WARPS];
     float part[2][TW_WARPS][TW_CHUNK];   // sums of a chunk's tokens over the rows of a warp's heads
 };
 
+// 8 RH query rows of a head as columns of the products: lane (g, t) holds the dimensions of rows g (and 8 + g), and what the columns
+// 2t, 2t + 1 (+ 8) need besides
 template <int D, typename Keys, typename Act, int RH>
-struct Rows {                            // 8 RH query rows of a head in registers: lane (g, t) holds rows g and 8 + g
+struct Rows {
     uint4 q[RH][D / 32];
-    int pos[RH], floor[RH], pmin, pmax;
-    float scale[RH], lse2[RH];
-    bool none[RH];                       // the row is not there, or it saw nothing: it adds nothing, whatever the keys hold
+    int pos[RH][2], floor[RH][2], pmin, pmax;
+    float scale[RH][2], lse2[RH][2];
+    bool none[RH][2];                    // the row is not there, or it saw nothing: it adds nothing, whatever the keys hold
     __device__ __forceinline__ void load(const VtkWeightsArgs &w, const Known &k, int rt, int head)
     {
         const VtkAttnArgs &a = w.at;
@@ -114,21 +129,25 @@ struct Rows {                            // 8 RH query rows of a head in registe
         pmax = -1;
 #pragma unroll
         for (int h = 0; h < RH; ++h) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int row = rt * 8 * RH + 8 * h + 2 * t + e;
+                const bool have = row < rows;
+                const int64_t at = k.q0 + (have ? row / a.group : 0);
+                const float l = have ? w.lse_in[at * a.hq + head * a.group + row % a.group] : -INFINITY;
+                pos[h][e] = have ? min(a.positions[at], INT32_MAX - 1) : -1;     // (INT32_MAX is the id of what is not there)
+                floor[h][e] = vtk_floor(pos[h][e], a.window);
+                none[h][e] = l == -INFINITY;
+                lse2[h][e] = l * 1.4426950408889634f;
+                scale[h][e] = a.scale_log2;
+                if (have) {
+                    pmin = pos[h][e] < pmin ? pos[h][e] : pmin;
+                    pmax = pos[h][e] > pmax ? pos[h][e] : pmax;
+                }
+            }
             const int row = rt * 8 * RH + 8 * h + g;
             const bool have = row < rows;
-            const int tok = have ? row / a.group : 0, qh = head * a.group + (have ? row % a.group : 0);
-            const int64_t at = k.q0 + tok;
-            pos[h] = have ? min(a.positions[at], INT32_MAX - 1) : -1;       // (INT32_MAX is the id of what is not there)
-            floor[h] = vtk_floor(pos[h], a.window);
-            const float l = have ? w.lse_in[at * a.hq + qh] : INFINITY;
-            none[h] = !have || l == -INFINITY;
-            lse2[h] = l * 1.4426950408889634f;
-            scale[h] = a.scale_log2;
-            if (have) {
-                pmin = pos[h] < pmin ? pos[h] : pmin;
-                pmax = pos[h] > pmax ? pos[h] : pmax;
-            }
-            const uint16_t *p = a.q + at * a.q_stride + (int64_t)qh * D;
+            const uint16_t *p = a.q + (k.q0 + (have ? row / a.group : 0)) * a.q_stride + (int64_t)(head * a.group + (have ? row % a.group : 0)) * D;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) q[h][j] = have ? *reinterpret_cast<const uint4 *>(p + Keys::kdim(t, j)) : make_uint4(0, 0, 0, 0);
             if (Keys::FP4 && Act::kind == VTOKEN_KV_BF16) {          // bf16 queries in half precision: see attention.cu
@@ -143,8 +162,9 @@ struct Rows {                            // 8 RH query rows of a head in registe
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 int e2 = (int)(__float_as_uint(top) >> 23) - 127;
                 e2 = 14 - (e2 < -100 ? -100 : e2);
-                const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
-                scale[h] *= __uint_as_float((uint32_t)(127 - e2) << 23);
+                const float up = __uint_as_float((uint32_t)(127 + e2) << 23), down = __uint_as_float((uint32_t)(127 - e2) << 23);
+                scale[h][0] *= __shfl_sync(0xffffffffu, down, 8 * t);
+                scale[h][1] *= __shfl_sync(0xffffffffu, down, 8 * t + 4);
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) {
                     vtk_unpack8<VtkBf16>(q[h][j], x);
@@ -159,13 +179,15 @@ struct Rows {                            // 8 RH query rows of a head in registe
     }
 };
 
-// RH: 8-row halves of the instruction that are used
+// RH: columns of 8 query rows at a time
 template <int D, typename Keys, typename Act, int RH>
 __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __grid_constant__ VtkWeightsArgs w)
 {
     using Mma = typename Keys::Mma;
+    constexpr int ST = Keys::STAGES;
     const VtkAttnArgs &a = w.at;
-    __shared__ Shared sh;
+    extern __shared__ __align__(128) uint8_t raw[];
+    Shared<Keys> &sh = *reinterpret_cast<Shared<Keys> *>(raw);
     vtk_release_successor();
     vtk_wait_for_predecessor();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -194,8 +216,10 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
     };
     count(chunk, true);
     if (clipped && blockIdx.x == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
-    while (chunk > 16 && sh.prefix[TW_NT] < (int64_t)gridDim.x * 2) {
-        chunk /= 2;
+    const int64_t enough = (int64_t)gridDim.x * 2, some = sh.prefix[TW_NT];
+    if (some < enough) {
+        while (chunk > TW_TILE && some * (TW_CHUNK / chunk) < enough) chunk /= 2;
+        __syncthreads();
         count(chunk, false);
     }
     const int64_t W = sh.prefix[TW_NT], per = W / gridDim.x, more = W - per * gridDim.x;
@@ -217,136 +241,159 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
         if (left < n) break;
         left -= n;
     }
-    int at = (int)left * chunk;
+    int at0 = (int)left * chunk;
 
     // ---- warps: heads side by side, and tiles of 16 tokens ----
     int heads = 1;
     while (heads < TW_WARPS && heads < a.hkv) heads <<= 1;
     const int lanes = TW_WARPS / heads, hl = warp / lanes, tw = warp % lanes, rounds = (a.hkv + heads - 1) / heads;
+    const int turns = chunk / TW_TILE > lanes ? chunk / TW_TILE / lanes : 1;         // tiles of a warp in a chunk, for each of its heads
+    const uint32_t ring = vtk_smem_u32(sh.ring[warp]);
     Rows<D, Keys, Act, RH> q;
-    int loaded_r = -1, loaded_head = -1, buffer = 0;
     bool bad_slot = false, bad_id = false;
-    for (; c0 < c1; ++c0, buffer ^= 1) {
-        const int n = k.len - at < chunk ? k.len - at : chunk, tiles = (n + 15) / 16;
+    int buffer = 0;
+    // ---- runs of chunks in one request; the ring is filled across its chunks ----
+    while (c0 < c1) {
+        const int64_t here = chunks_of(k, chunk) - at0 / chunk;
+        const int chunks = (int)(here < c1 - c0 ? here : c1 - c0);
+        const int end = k.len - at0 > (int64_t)chunks * chunk ? at0 + chunks * chunk : k.len;
         const int row_tiles = (k.qn * a.group + 8 * RH - 1) / (8 * RH);
-        float *part = sh.part[buffer][warp];
-        for (int round = 0; round < rounds; ++round) {
-            const int head = round * heads + hl;
-            if (head >= a.hkv) continue;
-            if (loaded_r != r || loaded_head != head) {
-                q.load(w, k, 0, head);
-                loaded_r = r;
-                loaded_head = head;
+        int pmin = INT32_MAX, pmax = -1;                     // of all rows
+        for (int i = lane; i < k.qn; i += 32) {
+            const int p = min(a.positions[k.q0 + i], INT32_MAX - 1);
+            pmin = p < pmin ? p : pmin;
+            pmax = p > pmax ? p : pmax;
+        }
+        pmin = __reduce_min_sync(0xffffffffu, pmin);
+        pmax = __reduce_max_sync(0xffffffffu, pmax);
+        const int floor_min = vtk_floor(pmin, a.window);
+        struct Place {                                       // the warp's next tile
+            int c, round, turn;
+        };
+        auto advance = [&](Place &p) {
+            if (++p.turn < turns) return;
+            p.turn = 0;
+            if (++p.round < rounds) return;
+            p.round = 0;
+            ++p.c;
+        };
+        Place get = {0, 0, 0};
+        int issued = 0;
+        struct Next { int slot, id, head; bool more; };
+        auto look = [&]() {                                  // slots and ids of a tile's tokens, a step ahead of its copies
+            Next n = {-1, INT32_MAX, get.round * heads + hl, get.c < chunks};
+            const int tile = get.turn * lanes + tw, i = at0 + get.c * chunk + tile * TW_TILE + lane;
+            if (n.more && lane < TW_TILE && tile * TW_TILE < chunk && i < end && n.head < a.hkv) {
+                n.slot = a.cache_slots[k.base + i];
+                n.id = a.cache_ids.null() ? i : a.cache_ids[k.base + i];
             }
-            // slots of a tile's tokens two tiles ahead, their keys one ahead
-            struct Tokens { int id[2], slot[2]; };
-            auto look = [&](int tile) {
-                Tokens x;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int i = tile * 16 + 8 * u + g;
-                    x.id[u] = INT32_MAX;
-                    x.slot[u] = -1;
-                    if (i < n) {
-                        x.id[u] = a.cache_ids.null() ? at + i : a.cache_ids[k.base + at + i];
-                        x.slot[u] = a.cache_slots[k.base + at + i];
-                    }
+            advance(get);
+            return n;
+        };
+        auto issue = [&](Next n) {
+            if (n.more) {
+                if ((int64_t)n.slot >= a.slots_per_layer) {
+                    bad_slot = true;
+                    n.slot = -1;
                 }
-                return x;
-            };
-            auto fetch = [&](Tokens &x, Keys &keys) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    if ((int64_t)x.slot[u] >= a.slots_per_layer) {
-                        bad_slot = true;
-                        x.slot[u] = -1;
-                    }
-                    // (with more row tiles than one the rows' span is not known here)
-                    if (row_tiles == 1 && !vtk_sees(x.id[u], q.pmax, vtk_floor(q.pmin, a.window), a.sinks)) x.slot[u] = -1;
+                if (n.slot < 0 || !vtk_sees(n.id, pmax, floor_min, a.sinks)) {
+                    n.slot = -1;
+                    n.id = INT32_MAX;
                 }
-                keys.load(a, head, t, x.slot[0], x.slot[1]);
-            };
-            Tokens now = look(tw), next = look(tw + lanes);
-            Keys keys, keys_next;
-            fetch(now, keys);
-            for (int tile = tw; tile < tiles; tile += lanes) {
-                const Tokens after = look(tile + 2 * lanes);
-                fetch(next, keys_next);
-                float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};          // of tokens 8 u + 2 t + e, over rows g (and 8 + g)
-                if (__any_sync(0xffffffffu, now.slot[0] >= 0 || now.slot[1] >= 0)) {
-                    for (int rt = 0; rt < row_tiles; ++rt) {
-                        if (row_tiles > 1) q.load(w, k, rt, head);
-                        const bool full = __all_sync(0xffffffffu, now.slot[0] >= 0 && now.slot[1] >= 0 &&
-                                                     vtk_sees(now.id[0], q.pmin, vtk_floor(q.pmax, a.window), a.sinks) &&
-                                                     vtk_sees(now.id[1], q.pmin, vtk_floor(q.pmax, a.window), a.sinks));
+                const int stage = issued % ST;
+                if (lane < TW_TILE) sh.ids[warp][stage][lane] = n.id;
+                if (__any_sync(0xffffffffu, n.slot >= 0)) Keys::issue(ring + stage * Keys::STAGE, a, n.head, n.slot);
+                ++issued;
+            }
+            cp_commit();
+        };
+        Next next;
+        {
+            Next first[ST - 1];
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            float s[4] = {0.f, 0.f, 0.f, 0.f};
-                            uint4 kf[D / 32];
-                            keys.get(u, kf);
+            for (int i = 0; i < ST - 1; ++i) first[i] = look();
+            next = look();
 #pragma unroll
-                            for (int j = 0; j < D / 32; ++j) {
-                                vtk_mma<Mma>(s, q.q[0][j].x, RH == 2 ? q.q[RH - 1][j].x : 0u, q.q[0][j].y, RH == 2 ? q.q[RH - 1][j].y : 0u, kf[j].x, kf[j].y);
-                                vtk_mma<Mma>(s, q.q[0][j].z, RH == 2 ? q.q[RH - 1][j].z : 0u, q.q[0][j].w, RH == 2 ? q.q[RH - 1][j].w : 0u, kf[j].z, kf[j].w);
-                            }
-                            int id[2] = {0, 0}, slot[2] = {0, 0};
-                            if (!full) {
+            for (int i = 0; i < ST - 1; ++i) issue(first[i]);
+        }
+        if (rounds == 1 && row_tiles == 1 && hl < a.hkv) q.load(w, k, 0, hl);
+        int used = 0;
+        for (int c = 0; c < chunks; ++c, buffer ^= 1) {
+            const int at = at0 + c * chunk, n = end - at < chunk ? end - at : chunk;
+            float *part = sh.part[buffer][warp];
+            for (int round = 0; round < rounds; ++round) {
+                const int head = round * heads + hl;
+                if (rounds > 1 && row_tiles == 1 && head < a.hkv) q.load(w, k, 0, head);
+                for (int turn = 0; turn < turns; ++turn, ++used) {
+                    cp_wait<ST - 2>();
+                    __syncwarp();
+                    issue(next);
+                    next = look();
+                    const int tile = turn * lanes + tw;
+                    if (head >= a.hkv || tile * TW_TILE >= n) continue;
+                    const int stage = used % ST, id[2] = {sh.ids[warp][stage][g], sh.ids[warp][stage][8 + g]};
+                    float sum[2] = {0.f, 0.f};               // of tokens g and 8 + g, over columns 2t and 2t + 1 (+ 8)
+                    if (__any_sync(0xffffffffu, id[0] != INT32_MAX || id[1] != INT32_MAX)) {
+                        uint4 kf[2][D / 32];
 #pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    id[e] = __shfl_sync(0xffffffffu, now.id[u], 4 * (2 * t + e));
-                                    slot[e] = __shfl_sync(0xffffffffu, now.slot[u], 4 * (2 * t + e));
+                        for (int u = 0; u < 2; ++u) Keys::get(sh.ring[warp][stage], head, u, g, t, kf[u]);
+                        for (int rt = 0; rt < row_tiles; ++rt) {
+                            if (row_tiles > 1) q.load(w, k, rt, head);
+                            const int floor_max = vtk_floor(q.pmax, a.window);
+                            const bool full = __all_sync(0xffffffffu, vtk_sees(id[0], q.pmin, floor_max, a.sinks) && vtk_sees(id[1], q.pmin, floor_max, a.sinks));
+#pragma unroll
+                            for (int h = 0; h < RH; ++h) {
+                                float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                                for (int j = 0; j < D / 32; ++j) {
+                                    vtk_mma<Mma>(s, kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, q.q[h][j].x, q.q[h][j].y);
+                                    vtk_mma<Mma>(s, kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, q.q[h][j].z, q.q[h][j].w);
                                 }
+#pragma unroll
+                                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e) {
+                                        float y = vtk_exp2(fmaf(s[2 * u + e], q.scale[h][e], -q.lse2[h][e]));
+                                        if (q.none[h][e]) y = 0.f;
+                                        if (!full && !vtk_sees(id[u], q.pos[h][e], q.floor[h][e], a.sinks)) y = 0.f;
+                                        sum[u] += y;
+                                    }
                             }
-#pragma unroll
-                            for (int h = 0; h < RH; ++h)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    float y = vtk_exp2(fmaf(s[2 * h + e], q.scale[h], -q.lse2[h]));
-                                    if (q.none[h]) y = 0.f;
-                                    if (!full && !(slot[e] >= 0 && vtk_sees(id[e], q.pos[h], q.floor[h], a.sinks))) y = 0.f;
-                                    sum[u][e] += y;
-                                }
                         }
                     }
-                    if (row_tiles > 1) loaded_head = -1;
-                }
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float y = sum[u][e];
-                        y += __shfl_xor_sync(0xffffffffu, y, 4);
-                        y += __shfl_xor_sync(0xffffffffu, y, 8);
-                        y += __shfl_xor_sync(0xffffffffu, y, 16);
-                        if (g == 0) {
-                            float *p = part + tile * 16 + 8 * u + 2 * t + e;
-                            *p = round == 0 ? y : *p + y;
-                        }
+                    for (int u = 0; u < 2; ++u) {
+                        sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
+                        sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
                     }
-                now = next;
-                keys = keys_next;
-                next = after;
+                    if (t < 2) {
+                        float *p = part + tile * TW_TILE + 8 * t + g;
+                        const float y = t == 0 ? sum[0] : sum[1];
+                        *p = round == 0 ? y : *p + y;
+                    }
+                }
+            }
+            __syncthreads();                                 // (the next chunk's sums go to the other buffer)
+            if (tid < n) {
+                const int id = a.cache_ids.null() ? at + tid : a.cache_ids[k.base + at + tid];
+                if (id >= 0 && id < k.range) {
+                    const int lane_of = tid / TW_TILE % lanes;
+                    float y = 0.f;
+                    for (int h = 0; h < heads && h < a.hkv; ++h) y += sh.part[buffer][h * lanes + lane_of][tid];
+                    if (!w.prev.null()) y = fmaf(w.decay, w.prev[k.base + id], y);
+                    w.scores[k.base + id] = y;
+                } else {
+                    bad_id = true;
+                }
             }
         }
-        __syncthreads();                                     // (the next chunk's sums go to the other buffer)
-        if (tid < n) {
-            const int id = a.cache_ids.null() ? at + tid : a.cache_ids[k.base + at + tid];
-            if (id >= 0 && id < k.range) {
-                const int lane_of = tid / 16 % lanes;
-                float y = 0.f;
-                for (int h = 0; h < heads && h < a.hkv; ++h) y += sh.part[buffer][h * lanes + lane_of][tid];
-                if (!w.prev.null()) y = fmaf(w.decay, w.prev[k.base + id], y);
-                w.scores[k.base + id] = y;
-            } else {
-                bad_id = true;
-            }
-        }
-        if (k.len - at > chunk) {
-            at += chunk;
-        } else if (c0 + 1 < c1) {
+        cp_wait<0>();
+        __syncwarp();
+        c0 += chunks;
+        if (c0 < c1) {
             bool c = false;
             do k = look_up(a, ++r, c); while (chunks_of(k, chunk) == 0);
-            at = 0;
+            at0 = 0;
         }
     }
     if (bad_slot) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
@@ -357,8 +404,12 @@ template <int D, typename Keys, typename Act>
 int launch(vtoken_ctx *ctx, const VtkWeightsArgs &w, bool wide, cudaStream_t st)
 {
     const dim3 grid(ctx->num_sms * TW_CTAS), block(TW_NT);
-    VTK_CUDA(ctx, wide ? vtk_launch_dependent(ctx, token_weights_kernel<D, Keys, Act, 2>, grid, block, 0, st, w)
-                       : vtk_launch_dependent(ctx, token_weights_kernel<D, Keys, Act, 1>, grid, block, 0, st, w));
+    constexpr int smem = (int)sizeof(Shared<Keys>);
+    static_assert(TW_CTAS * (smem + 1024) <= 233472, "shared memory of an SM");
+    static std::atomic<int> allowed[2] = {{-1}, {-1}};       // the device that knows of the kernels' shared memory
+    auto kernel = wide ? token_weights_kernel<D, Keys, Act, 2> : token_weights_kernel<D, Keys, Act, 1>;
+    VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed[wide], (const void *)kernel, smem));
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, grid, block, smem, st, w));
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
 }

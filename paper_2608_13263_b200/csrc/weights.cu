@@ -4,7 +4,7 @@
 // itself, so there is nothing to join.  Bound by HBM: each visible K row is read once.
 //
 // All caches are cut into chunks of 16 to 128 tokens (fewer when there are few chunks), and every CTA takes an equal run of chunks.
-// Within a chunk a warp has a key head and tiles of 16 tokens, copied several tiles ahead by cp.async into a ring of its own.  The
+// Within a chunk a warp has a key head and tiles of 16 tokens (32 over 4-bit rows, where instructions count), copied several tiles ahead by cp.async into a ring of its own.  The
 // product is taken as S^T = K Q^T, mma.m16n8k16 with the 16 tokens as rows and 8 query rows as columns: no row of the instruction is
 // empty, a lane's accumulators belong to two tokens whose ids it holds, and the sum over query rows is one over four lanes.  (As
 // S = Q K^T, with half of the instruction empty, twelve shuffles a tile and K one tile ahead in registers, 512 requests took 428 us,
@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int TW_NT = 256, TW_WARPS = TW_NT / 32, TW_CHUNK = 128, TW_CTAS = 2, TW_ROW_LIMIT = 32, TW_TILE = 16;
+constexpr int TW_NT = 256, TW_WARPS = TW_NT / 32, TW_CHUNK = 128, TW_CTAS = 2, TW_ROW_LIMIT = 32;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there)
 {
@@ -28,17 +28,19 @@ template <int D, typename Act>
 struct Keys16 {
     static constexpr bool FP4 = false;
     using Mma = Act;
-    static constexpr int PITCH = D * 2, STAGE = TW_TILE * PITCH, PIECES = D / 8, STAGES = D == 128 ? 3 : 5;
+    static constexpr int TILE = 16, PITCH = D * 2, STAGE = TILE * PITCH, PIECES = D / 8, STAGES = D == 128 ? 3 : 5;
     static __device__ __forceinline__ int kdim(int t, int j) { return 32 * j + 8 * t; }
-    // slot: lane i < 16 holds that of token i, negative = zeros
+    // slot: lane i < TILE holds that of token i, negative = zeros
     static __device__ __forceinline__ void issue(uint32_t dst, const VtkAttnArgs &a, int head, int slot)
     {
         const int lane = vtk_lane(), c = lane % PIECES, sub = lane / PIECES;
+        const uint32_t row_bytes = (uint32_t)a.row_bytes;
+        const uint8_t *rows = a.k_rows + (head * (D * 2) + 16 * c);
         constexpr int PER = 32 / PIECES;
 #pragma unroll
-        for (int i = 0; i < TW_TILE / PER; ++i) {
+        for (int i = 0; i < TILE / PER; ++i) {
             const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
-            cp_async16(dst + tok * PITCH + ((c ^ ((tok & 1) << 2)) << 4), a.k_rows + (s < 0 ? 0 : s) * a.row_bytes + head * (D * 2) + 16 * c, s >= 0);
+            cp_async16(dst + tok * PITCH + ((c ^ ((tok & 1) << 2)) << 4), rows + (uint64_t)(uint32_t)(s < 0 ? 0 : s) * row_bytes, s >= 0);
         }
     }
     static __device__ __forceinline__ void get(const uint8_t *at, int, int u, int g, int t, uint4 (&k)[D / 32])
@@ -53,19 +55,21 @@ template <int D>
 struct Keys4 {
     static constexpr bool FP4 = true;
     using Mma = VtkFp16;
-    static constexpr int PITCH = D / 2, CODES = TW_TILE * PITCH, STAGE = CODES + TW_TILE * 16, PIECES = D / 32, STAGES = 8;
+    static constexpr int TILE = 32, PITCH = D / 2, CODES = TILE * PITCH, STAGE = CODES + TILE * 16, PIECES = D / 32, STAGES = 4;
     static __device__ __forceinline__ int kdim(int t, int j) { return (D / 4) * t + 8 * j; }
     static __device__ __forceinline__ void issue(uint32_t dst, const VtkAttnArgs &a, int head, int slot)
     {
         const int lane = vtk_lane(), c = lane % PIECES, sub = lane / PIECES;
+        const uint32_t row_bytes = (uint32_t)a.row_bytes;
+        const uint8_t *rows = a.k_rows + (head * PITCH + 16 * c), *scales = a.k_rows + (a.hkv * PITCH + ((head * (D / 16)) & ~15));
         constexpr int PER = 32 / PIECES;
 #pragma unroll
-        for (int i = 0; i < TW_TILE / PER; ++i) {
+        for (int i = 0; i < TILE / PER; ++i) {
             const int tok = i * PER + sub, s = __shfl_sync(0xffffffffu, slot, tok);
-            cp_async16(dst + tok * PITCH + 16 * c, a.k_rows + (s < 0 ? 0 : s) * a.row_bytes + head * PITCH + 16 * c, s >= 0);
+            cp_async16(dst + tok * PITCH + 16 * c, rows + (uint64_t)(uint32_t)(s < 0 ? 0 : s) * row_bytes, s >= 0);
         }
-        if (lane < TW_TILE)              // scales: the aligned 16 bytes that hold the head's
-            cp_async16(dst + CODES + lane * 16, a.k_rows + (slot < 0 ? 0 : slot) * a.row_bytes + a.hkv * PITCH + ((head * (D / 16)) & ~15), slot >= 0);
+        // scales: the aligned 16 bytes that hold the head's
+        cp_async16(dst + CODES + lane * 16, scales + (uint64_t)(uint32_t)(slot < 0 ? 0 : slot) * row_bytes, slot >= 0);
     }
     static __device__ __forceinline__ void get(const uint8_t *at, int head, int u, int g, int t, uint4 (&k)[D / 32])
     {
@@ -107,7 +111,7 @@ __device__ __forceinline__ int64_t chunks_of(const Known &k, int chunk) { return
 template <typename Keys>
 struct Shared {
     alignas(128) uint8_t ring[TW_WARPS][Keys::STAGES][Keys::STAGE];
-    int ids[TW_WARPS][Keys::STAGES][TW_TILE];                // INT32_MAX: not there, or nobody sees it
+    int ids[TW_WARPS][Keys::STAGES][Keys::TILE];                // INT32_MAX: not there, or nobody sees it
     int64_t prefix[TW_NT + 1];           // chunks in front of each thread's requests
     int64_t warp_sum[TW_WARPS];
     float part[2][TW_WARPS][TW_CHUNK];   // sums of a chunk's tokens over the rows of a warp's heads
@@ -118,13 +122,14 @@ struct Shared {
 template <int D, typename Keys, typename Act, int RH>
 struct Rows {
     uint4 q[RH][D / 32];
-    int pos[RH][2], floor[RH][2], pmin, pmax;
+    int pos[RH][2], pmin, pmax, rows;    // rows: of these columns, at most 8 RH
     float scale[RH][2], lse2[RH][2];
     bool none[RH][2];                    // the row is not there, or it saw nothing: it adds nothing, whatever the keys hold
     __device__ __forceinline__ void load(const VtkWeightsArgs &w, const Known &k, int rt, int head)
     {
         const VtkAttnArgs &a = w.at;
-        const int lane = vtk_lane(), g = lane >> 2, t = lane & 3, rows = k.qn * a.group;
+        const int lane = vtk_lane(), g = lane >> 2, t = lane & 3, all = k.qn * a.group;
+        rows = all - rt * 8 * RH;
         pmin = INT32_MAX;
         pmax = -1;
 #pragma unroll
@@ -132,11 +137,10 @@ struct Rows {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int row = rt * 8 * RH + 8 * h + 2 * t + e;
-                const bool have = row < rows;
+                const bool have = row < all;
                 const int64_t at = k.q0 + (have ? row / a.group : 0);
                 const float l = have ? w.lse_in[at * a.hq + head * a.group + row % a.group] : -INFINITY;
                 pos[h][e] = have ? min(a.positions[at], INT32_MAX - 1) : -1;     // (INT32_MAX is the id of what is not there)
-                floor[h][e] = vtk_floor(pos[h][e], a.window);
                 none[h][e] = l == -INFINITY;
                 lse2[h][e] = l * 1.4426950408889634f;
                 scale[h][e] = a.scale_log2;
@@ -146,7 +150,7 @@ struct Rows {
                 }
             }
             const int row = rt * 8 * RH + 8 * h + g;
-            const bool have = row < rows;
+            const bool have = row < all;
             const uint16_t *p = a.q + (k.q0 + (have ? row / a.group : 0)) * a.q_stride + (int64_t)(head * a.group + (have ? row % a.group : 0)) * D;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) q[h][j] = have ? *reinterpret_cast<const uint4 *>(p + Keys::kdim(t, j)) : make_uint4(0, 0, 0, 0);
@@ -184,7 +188,7 @@ template <int D, typename Keys, typename Act, int RH>
 __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __grid_constant__ VtkWeightsArgs w)
 {
     using Mma = typename Keys::Mma;
-    constexpr int ST = Keys::STAGES;
+    constexpr int ST = Keys::STAGES, TILE = Keys::TILE;
     const VtkAttnArgs &a = w.at;
     extern __shared__ __align__(128) uint8_t raw[];
     Shared<Keys> &sh = *reinterpret_cast<Shared<Keys> *>(raw);
@@ -218,7 +222,7 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
     if (clipped && blockIdx.x == 0) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_CAPACITY);
     const int64_t enough = (int64_t)gridDim.x * 2, some = sh.prefix[TW_NT];
     if (some < enough) {
-        while (chunk > TW_TILE && some * (TW_CHUNK / chunk) < enough) chunk /= 2;
+        while (chunk > TILE && some * (TW_CHUNK / chunk) < enough) chunk /= 2;
         __syncthreads();
         count(chunk, false);
     }
@@ -247,7 +251,7 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
     int heads = 1;
     while (heads < TW_WARPS && heads < a.hkv) heads <<= 1;
     const int lanes = TW_WARPS / heads, hl = warp / lanes, tw = warp % lanes, rounds = (a.hkv + heads - 1) / heads;
-    const int turns = chunk / TW_TILE > lanes ? chunk / TW_TILE / lanes : 1;         // tiles of a warp in a chunk, for each of its heads
+    const int turns = chunk / TILE > lanes ? chunk / TILE / lanes : 1;         // tiles of a warp in a chunk, for each of its heads
     const uint32_t ring = vtk_smem_u32(sh.ring[warp]);
     Rows<D, Keys, Act, RH> q;
     bool bad_slot = false, bad_id = false;
@@ -282,8 +286,8 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
         struct Next { int slot, id, head; bool more; };
         auto look = [&]() {                                  // slots and ids of a tile's tokens, a step ahead of its copies
             Next n = {-1, INT32_MAX, get.round * heads + hl, get.c < chunks};
-            const int tile = get.turn * lanes + tw, i = at0 + get.c * chunk + tile * TW_TILE + lane;
-            if (n.more && lane < TW_TILE && tile * TW_TILE < chunk && i < end && n.head < a.hkv) {
+            const int tile = get.turn * lanes + tw, i = at0 + get.c * chunk + tile * TILE + lane;
+            if (n.more && lane < TILE && tile * TILE < chunk && i < end && n.head < a.hkv) {
                 n.slot = a.cache_slots[k.base + i];
                 n.id = a.cache_ids.null() ? i : a.cache_ids[k.base + i];
             }
@@ -301,7 +305,7 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
                     n.id = INT32_MAX;
                 }
                 const int stage = issued % ST;
-                if (lane < TW_TILE) sh.ids[warp][stage][lane] = n.id;
+                if (lane < TILE) sh.ids[warp][stage][lane] = n.id;
                 if (__any_sync(0xffffffffu, n.slot >= 0)) Keys::issue(ring + stage * Keys::STAGE, a, n.head, n.slot);
                 ++issued;
             }
@@ -330,46 +334,58 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
                     issue(next);
                     next = look();
                     const int tile = turn * lanes + tw;
-                    if (head >= a.hkv || tile * TW_TILE >= n) continue;
-                    const int stage = used % ST, id[2] = {sh.ids[warp][stage][g], sh.ids[warp][stage][8 + g]};
-                    float sum[2] = {0.f, 0.f};               // of tokens g and 8 + g, over columns 2t and 2t + 1 (+ 8)
-                    if (__any_sync(0xffffffffu, id[0] != INT32_MAX || id[1] != INT32_MAX)) {
-                        uint4 kf[2][D / 32];
+                    if (head >= a.hkv || tile * TILE >= n) continue;
+                    const int stage = used % ST;
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) Keys::get(sh.ring[warp][stage], head, u, g, t, kf[u]);
-                        for (int rt = 0; rt < row_tiles; ++rt) {
-                            if (row_tiles > 1) q.load(w, k, rt, head);
-                            const int floor_max = vtk_floor(q.pmax, a.window);
-                            const bool full = __all_sync(0xffffffffu, vtk_sees(id[0], q.pmin, floor_max, a.sinks) && vtk_sees(id[1], q.pmin, floor_max, a.sinks));
+                    for (int b = 0; b < TILE / 16; ++b) {
+                        const int id[2] = {sh.ids[warp][stage][16 * b + g], sh.ids[warp][stage][16 * b + 8 + g]};
+                        float sum[2] = {0.f, 0.f};           // of tokens g and 8 + g, over columns 2t and 2t + 1 (+ 8)
+                        if (__any_sync(0xffffffffu, id[0] != INT32_MAX || id[1] != INT32_MAX)) {
+                            uint4 kf[2][D / 32];
 #pragma unroll
-                            for (int h = 0; h < RH; ++h) {
-                                float s[4] = {0.f, 0.f, 0.f, 0.f};
+                            for (int u = 0; u < 2; ++u) Keys::get(sh.ring[warp][stage], head, 2 * b + u, g, t, kf[u]);
+                            for (int rt = 0; rt < row_tiles; ++rt) {
+                                if (row_tiles > 1) q.load(w, k, rt, head);
+                                const int floor_max = vtk_floor(q.pmax, a.window);
+                                const bool full = __all_sync(0xffffffffu, vtk_sees(id[0], q.pmin, floor_max, a.sinks) && vtk_sees(id[1], q.pmin, floor_max, a.sinks));
 #pragma unroll
-                                for (int j = 0; j < D / 32; ++j) {
-                                    vtk_mma<Mma>(s, kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, q.q[h][j].x, q.q[h][j].y);
-                                    vtk_mma<Mma>(s, kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, q.q[h][j].z, q.q[h][j].w);
-                                }
+                                for (int h = 0; h < RH; ++h) {
+                                    if (h == 1 && q.rows <= 8) break;    // (uniform)
+                                    float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                                    for (int e = 0; e < 2; ++e) {
-                                        float y = vtk_exp2(fmaf(s[2 * u + e], q.scale[h][e], -q.lse2[h][e]));
-                                        if (q.none[h][e]) y = 0.f;
-                                        if (!full && !vtk_sees(id[u], q.pos[h][e], q.floor[h][e], a.sinks)) y = 0.f;
-                                        sum[u] += y;
+                                    for (int j = 0; j < D / 32; ++j) {
+                                        vtk_mma<Mma>(s, kf[0][j].x, kf[1][j].x, kf[0][j].y, kf[1][j].y, q.q[h][j].x, q.q[h][j].y);
+                                        vtk_mma<Mma>(s, kf[0][j].z, kf[1][j].z, kf[0][j].w, kf[1][j].w, q.q[h][j].z, q.q[h][j].w);
                                     }
+                                    float y[2][2];
+#pragma unroll
+                                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e) {
+                                            y[u][e] = vtk_exp2(fmaf(s[2 * u + e], q.scale[h][e], -q.lse2[h][e]));
+                                            if (q.none[h][e]) y[u][e] = 0.f;
+                                        }
+                                    if (!full)
+#pragma unroll
+                                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                            for (int e = 0; e < 2; ++e)
+                                                if (!vtk_sees(id[u], q.pos[h][e], vtk_floor(q.pos[h][e], a.window), a.sinks)) y[u][e] = 0.f;
+#pragma unroll
+                                    for (int u = 0; u < 2; ++u) sum[u] += y[u][0] + y[u][1];
+                                }
                             }
                         }
-                    }
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
-                        sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
-                    }
-                    if (t < 2) {
-                        float *p = part + tile * TW_TILE + 8 * t + g;
-                        const float y = t == 0 ? sum[0] : sum[1];
-                        *p = round == 0 ? y : *p + y;
+                        for (int u = 0; u < 2; ++u) {
+                            sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
+                            sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
+                        }
+                        if (t < 2) {
+                            float *p = part + tile * TILE + 16 * b + 8 * t + g;
+                            const float y = t == 0 ? sum[0] : sum[1];
+                            *p = round == 0 ? y : *p + y;
+                        }
                     }
                 }
             }
@@ -377,7 +393,7 @@ __global__ void __launch_bounds__(TW_NT, TW_CTAS) token_weights_kernel(const __g
             if (tid < n) {
                 const int id = a.cache_ids.null() ? at + tid : a.cache_ids[k.base + at + tid];
                 if (id >= 0 && id < k.range) {
-                    const int lane_of = tid / TW_TILE % lanes;
+                    const int lane_of = tid / TILE % lanes;
                     float y = 0.f;
                     for (int h = 0; h < heads && h < a.hkv; ++h) y += sh.part[buffer][h * lanes + lane_of][tid];
                     if (!w.prev.null()) y = fmaf(w.decay, w.prev[k.base + id], y);

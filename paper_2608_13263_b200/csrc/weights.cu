@@ -445,7 +445,7 @@ extern "C" {
 int64_t vtoken_token_weights_workspace_bytes(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens)
 {
     if (!ctx || vtk_check_heads(ctx, heads, 0) != VTOKEN_OK || max_query_tokens < 0) return VTOKEN_EINVAL;
-    return vtk_weights_prompt_workspace(ctx, heads);
+    return vtk_weights_prompt_workspace(ctx, heads, max_query_tokens);
 }
 
 int vtoken_token_weights(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_weights_in *in, void *cuda_stream)
@@ -496,7 +496,7 @@ int vtoken_token_weights(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t lay
     w.prev = VTK_ARR(ctx, in->decay == 0.f ? (const float *)nullptr : in->prev, ctx->cfg.max_tokens);
     w.scores = VTK_ARR(ctx, in->scores, ctx->cfg.max_tokens);
     w.decay = in->decay;
-    const bool prompts = (int64_t)in->max_query_len * a.group > TW_ROW_LIMIT;
+    const bool prompts = (int64_t)in->max_query_len * a.group > TW_ROW_LIMIT && a.group <= 128;       // (a row tile holds whole query tokens)
     a.row_limit = prompts ? TW_ROW_LIMIT : INT32_MAX;
     const bool wide = (prompts ? 1 : (int64_t)in->max_query_len) * a.group > 8;
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -12,4 +12,4 @@ struct VtkWeightsArgs {
 
 // host: launcher of weights_prompt.cu, and its part of the workspace
 int vtk_launch_weights_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkWeightsArgs &w, void *workspace, cudaStream_t st);
-int64_t vtk_weights_prompt_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads);
+int64_t vtk_weights_prompt_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens);

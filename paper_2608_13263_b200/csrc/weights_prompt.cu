@@ -4,25 +4,29 @@
 // 2 D flops and one exponential a pair of query row and token.  The product is taken as S^T = K Q^T, tokens as the rows of the
 // accumulator: a thread then owns a token and the sum over query rows is a sum over its registers, where S = Q K^T would need one over
 // the lanes of a warp for every column.  256 x 128 pairs take 1024 cycles of the tensor pipe and 2048 of the 16 exponentials a
-// cycle: the exponentials are the bound.
+// cycle, so three of eight exponentials are computed by a polynomial on the other pipes, see exp2_pair.
 //
-// An item is (request, 256 tokens, key head, chunk of row tiles): its K rows stay in shared memory while the 128-row tiles of Q that
-// see any of them stream by.  Sums of an item go to the workspace; a second small kernel adds them up in the order of chunks and
-// heads and joins them with the scores before.  Roles, 24 warps:
+// An item is (request, 256 tokens, key head, chunk of row tiles): its K rows stay in shared memory while the tiles of Q that see any of
+// them stream by, whole query tokens, 128 rows at most, a hardware copy each.  Sums of an item go to the workspace; a second small
+// kernel adds them up in the order of chunks and heads and joins them with the scores before.  Roles, 24 warps:
 //   0 .. 15          thread = token: exponentials of a row of S^T, summed.  Two groups of 8 warps take the row tiles in turn, each
 //                    with an accumulator for the first and one for the second 128 tokens
-//   16 .. 19         copies of K rows (by slot, once an item) and Q rows into 128-byte-swizzled tiles; 4-bit keys expanded on the way
-//   20               one thread issues the products
-//   21               draws items; 22, 23 find the row tiles that see the item's tokens and lay out positions and logarithms
+//   16 .. 19         copies of K rows (by slot, once an item), 4-bit keys expanded on the way; bf16 queries over 4-bit keys converted
+//   20, 21           products of the first and second 128 tokens, issued by one thread each
+//   22               draws items and finds the row tiles that see the item's tokens
+//   23               positions and logarithms of a tile's rows, and the copy of its queries
 // Each role goes from item to item on its own, handed on by barriers in shared memory.  Every wait is bounded (wait_limit_ms): where
-// one runs out all roles leave and VTOKEN_FLAG_TIMEOUT is set.
+// one runs out all roles leave and VTOKEN_FLAG_TIMEOUT is set.  (One warp that issued all products, four that copied the queries
+// with cp.async and 128 arrivals a tile, and searches for row tiles between the tiles took 600 us for a prompt of 8192 tokens.)
+#include <cuda.h>
+
 #include "tensor.cuh"
 #include "weights.cuh"
 
 namespace {
 
-constexpr int WP_NT = 768, WP_SUMS = 16, WP_META = 4, WP_Q = 2, WP_PAIR = 2 * TC_TILE, WP_JOIN_NT = 256;
-constexpr int WP_READERS = WP_SUMS + 4 + 1;                      // warps that read a Meta
+constexpr int WP_NT = 768, WP_SUMS = 16, WP_COPY = WP_SUMS, WP_MMA = 20, WP_DRAW = 22, WP_ROWS = 23;
+constexpr int WP_META = 4, WP_PAIR = 2 * TC_TILE, WP_JOIN_NT = 256, WP_WORDS = 32;
 constexpr uint64_t WP_DRAIN_NS = 1000000000;
 
 struct Args {
@@ -32,27 +36,26 @@ struct Args {
     int64_t max_parts;
     int32_t row_limit;                   // requests of at most so many rows belong to weights.cu
     int32_t grid;                        // of the kernel that computes
+    int32_t tokens;                      // query tokens of a row tile
     uint64_t limit_ns;
-    int64_t stall;                       // (checked build) the item whose first rows never become complete
+    int64_t stall;                       // (checked build) the item whose first rows never come
 };
 
 // a request in this kernel
 struct Spread {
-    int q0, len;
-    int64_t base, rows, pairs, tiles;    // pairs of token tiles; row tiles
+    int q0, qn, len;
+    int64_t base, pairs, tiles;          // pairs of token tiles; row tiles
 };
 
 __device__ inline Spread spread_of(const Args &w, int r, bool &clipped)
 {
     const VtkAttnArgs &a = w.w.at;
     Spread s;
-    int qn;
     bool c;
-    vtk_request_rows(a, r, s.q0, qn, s.base, s.len, c);
+    vtk_request_rows(a, r, s.q0, s.qn, s.base, s.len, c);
     clipped |= c;
-    s.rows = (int64_t)qn * a.group;
-    s.pairs = s.rows > w.row_limit ? ((int64_t)s.len + WP_PAIR - 1) / WP_PAIR : 0;
-    s.tiles = (s.rows + TC_TILE - 1) / TC_TILE;
+    s.pairs = (int64_t)s.qn * a.group > w.row_limit ? ((int64_t)s.len + WP_PAIR - 1) / WP_PAIR : 0;
+    s.tiles = ((int64_t)s.qn + w.tokens - 1) / w.tokens;
     return s;
 }
 __device__ __forceinline__ int64_t chunks_of(const Spread &s, int64_t chunk) { return (s.tiles + chunk - 1) / chunk; }
@@ -92,15 +95,15 @@ struct Cut {
         if (threadIdx.x == 0) { R = n; seg = (n + NT - 1) / NT; }
         __syncthreads();
         scan(w, [&](const Spread &s) { return s.pairs * s.tiles * a.hkv; }, clipped);
-        // about six items a CTA, of 4 to 64 row tiles, as many as the workspace has room for
-        int64_t c = items[NT] / ((int64_t)w.grid * 6);
-        c = c < 4 ? 4 : (c > 64 ? 64 : c);
-        for (;; c *= 2) {
+        // about eight items a CTA, of 4 to 32 row tiles, as many as the workspace has room for
+        int64_t c = items[NT] / ((int64_t)w.grid * 8);
+        c = c < 4 ? 4 : (c > 32 ? 32 : c);
+        for (;; c = c * 2 > 32 * WP_WORDS ? 32 * WP_WORDS : c * 2) {
             bool again = false;
             scan(w, [&](const Spread &s) { return s.pairs * chunks_of(s, c) * a.hkv; }, again);
-            if (items[NT] <= w.max_parts || c >= (1ll << 40)) break;
+            if (items[NT] <= w.max_parts || c >= 32 * WP_WORDS) break;
         }
-        if (threadIdx.x == 0) chunk = c;                     // (a number of row tiles: far below 2^32)
+        if (threadIdx.x == 0) chunk = c;
         __syncthreads();
     }
     // the request of pair (or item) `i`, and what is left of i there
@@ -125,56 +128,96 @@ struct Cut {
 };
 
 struct Item {
-    int none, kv, q0, rows, first, n;    // query rows of the request; first cache entry and number of tokens
-    int tile0, tile1;                    // row tiles
+    int none, kv, q0, qn, first, n;      // query tokens of the request; first cache entry and number of tokens
+    int tile0, count;                    // first row tile of the chunk; how many see something
     int64_t base, ticket;
+    uint32_t sees[WP_WORDS];             // which
 };
 
 struct Meta {                            // a tile of query rows
-    int tile, pmin, pmax;                // tile -1: the item's end
-    int all[2];                          // of each half: every row is there and saw something
+    int pmin, pmax, whole;               // whole: every row of the tile is there and saw something
     alignas(16) float lse2[TC_TILE];     // minus the logarithm to base 2
     alignas(16) int pos[TC_TILE];        // -2^31: the row adds nothing
     alignas(16) float scale[TC_TILE];    // bf16 queries over 4-bit keys: factor of the row's scores
 };
 
-// The sum over a tile's query rows of what token `id` gets from them: 128 columns of the thread's accumulator row.  Two copies, as a
-// branch at every mask would keep the compiler from overlapping the chains of loads, products and exponentials (6500 cycles a tile
-// instead of 3700).
+// 2^x of two numbers below 128 that may be anything else downwards: x = n + f with |f| <= 1/2, 2^f as its Taylor series with the
+// coefficients moved so that the largest error on the interval is least (degree 5: 2^-22.2 in 32 bits, by a fit at the extrema), 2^n put into the exponent.
+// NaN stays NaN.
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float2 exp2_pair(float2 x)
+{
+    const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);      // 1.5 * 2^23
+    x.x = max_nan(x.x, -125.f);
+    x.y = max_nan(x.y, -125.f);
+    const float2 up = add2(x, magic), n = add2(up, minus);
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 p = fma2(f, make_float2(0.001327647245f, 0.001327647245f), make_float2(0.009675540961f, 0.009675540961f));
+    p = fma2(p, f, make_float2(0.05550713092f, 0.05550713092f));
+    p = fma2(p, f, make_float2(0.2402212024f, 0.2402212024f));
+    p = fma2(p, f, make_float2(0.693146944f, 0.693146944f));
+    p = fma2(p, f, make_float2(1.f, 1.f));
+    // (the low bits of `up` are n)
+    p.x *= __int_as_float((int)(__float_as_uint(up.x) << 23) + 0x3f800000);
+    p.y *= __int_as_float((int)(__float_as_uint(up.y) << 23) + 0x3f800000);
+    return p;
+}
+
+// 16 columns of a thread's accumulator row: what token `id` gets from 16 query rows
 template <bool SCALED, bool MASKED>
-__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id)
+__device__ __forceinline__ void sum_columns(const VtkAttnArgs &a, const Meta &m, const uint32_t (&s)[16], int col, int id, float2 (&sum)[2])
 {
     const float c = a.scale_log2;
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        const float4 l = *reinterpret_cast<const float4 *>(&m.lse2[col + i]);
+        float4 f = make_float4(c, c, c, c);
+        if (SCALED) {
+            f = *reinterpret_cast<const float4 *>(&m.scale[col + i]);
+            f.x *= c; f.y *= c; f.z *= c; f.w *= c;
+        }
+        float2 y0 = fma2(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), make_float2(f.x, f.y), make_float2(l.x, l.y));
+        float2 y1 = fma2(make_float2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), make_float2(f.z, f.w), make_float2(l.z, l.w));
+        y0.x = vtk_exp2(y0.x); y0.y = vtk_exp2(y0.y);
+        if (i < 12) {
+            y1 = exp2_pair(y1);
+        } else {
+            y1.x = vtk_exp2(y1.x); y1.y = vtk_exp2(y1.y);
+        }
+        if (MASKED) {
+            const int4 p = *reinterpret_cast<const int4 *>(&m.pos[col + i]);
+            y0.x = vtk_sees(id, p.x, vtk_floor(p.x, a.window), a.sinks) ? y0.x : 0.f;
+            y0.y = vtk_sees(id, p.y, vtk_floor(p.y, a.window), a.sinks) ? y0.y : 0.f;
+            y1.x = vtk_sees(id, p.z, vtk_floor(p.z, a.window), a.sinks) ? y1.x : 0.f;
+            y1.y = vtk_sees(id, p.w, vtk_floor(p.w, a.window), a.sinks) ? y1.y : 0.f;
+        }
+        sum[0] = add2(sum[0], y0);
+        sum[1] = add2(sum[1], y1);
+    }
+}
+
+// The sum over a tile's query rows.  Of `rows` columns the first `free` need no mask.  (A branch at every mask would keep the compiler
+// from overlapping the chains of loads, products and exponentials: 6500 cycles a tile instead of 3700, in an earlier form.)
+template <bool SCALED>
+__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, int rows, int free)
+{
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     uint32_t v[2][16];
     tc_ld16(src, v[0]);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        uint32_t(&now)[16] = v[q & 1];
+    auto step = [&](int col, uint32_t (&now)[16], uint32_t (&then)[16]) {
         tc_wait_ld(now);
-        if (q < 7) tc_ld16(src + 16 * (q + 1), v[(q + 1) & 1]);
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const float4 l = *reinterpret_cast<const float4 *>(&m.lse2[16 * q + i]);
-            float4 f = make_float4(c, c, c, c);
-            if (SCALED) {
-                f = *reinterpret_cast<const float4 *>(&m.scale[16 * q + i]);
-                f.x *= c; f.y *= c; f.z *= c; f.w *= c;
-            }
-            float2 y0 = fma2(make_float2(__uint_as_float(now[i]), __uint_as_float(now[i + 1])), make_float2(f.x, f.y), make_float2(l.x, l.y));
-            float2 y1 = fma2(make_float2(__uint_as_float(now[i + 2]), __uint_as_float(now[i + 3])), make_float2(f.z, f.w), make_float2(l.z, l.w));
-            y0.x = vtk_exp2(y0.x); y0.y = vtk_exp2(y0.y);
-            y1.x = vtk_exp2(y1.x); y1.y = vtk_exp2(y1.y);
-            if (MASKED) {
-                const int4 p = *reinterpret_cast<const int4 *>(&m.pos[16 * q + i]);
-                y0.x = vtk_sees(id, p.x, vtk_floor(p.x, a.window), a.sinks) ? y0.x : 0.f;
-                y0.y = vtk_sees(id, p.y, vtk_floor(p.y, a.window), a.sinks) ? y0.y : 0.f;
-                y1.x = vtk_sees(id, p.z, vtk_floor(p.z, a.window), a.sinks) ? y1.x : 0.f;
-                y1.y = vtk_sees(id, p.w, vtk_floor(p.w, a.window), a.sinks) ? y1.y : 0.f;
-            }
-            sum[0] = add2(sum[0], y0);
-            sum[1] = add2(sum[1], y1);
-        }
+        if (col + 16 < rows) tc_ld16(src + col + 16, then);
+        if (col + 16 <= free) sum_columns<SCALED, false>(a, m, now, col, id, sum);
+        else sum_columns<SCALED, true>(a, m, now, col, id, sum);
+    };
+    for (int col = 0; col < rows; col += 32) {
+        step(col, v[0], v[1]);
+        if (col + 16 < rows) step(col + 16, v[1], v[0]);
     }
     sum[0] = add2(sum[0], sum[1]);
     return sum[0].x + sum[0].y;
@@ -182,23 +225,24 @@ __device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, ui
 
 template <int D>
 struct Shared {
+    static constexpr int Q = D == 128 ? 2 : 4;               // tiles of queries
     uint8_t k[2][2][D / 64][TC_TILE * 128];
-    uint8_t q[WP_Q][D / 64][TC_TILE * 128];
+    uint8_t q[Q][D / 64][TC_TILE * 128];
     Meta meta[WP_META];
     Item item[2];
     float other[2][WP_PAIR];             // the second group's sums of an item
     Cut<WP_NT> cut;
     uint64_t item_full[2], item_empty[2], meta_full[WP_META], meta_empty[WP_META], scale_full[WP_META], k_full[2], k_empty[2], other_full[2];
-    uint64_t q_full[WP_Q], q_empty[WP_Q], s_full[2][2], s_empty[2][2], drain;
+    uint64_t q_full[Q], q_empty[Q], s_full[2][2], s_empty[2][2], drain[2];
     uint32_t tmem;
     int abort;
 };
 
 template <int D, bool FP4, typename Act>
-__global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_constant__ Args w)
+__global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_constant__ Args w, const __grid_constant__ CUtensorMap queries)
 {
     using Mma = typename std::conditional<FP4, VtkFp16, Act>::type;
-    constexpr int PIECES = D / 8, PANEL = TC_TILE * 128;
+    constexpr int PIECES = D / 8, PANEL = TC_TILE * 128, Q = Shared<D>::Q;
     constexpr bool SCALED = FP4 && Act::kind == VTOKEN_KV_BF16;
     const VtkAttnArgs &a = w.w.at;
     extern __shared__ uint8_t raw[];
@@ -208,17 +252,16 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            vtk_mbar_init(&sh.item_full[i], 1); vtk_mbar_init(&sh.item_empty[i], WP_READERS + 2);
-            vtk_mbar_init(&sh.k_full[i], 128); vtk_mbar_init(&sh.k_empty[i], 1); vtk_mbar_init(&sh.other_full[i], 8);
+            vtk_mbar_init(&sh.item_full[i], 1); vtk_mbar_init(&sh.item_empty[i], WP_SUMS + 4 + 2 + 1);
+            vtk_mbar_init(&sh.k_full[i], FP4 ? 4 : 128); vtk_mbar_init(&sh.k_empty[i], 2); vtk_mbar_init(&sh.other_full[i], 8); vtk_mbar_init(&sh.drain[i], 1);
             for (int b = 0; b < 2; ++b) { vtk_mbar_init(&sh.s_full[i][b], 1); vtk_mbar_init(&sh.s_empty[i][b], 4); }
         }
-        for (int i = 0; i < WP_META; ++i) { vtk_mbar_init(&sh.meta_full[i], 2); vtk_mbar_init(&sh.meta_empty[i], WP_READERS); vtk_mbar_init(&sh.scale_full[i], 128); }
-        for (int i = 0; i < WP_Q; ++i) { vtk_mbar_init(&sh.q_full[i], 128); vtk_mbar_init(&sh.q_empty[i], 1); }
-        vtk_mbar_init(&sh.drain, 1);
+        for (int i = 0; i < WP_META; ++i) { vtk_mbar_init(&sh.meta_full[i], 1); vtk_mbar_init(&sh.meta_empty[i], 8 + (SCALED ? 4 : 0)); vtk_mbar_init(&sh.scale_full[i], 4); }
+        for (int i = 0; i < Q; ++i) { vtk_mbar_init(&sh.q_full[i], SCALED ? 4 : 1); vtk_mbar_init(&sh.q_empty[i], 2); }
         sh.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == WP_SUMS + 4) {
+    if (warp == WP_MMA) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(vtk_smem_u32(&sh.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
@@ -229,6 +272,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
     __syncthreads();
     tc_after_sync();
     const uint32_t tmem = sh.tmem;
+    const int rows = w.tokens * a.group;                     // of a tile
     constexpr uint32_t IDESC = (1u << 4) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 7) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 10) |
                                ((uint32_t)(TC_TILE >> 4) << 24) | ((uint32_t)(TC_TILE >> 3) << 17);
     auto wait_phase = [&](uint64_t *bar, uint32_t parity, uint64_t limit) {
@@ -240,38 +284,34 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
         __syncwarp();
         if (lane == 0) vtk_mbar_arrive(bar);
     };
+    auto stalled = [&](const Item &it) {
+#ifdef VTOKEN_CHECKED
+        return it.ticket == w.stall;
+#else
+        return false;
+#endif
+    };
 
-    // Every role runs over the items and, within one, over the row tiles that see something of it.
-    uint32_t n_item = 0, n_meta = 0;
+    // Every role runs over the items and, within one, over the row tiles that see something of it; the tiles are counted throughout.
+    uint32_t n_item = 0, n_tile = 0, n_key = 0;
     auto each_item = [&](auto &&body) {
         for (;; ++n_item) {
             const int s = n_item & 1;
             if (!wait(&sh.item_full[s], n_item, 2)) return;
-            const Item it = sh.item[s];
+            const Item &it = sh.item[s];
             if (it.none || !body(it)) return;
             arrive(&sh.item_empty[s]);
-        }
-    };
-    auto each_tile = [&](auto &&body) {                      // false: given up
-        for (;;) {
-            const int s = n_meta % WP_META;
-            if (!wait(&sh.meta_full[s], n_meta, WP_META)) return false;
-            const bool end = sh.meta[s].tile < 0;
-            if (!end && !body(sh.meta[s])) return false;
-            arrive(&sh.meta_empty[s]);
-            ++n_meta;
-            if (end) return true;
+            ++n_key;
         }
     };
 
     if (warp < WP_SUMS) {
         // ================= exponentials: thread = token =================
-        const int group = warp >> 3, x = (warp >> 2) & 1, row = tid & 127;
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21;                       // 32 lanes a warp
-        uint32_t n_mine = 0, n_q = 0;
+        const int group = warp >> 3, x = (warp >> 2) & 1, row = tid & 127, at = x * TC_TILE + row;
+        const uint32_t src = tmem + ((uint32_t)(warp & 3) << 21) + (x * 2 + group) * TC_TILE;         // 32 lanes a warp
+        uint32_t n_mine = 0;
         bool bad_slot = false;
         each_item([&](const Item &it) {
-            const int at = x * TC_TILE + row;
             int id = INT32_MAX;
             bool there = false;
             if (at < it.n) {
@@ -283,23 +323,26 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
             const bool every = __all_sync(0xffffffffu, there);
             const int id_lo = __reduce_min_sync(0xffffffffu, id), id_hi = __reduce_max_sync(0xffffffffu, there ? id : -1);
             const bool mine = x * TC_TILE < it.n;                                // (uniform)
+            const int count = it.count;
             float total = 0.f;
-            const bool ok = each_tile([&](const Meta &m) {
-                const uint32_t turn = n_q++;
-                if (!mine || (int)(turn & 1) != group) return true;
-                if (!wait(&sh.s_full[x][group], n_mine, 1)) return false;
-                if (SCALED && !wait(&sh.scale_full[turn % WP_META], turn, WP_META)) return false;
-                tc_after_sync();
-                const uint32_t src = tmem + lanes + (x * 2 + group) * TC_TILE;
-                const bool some = m.pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(m.pmin, a.window) || id_lo < a.sinks);
-                const bool full = every && m.all[0] && m.all[1] && id_hi <= m.pmin && (id_lo > vtk_floor(m.pmax, a.window) || id_hi < a.sinks);
-                if (some) total += full ? row_sum<SCALED, false>(a, m, src, id) : row_sum<SCALED, true>(a, m, src, id);
-                tc_before_sync();
-                arrive(&sh.s_empty[x][group]);
-                ++n_mine;
-                return true;
-            });
-            if (!ok) return false;
+            for (int j = (int)((n_tile ^ group) & 1); j < count; j += 2) {       // (tiles of the other group pass by)
+                const uint32_t n = n_tile + j, slot = n % WP_META;
+                if (!wait(&sh.meta_full[slot], n, WP_META)) return false;
+                const Meta &m = sh.meta[slot];
+                if (mine) {
+                    if (!wait(&sh.s_full[x][group], n_mine, 1)) return false;
+                    if (SCALED && !wait(&sh.scale_full[slot], n, WP_META)) return false;
+                    tc_after_sync();
+                    const bool some = m.pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(m.pmin, a.window) || id_lo < a.sinks);
+                    const bool full = every && m.whole && id_hi <= m.pmin && (id_lo > vtk_floor(m.pmax, a.window) || id_hi < a.sinks);
+                    if (some) total += row_sum<SCALED>(a, m, src, id, rows, full ? rows : 0);
+                    tc_before_sync();
+                    arrive(&sh.s_empty[x][group]);
+                    ++n_mine;
+                }
+                arrive(&sh.meta_empty[slot]);
+            }
+            n_tile += count;
             const int turn = n_item & 1;
             if (group == 1) {
                 sh.other[turn][at] = total;
@@ -311,20 +354,12 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
             return true;
         });
         if (bad_slot) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_SLOT);
-    } else if (warp < WP_SUMS + 4) {
+    } else if (warp < WP_COPY + 4) {
         // ================= copies =================
-        const int pt = tid - WP_SUMS * 32;
-        uint32_t n_k = 0, n_q = 0;
-        auto stalled = [&](const Item &it) {
-#ifdef VTOKEN_CHECKED
-            return it.ticket == w.stall;
-#else
-            return false;
-#endif
-        };
-        auto keys = [&](const Item &it) {
-            const int kb = n_k & 1;
-            if (!wait_empty(&sh.k_empty[kb], n_k, 2)) return false;
+        const int pt = tid - WP_COPY * 32;
+        each_item([&](const Item &it) {
+            const int kb = n_key & 1;
+            if (!wait_empty(&sh.k_empty[kb], n_key, 2)) return false;
             auto slot_of = [&](int at) {
                 const int64_t slot = at < it.n ? a.cache_slots[it.base + it.first + at] : -1;
                 return slot < a.slots_per_layer ? (int)slot : -1;
@@ -377,123 +412,97 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                 cp_arrive(&sh.k_full[kb]);
             } else {
                 async_proxy_fence();
-                vtk_mbar_arrive(&sh.k_full[kb]);
+                arrive(&sh.k_full[kb]);
             }
-            ++n_k;
-            return true;
-        };
-        each_item([&](const Item &it) {
+            if (!SCALED) return true;
+            // bf16 queries in half precision: see attention.cu
+            const int tok = pt / a.group, head = pt % a.group, words = (it.count > 0 ? WP_WORDS : 0);
             bool first = true;
-            return each_tile([&](Meta &m) {
-                if (first && !keys(it)) return false;
-                const int stage = n_q % WP_Q;
-                if (!wait_empty(&sh.q_empty[stage], n_q, WP_Q)) return false;
-                const uint32_t dst = vtk_smem_u32(sh.q[stage]);
-                if (!FP4) {
-                    constexpr int ROWS = PIECES;             // (as the keys: each thread looks up one of its warp's 32 rows)
-                    const int piece = pt % PIECES, row0 = pt / PIECES * ROWS, at = m.tile * TC_TILE + pt;
-                    int64_t mine = -1;                       // where the row starts
-                    if (at < it.rows) mine = (int64_t)(it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
-#pragma unroll
-                    for (int i = 0; i < ROWS; ++i) {
-                        const int64_t row = __shfl_sync(0xffffffffu, mine, lane / PIECES * ROWS + i);
-                        cp_async16(dst + swizzled(row0 + i, piece), a.q + (row < 0 ? 0 : row) + 8 * piece, row >= 0);
-                    }
-                    if (!(first && stalled(it)) || pt > 0) cp_arrive(&sh.q_full[stage]);
-                } else {
-                    const int at = m.tile * TC_TILE + pt;
-                    const bool there = at < it.rows;
-                    const uint16_t *src = a.q;
-                    if (there) src += (int64_t)(it.q0 + at / a.group) * a.q_stride + (int64_t)(it.kv * a.group + at % a.group) * D;
-                    float up = 1.f;
-                    if (SCALED) {                            // bf16 queries in half precision: see attention.cu
-                        float top = 0.f, v[8];
-                        for (int i = 0; i < PIECES; ++i) {
-                            vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0), v);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-                        }
-                        int e2 = (int)(__float_as_uint(top) >> 23) - 127;
-                        e2 = 14 - (e2 < -100 ? -100 : e2);
-                        up = __uint_as_float((uint32_t)(127 + e2) << 23);
-                        m.scale[pt] = __uint_as_float((uint32_t)(127 - e2) << 23);
-                        vtk_mbar_arrive(&sh.scale_full[n_q % WP_META]);      // (of the rows that see something: fewer than entries)
-                    }
+            for (int word = 0; word < words; ++word)
+                for (uint32_t left = it.sees[word]; left != 0; left &= left - 1, ++n_tile, first = false) {
+                    const uint32_t slot = n_tile % WP_META, stage = n_tile % Q;
+                    if (!wait(&sh.meta_full[slot], n_tile, WP_META)) return false;
+                    const int64_t at = (int64_t)(it.tile0 + 32 * word + __ffs(left) - 1) * w.tokens + tok;
+                    const bool there = pt < rows && at < it.qn;
+                    const uint16_t *from = a.q;
+                    if (there) from += (it.q0 + at) * a.q_stride + (int64_t)(it.kv * a.group + head) * D;
+                    float top = 0.f, v[8];
                     for (int i = 0; i < PIECES; ++i) {
-                        uint4 word = there ? *reinterpret_cast<const uint4 *>(src + 8 * i) : make_uint4(0, 0, 0, 0);
-                        if (SCALED) {
-                            float v[8];
-                            vtk_unpack8<VtkBf16>(word, v);
+                        vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(from + 8 * i) : make_uint4(0, 0, 0, 0), v);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= up;
-                            word = vtk_pack8<VtkFp16>(v);
-                        }
-                        st_shared16(dst + swizzled(pt, i), word);
+                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+                    }
+                    int e2 = (int)(__float_as_uint(top) >> 23) - 127;
+                    e2 = 14 - (e2 < -100 ? -100 : e2);
+                    const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
+                    sh.meta[slot].scale[pt] = __uint_as_float((uint32_t)(127 - e2) << 23);
+                    arrive(&sh.scale_full[slot]);
+                    arrive(&sh.meta_empty[slot]);
+                    if (!wait_empty(&sh.q_empty[stage], n_tile, Q)) return false;
+                    const uint32_t dst = vtk_smem_u32(sh.q[stage]);
+                    for (int i = 0; i < PIECES; ++i) {
+                        vtk_unpack8<VtkBf16>(there ? *reinterpret_cast<const uint4 *>(from + 8 * i) : make_uint4(0, 0, 0, 0), v);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] *= up;
+                        st_shared16(dst + swizzled(pt, i), vtk_pack8<VtkFp16>(v));
                     }
                     async_proxy_fence();
-                    if (!(first && stalled(it)) || pt > 0) vtk_mbar_arrive(&sh.q_full[stage]);
+                    if (!(first && stalled(it)) || pt >= 32) arrive(&sh.q_full[stage]);
                 }
-                first = false;
-                ++n_q;
-                return true;
-            });
+            return true;
         });
         if (!FP4) cp_wait_all();
-    } else if (warp == WP_SUMS + 4) {
+    } else if (warp < WP_MMA + 2) {
         // ================= products =================
         const bool one = tc_elect();
-        uint32_t n_k = 0, n_q = 0, n_acc[2][2] = {{0, 0}, {0, 0}};
+        const int x = warp - WP_MMA;
+        uint32_t n_acc[2] = {0, 0};
         each_item([&](const Item &it) {
-            bool first = true;
-            const bool two = it.n > TC_TILE;
-            const int kb = n_k & 1;
-            const bool ok = each_tile([&](const Meta &) {
-                if (first && !wait(&sh.k_full[kb], n_k, 2)) return false;
-                first = false;
-                const int stage = n_q % WP_Q;
-                if (!wait(&sh.q_full[stage], n_q, WP_Q)) return false;
-                async_proxy_fence();
-                const int b = n_q & 1;
-                for (int x = 0; x < (two ? 2 : 1); ++x) {
-                    if (!wait_empty(&sh.s_empty[x][b], n_acc[x][b], 1)) return false;
+            const bool mine = x == 0 || it.n > TC_TILE;
+            const int kb = n_key & 1, count = it.count;
+            if (!wait(&sh.k_full[kb], n_key, 2)) return false;
+            const uint64_t kd = operand(vtk_smem_u32(sh.k[kb][x]));
+            for (int j = 0; j < count; ++j, ++n_tile) {
+                const int stage = n_tile % Q, b = n_tile & 1;
+                if (!wait(&sh.q_full[stage], n_tile, Q)) return false;           // (also where there is nothing to do: not to run ahead)
+                if (mine) {
+                    if (!wait_empty(&sh.s_empty[x][b], n_acc[b], 1)) return false;
+                    async_proxy_fence();
                     tc_after_sync();
-                    const uint64_t kd = operand(vtk_smem_u32(sh.k[kb][x])), qd = operand(vtk_smem_u32(sh.q[stage]));
+                    const uint64_t qd = operand(vtk_smem_u32(sh.q[stage]));
+                    const uint32_t acc = tmem + (x * 2 + b) * TC_TILE;
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t off = ((k / 4) * PANEL + (k % 4) * 32) >> 4;
-                        tc_mma_ss(one, tmem + (x * 2 + b) * TC_TILE, kd + off, qd + off, IDESC, k > 0);
+                        tc_mma_ss(one, acc, kd + off, qd + off, IDESC, k > 0);
                     }
                     tc_commit(one, &sh.s_full[x][b]);
-                    ++n_acc[x][b];
+                    ++n_acc[b];
                 }
                 tc_commit(one, &sh.q_empty[stage]);
-                ++n_q;
-                return true;
-            });
-            if (!first) {
-                tc_commit(one, &sh.k_empty[kb]);
-                ++n_k;
             }
-            return ok;
+            tc_commit(one, &sh.k_empty[kb]);
+            return true;
         });
         // what was issued ends before the tensor memory goes
-        tc_commit(one, &sh.drain);
+        tc_commit(one, &sh.drain[x]);
         const uint64_t t0 = vtk_global_ns();
-        while (!vtk_mbar_try(&sh.drain, 0) && vtk_global_ns() - t0 < WP_DRAIN_NS) {}
+        while (!vtk_mbar_try(&sh.drain[x], 0) && vtk_global_ns() - t0 < WP_DRAIN_NS) {}
         __syncwarp();
-    } else if (warp == WP_SUMS + 5) {
+    } else if (warp == WP_DRAW) {
         // ================= items =================
-        for (;; ++n_item) {
-            const int s = n_item & 1;
-            // (an item's roles wait once a tile, and each of those waits has the limit)
-            if (!wait_phase(&sh.item_empty[s], ((n_item / 2) & 1) ^ 1, w.limit_ns * (uint64_t)(sh.cut.chunk + 2))) break;
-            int64_t idx = 0;
-            if (lane == 0) idx = (int64_t)atomicAdd(w.tickets, 1u);
-            idx = __shfl_sync(0xffffffffu, idx, 0);
-            Item it;
-            it.none = 1;
-            it.ticket = idx;
-            if (idx < sh.cut.items[WP_NT] && idx < w.max_parts) {
+        for (bool more = true; more; ++n_item) {
+            Item it;                                         // (its words are written below)
+            uint32_t mine = 0;                               // lane i: word i
+            for (;;) {
+                int64_t idx = 0;
+                if (lane == 0) idx = (int64_t)atomicAdd(w.tickets, 1u);
+                idx = __shfl_sync(0xffffffffu, idx, 0);
+                it.none = 1;
+                it.ticket = idx;
+                it.count = 0;
+                mine = 0;
+                if (idx >= sh.cut.items[WP_NT] || idx >= w.max_parts) break;
                 Spread sp;
                 int64_t left = idx, before;
                 sh.cut.find(w, sh.cut.items, true, left, before, sp);
@@ -503,82 +512,118 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                 left /= a.hkv;
                 const int64_t c = left % chunks, pair = left / chunks;
                 it.tile0 = (int)(c * sh.cut.chunk);
-                it.tile1 = (int)((c + 1) * sh.cut.chunk < sp.tiles ? (c + 1) * sh.cut.chunk : sp.tiles);
+                const int tiles = (int)((c + 1) * sh.cut.chunk < sp.tiles ? sh.cut.chunk : sp.tiles - c * sh.cut.chunk);
                 it.q0 = sp.q0;
-                it.rows = (int)sp.rows;
+                it.qn = sp.qn;
                 it.first = (int)(pair * WP_PAIR);
                 it.n = sp.len - it.first < WP_PAIR ? sp.len - it.first : WP_PAIR;
                 it.base = sp.base;
+                const int id_lo = a.cache_ids.null() ? it.first : a.cache_ids[it.base + it.first];
+                const int id_hi = a.cache_ids.null() ? it.first + it.n - 1 : a.cache_ids[it.base + it.first + it.n - 1];
+                for (int word = 0; 32 * word < tiles; ++word) {
+                    int pmin = INT32_MAX, pmax = INT32_MIN;
+                    const int tile = 32 * word + lane;
+                    if (tile < tiles) {
+                        const int64_t t0 = (int64_t)(it.tile0 + tile) * w.tokens, t1 = t0 + w.tokens < it.qn ? t0 + w.tokens : it.qn;
+#pragma unroll 8
+                        for (int64_t t = t0; t < t1; ++t) {
+                            const int p = a.positions[it.q0 + t];
+                            pmin = p < pmin ? p : pmin;
+                            pmax = p > pmax ? p : pmax;
+                        }
+                    }
+                    const bool sees = tile < tiles && pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(pmin, a.window) || id_lo < a.sinks);
+                    const uint32_t found = __ballot_sync(0xffffffffu, sees);
+                    it.count += __popc(found);
+                    if (lane == word) mine = found;
+                }
+                if (it.count > 0) break;
+                for (int i = lane; i < WP_PAIR; i += 32) w.parts[idx * WP_PAIR + i] = 0.f;       // nobody sees anything of it
             }
-            if (lane == 0) sh.item[s] = it;
+            more = !it.none;
+            const int s = n_item & 1;
+            // (an item's roles wait once a tile, and each of those waits has the limit)
+            if (!wait_phase(&sh.item_empty[s], ((n_item / 2) & 1) ^ 1, w.limit_ns * (uint64_t)(sh.cut.chunk + 2))) break;
+            Item &to = sh.item[s];
+            to.sees[lane] = mine;
+            if (lane == 0) {
+                to.none = it.none; to.kv = it.kv; to.q0 = it.q0; to.qn = it.qn; to.first = it.first; to.n = it.n;
+                to.tile0 = it.tile0; to.count = it.count; to.base = it.base; to.ticket = it.ticket;
+            }
             arrive(&sh.item_full[s]);
-            if (it.none) break;
         }
     } else {
-        // ================= row tiles: which ones see something, positions and logarithms =================
-        const int half = warp - (WP_SUMS + 6);
+        // ================= rows: positions, logarithms, queries =================
+        static_assert(WP_WORDS == 32 && WP_ROWS == WP_NT / 32 - 1, "a lane a word; the last warp");
+        int tok[4], head[4];                                 // of rows lane, lane + 32, ...
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            tok[i] = (32 * i + lane) / a.group;
+            head[i] = (32 * i + lane) % a.group;
+        }
         each_item([&](const Item &it) {
-            const int id_lo = a.cache_ids.null() ? it.first : a.cache_ids[it.base + it.first];
-            const int id_hi = a.cache_ids.null() ? it.first + it.n - 1 : a.cache_ids[it.base + it.first + it.n - 1];
-            auto put = [&](int tile, int pmin, int pmax) {
-                float l[2] = {-INFINITY, -INFINITY};
-                int p[2] = {INT32_MIN, INT32_MIN};
-                bool all = true;
-                if (tile >= 0) {
+            const int words = it.count > 0 ? WP_WORDS : 0;
+            bool first = true;
+            for (int word = 0; word < words; ++word)
+                for (uint32_t left = it.sees[word]; left != 0; left &= left - 1, ++n_tile, first = false) {
+                    const int64_t t0 = (int64_t)(it.tile0 + 32 * word + __ffs(left) - 1) * w.tokens;
+                    float l[4];
+                    int p[4], pmin = INT32_MAX, pmax = INT32_MIN;
+                    bool whole = true;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int at = tile * TC_TILE + 64 * half + 32 * i + lane;
-                        if (at < it.rows) {
-                            const int64_t tok = it.q0 + at / a.group;
-                            l[i] = w.w.lse_in[tok * a.hq + it.kv * a.group + at % a.group];
-                            p[i] = a.positions[tok];
+                    for (int i = 0; i < 4; ++i) {
+                        l[i] = -INFINITY;
+                        p[i] = INT32_MIN;
+                        if (32 * i + lane >= rows) continue;
+                        if (t0 + tok[i] < it.qn) {
+                            const int64_t at = it.q0 + t0 + tok[i];
+                            l[i] = w.w.lse_in[at * a.hq + it.kv * a.group + head[i]];
+                            p[i] = a.positions[at];
+                            pmin = p[i] < pmin ? p[i] : pmin;
+                            pmax = p[i] > pmax ? p[i] : pmax;
                         }
-                        all &= l[i] != -INFINITY;
+                        whole &= l[i] != -INFINITY;
                     }
-                    all = __all_sync(0xffffffffu, all);
-                }
-                const int s = n_meta % WP_META;
-                if (!wait_empty(&sh.meta_empty[s], n_meta, WP_META)) return false;
-                Meta &m = sh.meta[s];
+                    pmin = __reduce_min_sync(0xffffffffu, pmin);
+                    pmax = __reduce_max_sync(0xffffffffu, pmax);
+                    whole = __all_sync(0xffffffffu, whole);
+                    const int stage = n_tile % Q, slot = n_tile % WP_META;
+                    if (!SCALED) {
+                        if (!wait_empty(&sh.q_empty[stage], n_tile, Q)) return false;
+                        if (lane == 0 && !(first && stalled(it))) {
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(vtk_smem_u32(&sh.q_full[stage])), "r"(rows * D * 2) : "memory");
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int row = 64 * half + 32 * i + lane;
-                    m.lse2[row] = l[i] * -1.4426950408889634f;
-                    m.pos[row] = l[i] == -INFINITY ? INT32_MIN : (p[i] < INT32_MAX - 1 ? p[i] : INT32_MAX - 1);      // (INT32_MAX: what is not there)
-                }
-                if (lane == 0) {
-                    m.all[half] = all;
-                    if (half == 0) {
-                        m.tile = tile;
+                            for (int panel = 0; panel < D / 64; ++panel)
+                                asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                                             ::"r"(vtk_smem_u32(sh.q[stage][panel])), "l"(&queries), "r"(64 * panel), "r"(it.kv * a.group), "r"((int)(it.q0 + t0)),
+                                               "r"(vtk_smem_u32(&sh.q_full[stage])) : "memory");
+                        }
+                        __syncwarp();
+                    }
+                    if (!wait_empty(&sh.meta_empty[slot], n_tile, WP_META)) return false;
+                    Meta &m = sh.meta[slot];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        m.lse2[32 * i + lane] = l[i] * -1.4426950408889634f;
+                        m.pos[32 * i + lane] = l[i] == -INFINITY ? INT32_MIN : (p[i] < INT32_MAX - 1 ? p[i] : INT32_MAX - 1);    // (INT32_MAX: what is not there)
+                    }
+                    if (lane == 0) {
                         m.pmin = pmin;
                         m.pmax = pmax;
+                        m.whole = whole;
                     }
+                    arrive(&sh.meta_full[slot]);
                 }
-                arrive(&sh.meta_full[s]);
-                ++n_meta;
-                return true;
-            };
-            for (int t0 = it.tile0; t0 < it.tile1; t0 += 32) {
-                int pmin = INT32_MAX, pmax = INT32_MIN;
-                if (t0 + lane < it.tile1) {
-                    const int first = (t0 + lane) * TC_TILE, last = first + TC_TILE < it.rows ? first + TC_TILE - 1 : it.rows - 1;
-#pragma unroll 4
-                    for (int t = first / a.group; t <= last / a.group; ++t) {
-                        const int p = a.positions[it.q0 + t];
-                        pmin = p < pmin ? p : pmin;
-                        pmax = p > pmax ? p : pmax;
-                    }
-                }
-                const bool sees = t0 + lane < it.tile1 && pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(pmin, a.window) || id_lo < a.sinks);
-                unsigned mask = __ballot_sync(0xffffffffu, sees);
-                while (mask) {
-                    const int src = __ffs(mask) - 1;
-                    mask &= mask - 1;
-                    if (!put(t0 + src, __shfl_sync(0xffffffffu, pmin, src), __shfl_sync(0xffffffffu, pmax, src))) return false;
-                }
-            }
-            return put(-1, 0, 0);
+            return true;
         });
+        if (!SCALED) {                                       // (after an abort: copies in flight land before the memory goes)
+            const uint64_t t0 = vtk_global_ns();
+            for (uint32_t i = 0; i < (uint32_t)Q && i < n_tile; ++i) {
+                const uint32_t n = n_tile - 1 - i;
+                while (*(volatile int *)&sh.abort != 0 && !vtk_mbar_try(&sh.q_full[n % Q], (n / Q) & 1) && vtk_global_ns() - t0 < WP_DRAIN_NS) {}
+            }
+            __syncwarp();
+        }
     }
     __syncthreads();
     if (tid == 0) {
@@ -586,7 +631,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
         __threadfence();
         if (atomicAdd(w.tickets + 1, 1u) == gridDim.x - 1) { w.tickets[0] = 0; w.tickets[1] = 0; }
     }
-    if (warp == WP_SUMS + 4) {
+    if (warp == WP_MMA) {
         tc_after_sync();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
     }
@@ -620,10 +665,42 @@ __global__ void __launch_bounds__(WP_JOIN_NT) weights_join_kernel(const __grid_c
     if (bad_id) atomicOr(a.flags, (uint32_t)VTOKEN_FLAG_BAD_VICTIM);
 }
 
-// what the items of a call can be: one chunk of row tiles everywhere, and some more chunks where there are few
-int64_t parts_of(const vtoken_ctx *ctx, const vtoken_heads *heads)
+// query tokens of a row tile: whole ones, so that a tile is one box of the queries
+int tokens_of(const vtoken_heads *heads)
 {
-    return ((ctx->cfg.max_tokens + WP_PAIR - 1) / WP_PAIR + ctx->cfg.max_requests) * heads->num_kv_heads + (int64_t)ctx->num_sms * 12;
+    const int group = heads->num_q_heads / heads->num_kv_heads;
+    return group < TC_TILE ? TC_TILE / group : 1;
+}
+
+// what the items of a call can be: chunks of 32 * WP_WORDS row tiles everywhere, and some more where there are few
+int64_t parts_of(const vtoken_ctx *ctx, const vtoken_heads *heads, int64_t max_query_tokens)
+{
+    const int64_t tiles = max_query_tokens / tokens_of(heads) + 1, chunks = (tiles + 32 * WP_WORDS - 1) / (32 * WP_WORDS);
+    return ((ctx->cfg.max_tokens + WP_PAIR - 1) / WP_PAIR + ctx->cfg.max_requests) * heads->num_kv_heads * chunks + (int64_t)ctx->num_sms * 16;
+}
+
+// the queries as [tokens][heads][dimensions]; a box is 64 dimensions of a key head's query heads of a tile's tokens
+cudaError_t map_queries(const VtkAttnArgs &a, int head_dim, bool bf16, int tokens, CUtensorMap *map)
+{
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<Encode> known{nullptr};
+    Encode encode = known.load(std::memory_order_relaxed);
+    if (encode == nullptr) {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+        if (e != cudaSuccess) return e;
+        if (found != cudaDriverEntryPointSuccess || f == nullptr) return cudaErrorNotSupported;
+        encode = (Encode)f;
+        known.store(encode, std::memory_order_relaxed);
+    }
+    const cuuint64_t size[3] = {(cuuint64_t)head_dim, (cuuint64_t)a.hq, (cuuint64_t)a.max_query_tokens};
+    const cuuint64_t stride[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)tokens}, step[3] = {1, 1, 1};
+    const CUresult r = encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<uint16_t *>(a.q), size, stride, box, step,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 template <int D, bool FP4, typename Act>
@@ -631,10 +708,13 @@ int launch(vtoken_ctx *ctx, const Args &w, cudaStream_t st)
 {
     constexpr int smem = (int)sizeof(Shared<D>) + 1024;
     static_assert(smem <= 232448, "shared memory of a CTA");
+    constexpr bool bf = Act::kind == VTOKEN_KV_BF16;
+    alignas(64) CUtensorMap map = {};
+    if (!(FP4 && bf)) VTK_CUDA(ctx, map_queries(w.w.at, D, bf, w.tokens, &map));
     auto kernel = weights_prompt_kernel<D, FP4, Act>;
     static std::atomic<int> allowed{-1};                     // the device that knows of this kernel's shared memory
     VTK_CUDA(ctx, vtk_allow_smem(ctx, allowed, (const void *)kernel, smem));
-    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(w.grid), dim3(WP_NT), smem, st, w));
+    VTK_CUDA(ctx, vtk_launch_dependent(ctx, kernel, dim3(w.grid), dim3(WP_NT), smem, st, w, map));
     VTK_CUDA(ctx, vtk_launch_dependent(ctx, weights_join_kernel, dim3(ctx->num_sms * 2), dim3(WP_JOIN_NT), 0, st, w));
     VTK_CUDA(ctx, cudaGetLastError());
     return VTOKEN_OK;
@@ -649,7 +729,10 @@ int launch_by_type(vtoken_ctx *ctx, const vtoken_heads *h, const Args &w, cudaSt
 
 }  // namespace
 
-int64_t vtk_weights_prompt_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads) { return 16 + parts_of(ctx, heads) * WP_PAIR * 4; }
+int64_t vtk_weights_prompt_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens)
+{
+    return 16 + parts_of(ctx, heads, max_query_tokens) * WP_PAIR * 4;
+}
 
 int vtk_launch_weights_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkWeightsArgs &weights, void *workspace, cudaStream_t st)
 {
@@ -657,9 +740,10 @@ int vtk_launch_weights_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const 
     w.w = weights;
     w.tickets = (uint32_t *)workspace;
     w.parts = (float *)((uint8_t *)workspace + 16);
-    w.max_parts = parts_of(ctx, heads);
+    w.max_parts = parts_of(ctx, heads, weights.at.max_query_tokens);
     w.row_limit = weights.at.row_limit;
     w.grid = ctx->num_sms;
+    w.tokens = tokens_of(heads);
     w.limit_ns = (uint64_t)ctx->wait_limit_ns;
     w.stall = ctx->stall_item;
     return heads->head_dim == 128 ? launch_by_type<128>(ctx, heads, w, st) : launch_by_type<64>(ctx, heads, w, st);

@@ -4,7 +4,7 @@
 // 2 D flops and one exponential a pair of query row and token.  The product is taken as S^T = K Q^T, tokens as the rows of the
 // accumulator: a thread then owns a token and the sum over query rows is a sum over its registers, where S = Q K^T would need one over
 // the lanes of a warp for every column.  256 x 128 pairs take 1024 cycles of the tensor pipe and 2048 of the 16 exponentials a
-// cycle, so three of eight exponentials are computed by a polynomial on the other pipes, see exp2_pair.
+// cycle: the exponentials are the bound.
 //
 // An item is (request, 256 tokens, key head, chunk of row tiles): its K rows stay in shared memory while the tiles of Q that see any of
 // them stream by, whole query tokens, 128 rows at most, a hardware copy each.  Sums of an item go to the workspace; a second small
@@ -141,54 +141,22 @@ struct Meta {                            // a tile of query rows
     alignas(16) float scale[TC_TILE];    // bf16 queries over 4-bit keys: factor of the row's scores
 };
 
-// 2^x of two numbers below 128 that may be anything else downwards: x = n + f with |f| <= 1/2, 2^f as its Taylor series with the
-// coefficients moved so that the largest error on the interval is least (degree 5: 2^-22.2 in 32 bits, by a fit at the extrema), 2^n put into the exponent.
-// NaN stays NaN.
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
-__device__ __forceinline__ float2 exp2_pair(float2 x)
-{
-    const float2 magic = make_float2(12582912.f, 12582912.f), minus = make_float2(-12582912.f, -12582912.f);      // 1.5 * 2^23
-    x.x = max_nan(x.x, -125.f);
-    x.y = max_nan(x.y, -125.f);
-    const float2 up = add2(x, magic), n = add2(up, minus);
-    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 p = fma2(f, make_float2(0.001327647245f, 0.001327647245f), make_float2(0.009675540961f, 0.009675540961f));
-    p = fma2(p, f, make_float2(0.05550713092f, 0.05550713092f));
-    p = fma2(p, f, make_float2(0.2402212024f, 0.2402212024f));
-    p = fma2(p, f, make_float2(0.693146944f, 0.693146944f));
-    p = fma2(p, f, make_float2(1.f, 1.f));
-    // (the low bits of `up` are n)
-    p.x *= __int_as_float((int)(__float_as_uint(up.x) << 23) + 0x3f800000);
-    p.y *= __int_as_float((int)(__float_as_uint(up.y) << 23) + 0x3f800000);
-    return p;
-}
-
-// 16 columns of a thread's accumulator row: what token `id` gets from 16 query rows
+// 16 columns of a thread's accumulator row: what token `id` gets from 16 query rows, l: minus their logarithms
 template <bool SCALED, bool MASKED>
-__device__ __forceinline__ void sum_columns(const VtkAttnArgs &a, const Meta &m, const uint32_t (&s)[16], int col, int id, float2 (&sum)[2])
+__device__ __forceinline__ void sum_columns(const VtkAttnArgs &a, const Meta &m, const uint32_t (&s)[16], const float4 (&l)[4], int col, int id, float2 (&sum)[2])
 {
     const float c = a.scale_log2;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-        const float4 l = *reinterpret_cast<const float4 *>(&m.lse2[col + i]);
         float4 f = make_float4(c, c, c, c);
         if (SCALED) {
             f = *reinterpret_cast<const float4 *>(&m.scale[col + i]);
             f.x *= c; f.y *= c; f.z *= c; f.w *= c;
         }
-        float2 y0 = fma2(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), make_float2(f.x, f.y), make_float2(l.x, l.y));
-        float2 y1 = fma2(make_float2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), make_float2(f.z, f.w), make_float2(l.z, l.w));
+        float2 y0 = fma2(make_float2(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), make_float2(f.x, f.y), make_float2(l[i / 4].x, l[i / 4].y));
+        float2 y1 = fma2(make_float2(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), make_float2(f.z, f.w), make_float2(l[i / 4].z, l[i / 4].w));
         y0.x = vtk_exp2(y0.x); y0.y = vtk_exp2(y0.y);
-        if (i < 12) {
-            y1 = exp2_pair(y1);
-        } else {
-            y1.x = vtk_exp2(y1.x); y1.y = vtk_exp2(y1.y);
-        }
+        y1.x = vtk_exp2(y1.x); y1.y = vtk_exp2(y1.y);
         if (MASKED) {
             const int4 p = *reinterpret_cast<const int4 *>(&m.pos[col + i]);
             y0.x = vtk_sees(id, p.x, vtk_floor(p.x, a.window), a.sinks) ? y0.x : 0.f;
@@ -201,23 +169,34 @@ __device__ __forceinline__ void sum_columns(const VtkAttnArgs &a, const Meta &m,
     }
 }
 
-// The sum over a tile's query rows.  Of `rows` columns the first `free` need no mask.  (A branch at every mask would keep the compiler
-// from overlapping the chains of loads, products and exponentials: 6500 cycles a tile instead of 3700, in an earlier form.)
+// The sum over a tile's query rows.  free: none of them needs a mask.  (A branch at every mask would keep the compiler from
+// overlapping the chains of loads, products and exponentials: 6500 cycles a tile instead of 3700, in an earlier form.)
 template <bool SCALED>
-__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, int rows, int free)
+__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, int rows, bool free)
 {
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     uint32_t v[2][16];
     tc_ld16(src, v[0]);
-    auto step = [&](int col, uint32_t (&now)[16], uint32_t (&then)[16]) {
+    auto step = [&](int col, uint32_t (&now)[16], uint32_t (&then)[16], bool masked) {
+        float4 l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l[i] = *reinterpret_cast<const float4 *>(&m.lse2[col + 4 * i]);
         tc_wait_ld(now);
         if (col + 16 < rows) tc_ld16(src + col + 16, then);
-        if (col + 16 <= free) sum_columns<SCALED, false>(a, m, now, col, id, sum);
-        else sum_columns<SCALED, true>(a, m, now, col, id, sum);
+        if (masked) sum_columns<SCALED, true>(a, m, now, l, col, id, sum);
+        else sum_columns<SCALED, false>(a, m, now, l, col, id, sum);
     };
-    for (int col = 0; col < rows; col += 32) {
-        step(col, v[0], v[1]);
-        if (col + 16 < rows) step(col + 16, v[1], v[0]);
+    if (free && rows == TC_TILE) {
+#pragma unroll
+        for (int col = 0; col < TC_TILE; col += 32) {
+            step(col, v[0], v[1], false);
+            step(col + 16, v[1], v[0], false);
+        }
+    } else {                                                 // (columns behind the rows are masked)
+        for (int col = 0; col < rows; col += 32) {
+            step(col, v[0], v[1], !free || col + 16 > rows);
+            if (col + 16 < rows) step(col + 16, v[1], v[0], !free || col + 32 > rows);
+        }
     }
     sum[0] = add2(sum[0], sum[1]);
     return sum[0].x + sum[0].y;
@@ -233,7 +212,7 @@ struct Shared {
     float other[2][WP_PAIR];             // the second group's sums of an item
     Cut<WP_NT> cut;
     uint64_t item_full[2], item_empty[2], meta_full[WP_META], meta_empty[WP_META], scale_full[WP_META], k_full[2], k_empty[2], other_full[2];
-    uint64_t q_full[Q], q_empty[Q], s_full[2][2], s_empty[2][2], drain[2];
+    uint64_t q_full[Q], q_empty[Q], s_full[2][2], s_empty[2][2], drain[2];                // scores: of 128 tokens, group
     uint32_t tmem;
     int abort;
 };
@@ -335,7 +314,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                     tc_after_sync();
                     const bool some = m.pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(m.pmin, a.window) || id_lo < a.sinks);
                     const bool full = every && m.whole && id_hi <= m.pmin && (id_lo > vtk_floor(m.pmax, a.window) || id_hi < a.sinks);
-                    if (some) total += row_sum<SCALED>(a, m, src, id, rows, full ? rows : 0);
+                    if (some) total += row_sum<SCALED>(a, m, src, id, rows, full);
                     tc_before_sync();
                     arrive(&sh.s_empty[x][group]);
                     ++n_mine;
@@ -555,65 +534,88 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
     } else {
         // ================= rows: positions, logarithms, queries =================
         static_assert(WP_WORDS == 32 && WP_ROWS == WP_NT / 32 - 1, "a lane a word; the last warp");
-        int tok[4], head[4];                                 // of rows lane, lane + 32, ...
+        int tok[4];                                          // of rows lane, lane + 32, ...; -1: there is none
+        int64_t lse_of[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            tok[i] = (32 * i + lane) / a.group;
-            head[i] = (32 * i + lane) % a.group;
+            tok[i] = 32 * i + lane < rows ? (32 * i + lane) / a.group : -1;
+            lse_of[i] = (int64_t)(tok[i] < 0 ? 0 : tok[i]) * a.hq + (32 * i + lane) % a.group;
         }
+        struct Values { float l[4]; int p[4]; };
         each_item([&](const Item &it) {
-            const int words = it.count > 0 ? WP_WORDS : 0;
-            bool first = true;
-            for (int word = 0; word < words; ++word)
-                for (uint32_t left = it.sees[word]; left != 0; left &= left - 1, ++n_tile, first = false) {
-                    const int64_t t0 = (int64_t)(it.tile0 + 32 * word + __ffs(left) - 1) * w.tokens;
-                    float l[4];
-                    int p[4], pmin = INT32_MAX, pmax = INT32_MIN;
-                    bool whole = true;
+            const int count = it.count;
+            int word = -1;
+            uint32_t left = 0;
+            auto next_tile = [&]() {
+                while (left == 0) left = it.sees[++word];
+                const int64_t t0 = (int64_t)(it.tile0 + 32 * word + __ffs(left) - 1) * w.tokens;
+                left &= left - 1;
+                return t0;
+            };
+            auto fetch = [&](int64_t t0) {                   // (without a branch, so that all eight are on their way at once)
+                Values v;
+                const float *lse = w.w.lse_in + (it.q0 + t0) * a.hq + it.kv * a.group;
+                const int32_t *pos = a.positions.at(it.q0 + t0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        l[i] = -INFINITY;
-                        p[i] = INT32_MIN;
-                        if (32 * i + lane >= rows) continue;
-                        if (t0 + tok[i] < it.qn) {
-                            const int64_t at = it.q0 + t0 + tok[i];
-                            l[i] = w.w.lse_in[at * a.hq + it.kv * a.group + head[i]];
-                            p[i] = a.positions[at];
-                            pmin = p[i] < pmin ? p[i] : pmin;
-                            pmax = p[i] > pmax ? p[i] : pmax;
-                        }
-                        whole &= l[i] != -INFINITY;
+                for (int i = 0; i < 4; ++i) {
+                    const bool there = tok[i] >= 0 && t0 + tok[i] < it.qn;
+                    v.l[i] = lse[there ? lse_of[i] : 0];
+                    v.p[i] = pos[there ? tok[i] : 0];
+                    if (!there) {
+                        v.l[i] = -INFINITY;
+                        v.p[i] = INT32_MIN;
                     }
-                    pmin = __reduce_min_sync(0xffffffffu, pmin);
-                    pmax = __reduce_max_sync(0xffffffffu, pmax);
-                    whole = __all_sync(0xffffffffu, whole);
-                    const int stage = n_tile % Q, slot = n_tile % WP_META;
-                    if (!SCALED) {
-                        if (!wait_empty(&sh.q_empty[stage], n_tile, Q)) return false;
-                        if (lane == 0 && !(first && stalled(it))) {
-                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(vtk_smem_u32(&sh.q_full[stage])), "r"(rows * D * 2) : "memory");
-#pragma unroll
-                            for (int panel = 0; panel < D / 64; ++panel)
-                                asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                                             ::"r"(vtk_smem_u32(sh.q[stage][panel])), "l"(&queries), "r"(64 * panel), "r"(it.kv * a.group), "r"((int)(it.q0 + t0)),
-                                               "r"(vtk_smem_u32(&sh.q_full[stage])) : "memory");
-                        }
-                        __syncwarp();
-                    }
-                    if (!wait_empty(&sh.meta_empty[slot], n_tile, WP_META)) return false;
-                    Meta &m = sh.meta[slot];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        m.lse2[32 * i + lane] = l[i] * -1.4426950408889634f;
-                        m.pos[32 * i + lane] = l[i] == -INFINITY ? INT32_MIN : (p[i] < INT32_MAX - 1 ? p[i] : INT32_MAX - 1);    // (INT32_MAX: what is not there)
-                    }
-                    if (lane == 0) {
-                        m.pmin = pmin;
-                        m.pmax = pmax;
-                        m.whole = whole;
-                    }
-                    arrive(&sh.meta_full[slot]);
                 }
+                return v;
+            };
+            int64_t t0 = next_tile();
+            Values now = fetch(t0);
+            for (int j = 0; j < count; ++j, ++n_tile) {
+                const int64_t at = t0;
+                Values then = now;
+                if (j + 1 < count) {
+                    t0 = next_tile();
+                    then = fetch(t0);
+                }
+                const int stage = n_tile % Q, slot = n_tile % WP_META;
+                if (!SCALED) {
+                    if (!wait_empty(&sh.q_empty[stage], n_tile, Q)) return false;
+                    if (lane == 0 && !(j == 0 && stalled(it))) {
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(vtk_smem_u32(&sh.q_full[stage])), "r"(rows * D * 2) : "memory");
+#pragma unroll
+                        for (int panel = 0; panel < D / 64; ++panel)
+                            asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                                         ::"r"(vtk_smem_u32(sh.q[stage][panel])), "l"(&queries), "r"(64 * panel), "r"(it.kv * a.group), "r"((int)(it.q0 + at)),
+                                           "r"(vtk_smem_u32(&sh.q_full[stage])) : "memory");
+                    }
+                    __syncwarp();
+                }
+                int pmin = INT32_MAX, pmax = INT32_MIN;
+                bool whole = true;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (tok[i] >= 0 && at + tok[i] < it.qn) pmin = now.p[i] < pmin ? now.p[i] : pmin;
+                    pmax = now.p[i] > pmax ? now.p[i] : pmax;
+                    whole &= tok[i] < 0 || now.l[i] != -INFINITY;
+                }
+                pmin = __reduce_min_sync(0xffffffffu, pmin);
+                pmax = __reduce_max_sync(0xffffffffu, pmax);
+                whole = __all_sync(0xffffffffu, whole);
+                if (!wait_empty(&sh.meta_empty[slot], n_tile, WP_META)) return false;
+                Meta &m = sh.meta[slot];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    m.lse2[32 * i + lane] = now.l[i] * -1.4426950408889634f;
+                    m.pos[32 * i + lane] = now.l[i] == -INFINITY ? INT32_MIN : (now.p[i] < INT32_MAX - 1 ? now.p[i] : INT32_MAX - 1);    // (INT32_MAX: what is not there)
+                }
+                if (lane == 0) {
+                    m.pmin = pmin;
+                    m.pmax = pmax;
+                    m.whole = whole;
+                }
+                arrive(&sh.meta_full[slot]);
+                now = then;
+            }
             return true;
         });
         if (!SCALED) {                                       // (after an abort: copies in flight land before the memory goes)

@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
             lse_of[i] = (int64_t)(tok[i] < 0 ? 0 : tok[i]) * a.hq + (32 * i + lane) % a.group;
         }
         struct Values { float l[4]; int p[4]; };
+        uint32_t started = 0, skipped = UINT32_MAX;          // copies, and one that was left out
         each_item([&](const Item &it) {
             const int count = it.count;
             int word = -1;
@@ -580,7 +581,9 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                 const int stage = n_tile % Q, slot = n_tile % WP_META;
                 if (!SCALED) {
                     if (!wait_empty(&sh.q_empty[stage], n_tile, Q)) return false;
-                    if (lane == 0 && !(j == 0 && stalled(it))) {
+                    if (j == 0 && stalled(it)) skipped = n_tile;
+                    started = n_tile + 1;
+                    if (lane == 0 && n_tile != skipped) {
                         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(vtk_smem_u32(&sh.q_full[stage])), "r"(rows * D * 2) : "memory");
 #pragma unroll
                         for (int panel = 0; panel < D / 64; ++panel)
@@ -620,9 +623,9 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
         });
         if (!SCALED) {                                       // (after an abort: copies in flight land before the memory goes)
             const uint64_t t0 = vtk_global_ns();
-            for (uint32_t i = 0; i < (uint32_t)Q && i < n_tile; ++i) {
-                const uint32_t n = n_tile - 1 - i;
-                while (*(volatile int *)&sh.abort != 0 && !vtk_mbar_try(&sh.q_full[n % Q], (n / Q) & 1) && vtk_global_ns() - t0 < WP_DRAIN_NS) {}
+            for (uint32_t i = 0; i < (uint32_t)Q && i < started; ++i) {
+                const uint32_t n = started - 1 - i;
+                while (n != skipped && *(volatile int *)&sh.abort != 0 && !vtk_mbar_try(&sh.q_full[n % Q], (n / Q) & 1) && vtk_global_ns() - t0 < WP_DRAIN_NS) {}
             }
             __syncwarp();
         }

@@ -45,7 +45,9 @@
  * ring, of the rest of its ticket and of the ticket it had requested ahead.  In the prompt kernel
  * of vtoken_attention the warps of a CTA also wait for one another's tiles, under the same limit;
  * what may be missing there are the outputs of the item (256 query rows of a key head) and of the
- * one the CTA had taken ahead.
+ * one the CTA had taken ahead.  The same holds for the kernel for many query rows of
+ * vtoken_token_weights (item: 256 tokens of a request, whose scores are then wrong) and for the
+ * prefixes of vtoken_attention_shared (item: 256 query rows of a group, whose outputs are then wrong).
  *
  * Threads: a context is not thread-safe.  Calls on one context must come from one thread at a
  * time; different contexts (different pools) are independent.

@@ -373,3 +373,28 @@ def test_refusals():
     with pytest.raises(vt.VtokenError):
         vt.vtoken_token_weights_workspace_bytes(c.ctx, c.heads, -1)
     c.close()
+
+
+@pytest.mark.parametrize("group", [65, 128, 130])
+def test_many_query_heads_on_a_key_head(group):
+    """Row tiles of one query token, and more heads than a tile has rows."""
+    rng = np.random.default_rng(17)
+    positions = [list(range(290, 300)), [63], list(range(130))]
+    run_and_check(problem(rng, ("bf16", "bf16", group, 1, 64), [300, 64, 130], positions, keep=0.8))
+
+
+def test_more_key_heads_than_warps_and_longer_caches():
+    rng = np.random.default_rng(18)
+    run_and_check(problem(rng, ("fp16", "fp16", 33, 11, 64), [3000, 17, 900], [[2999], [15, 16], list(range(800, 900))], keep=0.9))
+
+
+def test_a_projection_of_queries_as_the_input():
+    """Queries inside wider rows, and scores of layers added up call by call."""
+    rng = np.random.default_rng(19)
+    sc = problem(rng, ("bf16", "bf16", 8, 2, 128), [200, 500], [[199], list(range(440, 500))], q_pad=512, in_place=True)
+    first = sc.reference()[0]
+    sc.call().check()
+    sc.prev64 = to64(sc.out).copy()
+    sc.call().check()
+    assert (sc.reference()[0] >= first - 1e-6).all()
+    sc.st.c.close()

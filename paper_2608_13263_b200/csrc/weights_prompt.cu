@@ -137,15 +137,14 @@ struct Item {
 struct Meta {                            // a tile of query rows
     int pmin, pmax, whole;               // whole: every row of the tile is there and saw something
     alignas(16) float lse2[TC_TILE];     // minus the logarithm to base 2
-    alignas(16) int pos[TC_TILE];        // -2^31: the row adds nothing
+    alignas(16) int pos[TC_TILE];        // -1: the row adds nothing
     alignas(16) float scale[TC_TILE];    // bf16 queries over 4-bit keys: factor of the row's scores
 };
 
-// 16 columns of a thread's accumulator row: what token `id` gets from 16 query rows, l: minus their logarithms
+// 16 columns of a thread's accumulator row: what token `id` gets from 16 query rows.  A row at p sees it when 0 <= p - id < reach.
 template <bool SCALED, bool MASKED>
-__device__ __forceinline__ void sum_columns(const VtkAttnArgs &a, const Meta &m, const uint32_t (&s)[16], const float4 (&l)[4], int col, int id, float2 (&sum)[2])
+__device__ __forceinline__ void sum_columns(float c, const Meta &m, const uint32_t (&s)[16], const float4 (&l)[4], int col, int id, uint32_t reach, float2 (&sum)[2])
 {
-    const float c = a.scale_log2;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
         float4 f = make_float4(c, c, c, c);
@@ -159,44 +158,43 @@ __device__ __forceinline__ void sum_columns(const VtkAttnArgs &a, const Meta &m,
         y1.x = vtk_exp2(y1.x); y1.y = vtk_exp2(y1.y);
         if (MASKED) {
             const int4 p = *reinterpret_cast<const int4 *>(&m.pos[col + i]);
-            y0.x = vtk_sees(id, p.x, vtk_floor(p.x, a.window), a.sinks) ? y0.x : 0.f;
-            y0.y = vtk_sees(id, p.y, vtk_floor(p.y, a.window), a.sinks) ? y0.y : 0.f;
-            y1.x = vtk_sees(id, p.z, vtk_floor(p.z, a.window), a.sinks) ? y1.x : 0.f;
-            y1.y = vtk_sees(id, p.w, vtk_floor(p.w, a.window), a.sinks) ? y1.y : 0.f;
+            y0.x = (uint32_t)p.x - (uint32_t)id < reach ? y0.x : 0.f;
+            y0.y = (uint32_t)p.y - (uint32_t)id < reach ? y0.y : 0.f;
+            y1.x = (uint32_t)p.z - (uint32_t)id < reach ? y1.x : 0.f;
+            y1.y = (uint32_t)p.w - (uint32_t)id < reach ? y1.y : 0.f;
         }
         sum[0] = add2(sum[0], y0);
         sum[1] = add2(sum[1], y1);
     }
 }
 
-// The sum over a tile's query rows.  free: none of them needs a mask.  (A branch at every mask would keep the compiler from
-// overlapping the chains of loads, products and exponentials: 6500 cycles a tile instead of 3700, in an earlier form.)
+// The sum over a tile's query rows.  free: none of them needs a mask (the columns behind them do).  Two loops of two steps: a branch at
+// every mask would keep the compiler from overlapping the chains of loads, products and exponentials (6500 cycles a tile instead of
+// 3700, in an earlier form), and what is unrolled further is fetched for longer than short items last.
 template <bool SCALED>
-__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, int rows, bool free)
+__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, uint32_t reach, int rows, bool free)
 {
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     uint32_t v[2][16];
     tc_ld16(src, v[0]);
-    auto step = [&](int col, uint32_t (&now)[16], uint32_t (&then)[16], bool masked) {
+    auto step = [&](int col, uint32_t (&now)[16], uint32_t (&then)[16], auto masked) {
         float4 l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) l[i] = *reinterpret_cast<const float4 *>(&m.lse2[col + 4 * i]);
         tc_wait_ld(now);
         if (col + 16 < rows) tc_ld16(src + col + 16, then);
-        if (masked) sum_columns<SCALED, true>(a, m, now, l, col, id, sum);
-        else sum_columns<SCALED, false>(a, m, now, l, col, id, sum);
+        sum_columns<SCALED, decltype(masked)::value>(a.scale_log2, m, now, l, col, id, reach, sum);
     };
-    if (free && rows == TC_TILE) {
-#pragma unroll
-        for (int col = 0; col < TC_TILE; col += 32) {
-            step(col, v[0], v[1], false);
-            step(col + 16, v[1], v[0], false);
-        }
-    } else {                                                 // (columns behind the rows are masked)
-        for (int col = 0; col < rows; col += 32) {
-            step(col, v[0], v[1], !free || col + 16 > rows);
-            if (col + 16 < rows) step(col + 16, v[1], v[0], !free || col + 32 > rows);
-        }
+    int col = 0;
+#pragma unroll 1
+    for (; free && col + 32 <= rows; col += 32) {
+        step(col, v[0], v[1], std::false_type());
+        step(col + 16, v[1], v[0], std::false_type());
+    }
+#pragma unroll 1
+    for (; col < rows; col += 32) {
+        step(col, v[0], v[1], std::true_type());
+        if (col + 16 < rows) step(col + 16, v[1], v[0], std::true_type());
     }
     sum[0] = add2(sum[0], sum[1]);
     return sum[0].x + sum[0].y;
@@ -251,6 +249,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
     __syncthreads();
     tc_after_sync();
     const uint32_t tmem = sh.tmem;
+    if (!SCALED && tid == WP_ROWS * 32) asm volatile("prefetch.tensormap [%0];" ::"l"(&queries) : "memory");
     const int rows = w.tokens * a.group;                     // of a tile
     constexpr uint32_t IDESC = (1u << 4) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 7) | ((Mma::kind == VTOKEN_KV_BF16 ? 1u : 0u) << 10) |
                                ((uint32_t)(TC_TILE >> 4) << 24) | ((uint32_t)(TC_TILE >> 3) << 17);
@@ -302,6 +301,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
             const bool every = __all_sync(0xffffffffu, there);
             const int id_lo = __reduce_min_sync(0xffffffffu, id), id_hi = __reduce_max_sync(0xffffffffu, there ? id : -1);
             const bool mine = x * TC_TILE < it.n;                                // (uniform)
+            const uint32_t reach = a.window == 0 || id < a.sinks ? 0x80000000u : (uint32_t)a.window;
             const int count = it.count;
             float total = 0.f;
             for (int j = (int)((n_tile ^ group) & 1); j < count; j += 2) {       // (tiles of the other group pass by)
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                     tc_after_sync();
                     const bool some = m.pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(m.pmin, a.window) || id_lo < a.sinks);
                     const bool full = every && m.whole && id_hi <= m.pmin && (id_lo > vtk_floor(m.pmax, a.window) || id_hi < a.sinks);
-                    if (some) total += row_sum<SCALED>(a, m, src, id, rows, full);
+                    if (some) total += row_sum<SCALED>(a, m, src, id, reach, rows, full);
                     tc_before_sync();
                     arrive(&sh.s_empty[x][group]);
                     ++n_mine;
@@ -504,9 +504,11 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                     const int tile = 32 * word + lane;
                     if (tile < tiles) {
                         const int64_t t0 = (int64_t)(it.tile0 + tile) * w.tokens, t1 = t0 + w.tokens < it.qn ? t0 + w.tokens : it.qn;
-#pragma unroll 8
-                        for (int64_t t = t0; t < t1; ++t) {
-                            const int p = a.positions[it.q0 + t];
+                        const int32_t *pos = a.positions.at(it.q0 + t0, t1 - t0);
+                        const int n = (int)(t1 - t0);
+#pragma unroll 16
+                        for (int t = 0; t < n; ++t) {
+                            const int p = pos[t];
                             pmin = p < pmin ? p : pmin;
                             pmax = p > pmax ? p : pmax;
                         }
@@ -609,7 +611,7 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     m.lse2[32 * i + lane] = now.l[i] * -1.4426950408889634f;
-                    m.pos[32 * i + lane] = now.l[i] == -INFINITY ? INT32_MIN : (now.p[i] < INT32_MAX - 1 ? now.p[i] : INT32_MAX - 1);    // (INT32_MAX: what is not there)
+                    m.pos[32 * i + lane] = now.l[i] == -INFINITY || now.p[i] < 0 ? -1 : (now.p[i] < INT32_MAX - 1 ? now.p[i] : INT32_MAX - 1);   // (INT32_MAX: what is not there)
                 }
                 if (lane == 0) {
                     m.pmin = pmin;

@@ -171,8 +171,9 @@ __device__ __forceinline__ void sum_columns(float c, const Meta &m, const uint32
 // The sum over a tile's query rows.  free: none of them needs a mask (the columns behind them do).  Two loops of two steps: a branch at
 // every mask would keep the compiler from overlapping the chains of loads, products and exponentials (6500 cycles a tile instead of
 // 3700, in an earlier form), and what is unrolled further is fetched for longer than short items last.
-template <bool SCALED>
-__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, uint32_t reach, int rows, bool free)
+// release: called when the last columns are in registers, so that the next product need not wait for their exponentials.
+template <bool SCALED, typename F>
+__device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, uint32_t src, int id, uint32_t reach, int rows, bool free, F release)
 {
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     uint32_t v[2][16];
@@ -183,6 +184,7 @@ __device__ __forceinline__ float row_sum(const VtkAttnArgs &a, const Meta &m, ui
         for (int i = 0; i < 4; ++i) l[i] = *reinterpret_cast<const float4 *>(&m.lse2[col + 4 * i]);
         tc_wait_ld(now);
         if (col + 16 < rows) tc_ld16(src + col + 16, then);
+        else release();
         sum_columns<SCALED, decltype(masked)::value>(a.scale_log2, m, now, l, col, id, reach, sum);
     };
     int col = 0;
@@ -314,9 +316,12 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
                     tc_after_sync();
                     const bool some = m.pmax >= id_lo && (a.window == 0 || id_hi > vtk_floor(m.pmin, a.window) || id_lo < a.sinks);
                     const bool full = every && m.whole && id_hi <= m.pmin && (id_lo > vtk_floor(m.pmax, a.window) || id_hi < a.sinks);
-                    if (some) total += row_sum<SCALED>(a, m, src, id, reach, rows, full);
-                    tc_before_sync();
-                    arrive(&sh.s_empty[x][group]);
+                    auto release = [&]() {
+                        tc_before_sync();
+                        arrive(&sh.s_empty[x][group]);
+                    };
+                    if (some) total += row_sum<SCALED>(a, m, src, id, reach, rows, full, release);
+                    else release();
                     ++n_mine;
                 }
                 arrive(&sh.meta_empty[slot]);

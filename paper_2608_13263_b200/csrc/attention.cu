@@ -505,41 +505,6 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
                 for (int e = 0; e < 4; ++e) o[i][h][e] = 0.f;
 #pragma unroll
         for (int h = 0; h < RH; ++h) { m[h] = -INFINITY; l[h] = 0.f; }
-        if (SHARED && use.k->prefix && use.t0 == 0 && tw == 0 && rows > 0) {
-            // what the prefix left: maxima and sums of the rows g (and 8 + g), values of 2t and 2t + 1 (+ 8)
-            auto place = [&](int row) -> int64_t {
-                if (row >= rows) return -1;
-                int64_t tok;
-                int head;
-                split_row(a, rt * NR + row, tok, head);
-                return (tok + use.k->q0) * a.hq + kv * a.group + head;
-            };
-#pragma unroll
-            for (int h = 0; h < RH; ++h) {
-                const int64_t mine = place(g + 8 * h);
-                if (mine >= 0) {
-                    const float2 ml = __ldcg(&a.pre_ml[mine]);
-                    m[h] = ml.x;
-                    l[h] = t == 0 ? ml.y : 0.f;              // (the row's four lanes are added up at the end)
-                }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float seen = __shfl_sync(0xffffffffu, m[h], 8 * t + 4 * e);
-                    const int64_t at = place(8 * h + 2 * t + e);
-                    if (at < 0 || seen == -INFINITY) continue;           // (a prefix without a token that the row sees holds no values)
-                    const float *src = a.pre_o + at * D;
-#pragma unroll
-                    for (int i = 0; i < MT; i += 2) {
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(src + Rows::vdim(g, i / 4) + 2 * (i % 4)));
-                        o[i][h][e] = x.x;
-                        o[i][h][2 + e] = x.y;
-                        o[i + 1][h][e] = x.z;
-                        o[i + 1][h][2 + e] = x.w;
-                    }
-                }
-            }
-        }
-
         for (int tl = use.t0 + tw; tl < use.t1; tl += lanes, ++used) {
             cp_wait<ST - 2>();
             __syncwarp();
@@ -654,6 +619,38 @@ __global__ void __launch_bounds__(Rows::WARPS * 32, 1) attention_rows_kernel(con
         for (int h = 0; h < RH; ++h) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+        }
+        if (SHARED && use.k->prefix && use.t0 == 0 && tw == 0 && rows > 0) {
+            // The shared prefix in front: maxima and sums of the rows g (and 8 + g), values of 2t and 2t + 1 (+ 8).  (Here and not as the
+            // state that the tiles begin with: registers that wait for it would be spilled in the loop over the tiles, 4-bit rows 86 us
+            // instead of 71.)
+            auto place = [&](int row) -> int64_t {
+                int64_t tok;
+                int head;
+                split_row(a, rt * NR + (row < rows ? row : 0), tok, head);
+                return (tok + use.k->q0) * a.hq + kv * a.group + head;
+            };
+#pragma unroll
+            for (int h = 0; h < RH; ++h) {
+                const float2 ml = g + 8 * h < rows ? __ldcg(&a.pre_ml[place(g + 8 * h)]) : make_float2(-INFINITY, 0.f);
+                const float top = fmaxf(m[h], ml.x), f = weight(m[h], top), f2 = weight(ml.x, top);
+                l[h] = l[h] * f + ml.y * f2;
+                m[h] = top;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float mine = __shfl_sync(0xffffffffu, f, 8 * t + 4 * e), theirs = __shfl_sync(0xffffffffu, f2, 8 * t + 4 * e);
+                    const bool there = 8 * h + 2 * t + e < rows && theirs != 0.f;          // (a prefix without a token that the row sees holds no values)
+                    const float *src = a.pre_o + place(8 * h + 2 * t + e) * D;
+#pragma unroll
+                    for (int i = 0; i < MT; i += 2) {
+                        const float4 x = there ? __ldcg(reinterpret_cast<const float4 *>(src + Rows::vdim(g, i / 4) + 2 * (i % 4))) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        o[i][h][e] = o[i][h][e] * mine + x.x * theirs;
+                        o[i][h][2 + e] = o[i][h][2 + e] * mine + x.y * theirs;
+                        o[i + 1][h][e] = o[i + 1][h][e] * mine + x.z * theirs;
+                        o[i + 1][h][2 + e] = o[i + 1][h][2 + e] * mine + x.w * theirs;
+                    }
+                }
+            }
         }
         for (int half = lanes / 2; half > 0; half >>= 1) {
             if (tw >= half && tw < 2 * half) {

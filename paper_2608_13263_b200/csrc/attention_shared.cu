@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int AS_NT = 1024, AS_TILE = 128, AS_PAIR = 2 * AS_TILE, AS_MIN_TILES = 2, AS_GROUPS = 1024, AS_SIZED = 64;
+constexpr int AS_NT = 1024, AS_TILE = 128, AS_PAIR = 2 * AS_TILE, AS_MIN_TILES = 2, AS_GROUPS = 1024, AS_SIZED = 64, AS_SIZES = 256;
 
 struct Args {
     VtkAttnArgs a;
@@ -23,6 +23,12 @@ struct Args {
     int64_t rows;                        // rows of the parts
     int32_t ctas;                        // of the prompt kernel
 };
+
+// (a 64-bit division is a subroutine of several hundred cycles)
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
+{
+    return ((uint64_t)(x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
 
 __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *warp_sum)
 {
@@ -69,8 +75,12 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
         }
         return lo;
     };
+    int first_group = -1;                                    // of the thread's first request, and its first group
+    VtkPrefixGroup mine;
+    mine.len = 0;
     for (int r = tid; r < R; r += AS_NT) {
         const int g = group_of(r);
+        if (r == tid) first_group = g;
         if (g >= 0) {
             int q0, qn, len;
             int64_t base;
@@ -80,8 +90,9 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
             atomicMin(&group_len[g], want < 0 ? 0 : (want > len ? len : want));
             if (qn > 0 && (int64_t)qn * a.group <= a.row_limit) atomicAdd(&group_readers[g], 1);
         }
-        s.shared[r] = g;
+        if (r != tid) s.shared[r] = g;
     }
+    const int tokens = R > 0 ? vtk_clamp_offset(a.q_offsets[R], a.max_query_tokens) : 0;
     __syncthreads();
     // tiles in all, for parts of a size that gives every CTA one
     int64_t work = 0;
@@ -99,7 +110,7 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
         // (one reader: nothing to gain)
         if (now(&group_readers[g]) < 2 || x.end <= x.first || x.q1 <= x.q0 || x.len == INT32_MAX) x.len = 0;
         group_len[g] = x.len;
-        x.items = ((int64_t)(x.q1 - x.q0) * a.group + AS_PAIR - 1) / AS_PAIR * a.hkv;
+        x.items = (((int64_t)(x.q1 - x.q0) * a.group + AS_PAIR - 1) >> 8) * a.hkv;
         x.tiles = (x.len + AS_TILE - 1) / AS_TILE;
         x.splits = 0;
         x.rows = 0;
@@ -108,23 +119,24 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
             few_units[g] = x.len > 0 ? (int)x.items : 0;
             group_tiles[g] = x.tiles;
         }
+        if (g == tid) mine = x;
         s.groups[g] = x;
     }
     work = block_sum(work, warp_sum[0]);
-    const int tokens = R > 0 ? vtk_clamp_offset(a.q_offsets[R], a.max_query_tokens) : 0;
-    const int64_t most = tokens > 0 ? s.rows / ((int64_t)tokens * a.hq) : 1;      // parts that there is room for
+    const int64_t most = tokens > 0 ? divide(s.rows, (int64_t)tokens * a.hq) : 1;    // parts that there is room for
     // Tiles of a part.  A part costs about five tiles to start, and a CTA that gets one part more than the others is waited for: of sizes
     // upwards of one that gives every CTA its share the one with the fewest (rounds of parts) x (size + 5).
-    int64_t size = (work + s.ctas - 1) / s.ctas;
+    int64_t size = divide(work + s.ctas - 1, s.ctas);
     size = size < AS_MIN_TILES ? AS_MIN_TILES : size;
     if (G <= AS_SIZED) {
         int64_t cost = INT64_MAX;
-        int64_t items = 0;
-        const int64_t mine = size / 4 + 1 + tid;
-        if (mine >= AS_MIN_TILES) {
-            for (int g = 0; g < G; ++g) items += few_units[g] * ((group_tiles[g] + mine - 1) / mine);
-            const int64_t rounds = (items + s.ctas - 1) / s.ctas;
-            cost = (rounds * (mine + 5)) << 32 | mine;
+        const int64_t candidate = size / 4 + 1 + tid;
+        if (tid < AS_SIZES && candidate >= AS_MIN_TILES && candidate < (1 << 24)) {
+            const uint32_t each = (uint32_t)candidate;
+            int64_t items = 0;
+#pragma unroll 4
+            for (int g = 0; g < G; ++g) items += (int64_t)few_units[g] * (((uint32_t)group_tiles[g] + each - 1) / each);
+            cost = (divide(items + s.ctas - 1, s.ctas) * (candidate + 5)) << 24 | candidate;
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
@@ -135,21 +147,22 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
         __syncthreads();
         for (int w = 0; w < AS_NT / 32; ++w) cost = warp_sum[0][w] < cost ? warp_sum[0][w] : cost;
         __syncthreads();
-        size = cost & 0xffffffff;
+        if (cost != INT64_MAX) size = cost & 0xffffff;
     }
     int64_t items_before = 0, rows_before = 0;
     for (int g0 = 0; g0 < G; g0 += AS_NT) {
         const int g = g0 + tid;
         int64_t items = 0, rows = 0;
         int tiles = 0, splits = 0;
-        if (g < G && s.groups[g].len > 0) {
-            const int all = s.groups[g].tiles;
-            int64_t each = (all + most - 1) / most;
+        VtkPrefixGroup x = mine;
+        if (g0 > 0 && g < G) x = s.groups[g];
+        if (g < G && x.len > 0) {
+            int64_t each = divide(x.tiles + most - 1, most);
             each = each < size ? size : each;
-            splits = (int)((all + each - 1) / each);
-            tiles = (all + splits - 1) / splits;
-            items = s.groups[g].items * splits;
-            rows = splits > 1 ? (int64_t)(s.groups[g].q1 - s.groups[g].q0) * a.hq : 0;
+            splits = (int)divide(x.tiles + each - 1, each);
+            tiles = (x.tiles + splits - 1) / splits;
+            items = x.items * splits;
+            rows = splits > 1 ? (int64_t)(x.q1 - x.q0) * a.hq : 0;
         }
         const int64_t incl = vtk_warp_incl_scan(items), incl_rows = vtk_warp_incl_scan(rows);
         if (lane == 31) { warp_sum[0][warp] = incl; warp_sum[1][warp] = incl_rows; }
@@ -168,7 +181,10 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
         }
         __syncthreads();
     }
-    for (int r = tid; r < R; r += AS_NT) s.shared[r] = s.shared[r] < 0 ? 0 : now(&group_len[s.shared[r]]);
+    for (int r = tid; r < R; r += AS_NT) {
+        const int g = r == tid ? first_group : s.shared[r];
+        s.shared[r] = g < 0 ? 0 : now(&group_len[g]);
+    }
     if (tid == 0) {
         s.plan->items = items_before;
         s.plan->rows = rows_before;
@@ -202,11 +218,13 @@ __global__ void __launch_bounds__(256) shared_join_kernel(const __grid_constant_
         float top = -INFINITY, sum = 0.f, o[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) o[j] = 0.f;
-        for (int k = lane; k < parts; k += 32) top = fmaxf(top, __ldcg(&a.pre_ml[k * stride + at]).x);
+        const float2 ml0 = lane < parts ? __ldcg(&a.pre_ml[lane * stride + at]) : make_float2(-INFINITY, 0.f);
+        top = ml0.x;
+        for (int k = 32 + lane; k < parts; k += 32) top = fmaxf(top, __ldcg(&a.pre_ml[k * stride + at]).x);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         for (int k0 = 0; k0 < parts; k0 += 32) {
-            const float2 ml = k0 + lane < parts ? __ldcg(&a.pre_ml[(k0 + lane) * stride + at]) : make_float2(-INFINITY, 0.f);
+            const float2 ml = k0 == 0 ? ml0 : (k0 + lane < parts ? __ldcg(&a.pre_ml[(k0 + lane) * stride + at]) : make_float2(-INFINITY, 0.f));
             const float mine = ml.x == -INFINITY ? 0.f : vtk_exp2(ml.x - top);
             const int n = parts - k0 < 32 ? parts - k0 : 32;
 #pragma unroll 8

@@ -30,14 +30,18 @@ __device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
     return ((uint64_t)(x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *warp_sum)
+// warps: those that have something
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *warp_sum, int warps)
 {
+    const int warp = threadIdx.x >> 5;
+    if (warp < warps) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    if (vtk_lane() == 0) warp_sum[threadIdx.x >> 5] = x;
+        for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+        if (vtk_lane() == 0) warp_sum[warp] = x;
+    }
     __syncthreads();
     int64_t sum = 0;
-    for (int w = 0; w < AS_NT / 32; ++w) sum += warp_sum[w];
+    for (int w = 0; w < warps; ++w) sum += warp_sum[w];
     __syncthreads();
     return sum;
 }
@@ -122,7 +126,8 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
         if (g == tid) mine = x;
         s.groups[g] = x;
     }
-    work = block_sum(work, warp_sum[0]);
+    const int warps = G < AS_NT ? (G + 31) / 32 : AS_NT / 32;               // that have groups
+    work = block_sum(work, warp_sum[0], warps);
     const int64_t most = tokens > 0 ? divide(s.rows, (int64_t)tokens * a.hq) : 1;    // parts that there is room for
     // Tiles of a part.  A part costs about five tiles to start, and a CTA that gets one part more than the others is waited for: of sizes
     // upwards of one that gives every CTA its share the one with the fewest (rounds of parts) x (size + 5).
@@ -131,21 +136,23 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
     if (G <= AS_SIZED) {
         int64_t cost = INT64_MAX;
         const int64_t candidate = size / 4 + 1 + tid;
-        if (tid < AS_SIZES && candidate >= AS_MIN_TILES && candidate < (1 << 24)) {
-            const uint32_t each = (uint32_t)candidate;
-            int64_t items = 0;
+        if (tid < AS_SIZES) {
+            if (candidate >= AS_MIN_TILES && candidate < (1 << 22)) {
+                const float inverse = 1.f / (float)candidate;
+                int64_t items = 0;
 #pragma unroll 4
-            for (int g = 0; g < G; ++g) items += (int64_t)few_units[g] * (((uint32_t)group_tiles[g] + each - 1) / each);
-            cost = (divide(items + s.ctas - 1, s.ctas) * (candidate + 5)) << 24 | candidate;
-        }
+                for (int g = 0; g < G; ++g) items += (int64_t)few_units[g] * (int)(((float)group_tiles[g] - 0.5f) * inverse + 1.f);     // (parts: a quotient rounded up)
+                cost = (divide(items + s.ctas - 1, s.ctas) * (candidate + 5)) << 24 | candidate;
+            }
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            const int64_t o = __shfl_xor_sync(0xffffffffu, cost, d);
-            cost = o < cost ? o : cost;
+            for (int d = 16; d > 0; d >>= 1) {
+                const int64_t o = __shfl_xor_sync(0xffffffffu, cost, d);
+                cost = o < cost ? o : cost;
+            }
+            if (lane == 0) warp_sum[0][warp] = cost;
         }
-        if (lane == 0) warp_sum[0][warp] = cost;
         __syncthreads();
-        for (int w = 0; w < AS_NT / 32; ++w) cost = warp_sum[0][w] < cost ? warp_sum[0][w] : cost;
+        for (int w = 0; w < AS_SIZES / 32; ++w) cost = warp_sum[0][w] < cost ? warp_sum[0][w] : cost;
         __syncthreads();
         if (cost != INT64_MAX) size = cost & 0xffffff;
     }
@@ -164,11 +171,15 @@ __global__ void __launch_bounds__(AS_NT) shared_plan_kernel(const __grid_constan
             items = x.items * splits;
             rows = splits > 1 ? (int64_t)(x.q1 - x.q0) * a.hq : 0;
         }
-        const int64_t incl = vtk_warp_incl_scan(items), incl_rows = vtk_warp_incl_scan(rows);
-        if (lane == 31) { warp_sum[0][warp] = incl; warp_sum[1][warp] = incl_rows; }
+        int64_t incl = 0, incl_rows = 0;
+        if (warp < warps) {
+            incl = vtk_warp_incl_scan(items);
+            incl_rows = vtk_warp_incl_scan(rows);
+            if (lane == 31) { warp_sum[0][warp] = incl; warp_sum[1][warp] = incl_rows; }
+        }
         __syncthreads();
         int64_t in_front = items_before, rows_in_front = rows_before;
-        for (int w = 0; w < AS_NT / 32; ++w) {
+        for (int w = 0; w < warps; ++w) {
             if (w < warp) { in_front += warp_sum[0][w]; rows_in_front += warp_sum[1][w]; }
             items_before += warp_sum[0][w];
             rows_before += warp_sum[1][w];

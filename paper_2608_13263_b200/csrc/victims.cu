@@ -4,7 +4,11 @@
 // a histogram in shared memory, a scan, the digit that holds the rank), then the candidates below it -- and the last of those
 // equal to it -- are listed in order.  v follows from lengths and budget alone, so every CTA works out for itself where its
 // request's victims start, and one launch does it all.  Keys stay in shared memory as far as they fit; a long request is shared out
-// over a cluster, whose CTAs read one another's histograms.
+// over a cluster, whose CTAs each add up a share of all their bins.
+//
+// Bound by instructions and barriers, not by what is read: 512 requests of 1.5 M tokens in all, 18 MB, take 24 us, where the longest
+// request's CTA is waited for; six requests of 50 000 to 131 072 tokens 21 us on clusters of 16.  256 threads a request, so that four are
+// resident on an SM (512 threads: 46 us); every CTA of a cluster reading all bins of all others: 41 us for the six.
 #include <atomic>
 
 #include "attention.cuh"

@@ -302,3 +302,35 @@ def test_refusals():
     with pytest.raises(vt.VtokenError):
         vt.vtoken_attention_shared_workspace_bytes(g.c.ctx, g.c.heads, -1)
     g.close()
+
+
+@pytest.mark.parametrize("geometry", [GEOMETRIES[0], GEOMETRIES[4]], ids=["bf16", "fp4"])
+def test_a_masked_nan_next_to_single_tokens(geometry):
+    """Requests of one query token, whose own tokens are never masked: what they must not see is in the prefix alone."""
+    import torch
+    rng = np.random.default_rng(17)
+    g = Groups(rng, geometry, [(200, [1, 4, 2, 5, 2, 1])], lambda lens: [[199], [120], [149], [204], [3], [150]])
+    c, s = g.c, int(g.st.slots[0][150])
+    if c.kv == "fp4":
+        c.v_pool[c.layer, s, c.hkv * c.d // 2] = 0x7f
+        c.v64[s] = c.v64[s].copy()
+        c.v64[s][0, :16] = np.nan
+    else:
+        c.v_pool[c.layer, s, 3] = float("nan")
+        c.v64[s] = c.v64[s].copy()
+        c.v64[s][0, 3] = np.nan
+    torch.cuda.synchronize()
+    g.call()
+    out, _ = g.st.outputs()
+    ref, _, tol, _ = g.st.reference()
+    fine = np.isfinite(ref)
+    assert fine[[1, 2, 4]].all() and not fine[[0, 3, 5]].all((1, 2)).any()
+    assert np.array_equal(np.isfinite(out), fine)
+    assert (np.abs(out - ref)[fine] <= tol[fine]).all()
+    g.close()
+
+
+def test_many_short_requests_behind_windowed_prefixes():
+    """More segments than shares of tiles, most of the prefix out of sight."""
+    rng = np.random.default_rng(18)
+    run_and_check(Groups(rng, ("fp16", "fp16", 7, 1, 128), [(400, [28] * 14), (300, [5] * 20), (64, [33] * 30)], window=45))

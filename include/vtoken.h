@@ -662,8 +662,10 @@ typedef struct {                   /* all pointers DEVICE */
     int64_t out_stride;            /* elements, multiple of 8; 0: dense */
     float *lse;                    /* [max_query_tokens][num_q_heads] or NULL: natural logarithm of the sum of the
                                       exponentials of the scaled scores */
-    void *workspace;               /* 16-byte aligned, zeroed by the caller once, when it is allocated; each call leaves
-                                      it ready for the next.  Calls that may overlap need workspaces of their own */
+    void *workspace;               /* 16-byte aligned, zeroed by the caller once, when it is allocated; each call leaves it
+                                      ready for the next, of vtoken_attention, vtoken_attention_shared or vtoken_token_weights
+                                      alike: one that is large enough for each serves them in turn on one context.  Calls
+                                      that may overlap need workspaces of their own */
     int64_t workspace_bytes;       /* >= vtoken_attention_workspace_bytes (VTOKEN_ECAPACITY otherwise) */
 } vtoken_attention_in;
 
@@ -700,7 +702,7 @@ typedef struct {                   /* all pointers DEVICE; the fields of vtoken_
     const float *prev;             /* [max_tokens of the context] scores before the call; may be `scores` itself; NULL, or
                                       decay 0: none (nothing is read there) */
     float *scores;                 /* [max_tokens of the context] token i of request r is at tt_offsets[r] + i */
-    void *workspace;               /* as in vtoken_attention_in */
+    void *workspace;               /* as in vtoken_attention_in, and may be the same */
     int64_t workspace_bytes;       /* >= vtoken_token_weights_workspace_bytes (VTOKEN_ECAPACITY otherwise) */
 } vtoken_weights_in;
 

@@ -896,9 +896,9 @@ int launch_by_heads(vtoken_ctx *ctx, const vtoken_heads *heads, bool wide, const
 // rows, 8 with 16.
 int64_t vtk_attention_rows_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs *a)
 {
-    const int64_t shares = (int64_t)ctx->num_sms * 16, counters = shares * 4 + 16;       // (the prompt kernel's two tickets in front)
-    if (a) a->part = (float *)((uint8_t *)(a->counters - 4) + counters);
-    return counters + shares * 2 * 8 * (heads->head_dim + 2) * 4;
+    const int64_t shares = (int64_t)ctx->num_sms * VTK_CTA_SHARES, zeros = vtk_workspace_zeros(ctx);
+    if (a) a->part = (float *)((uint8_t *)a->counters - VTK_TICKET_BYTES + zeros);
+    return zeros + shares * 2 * 8 * (heads->head_dim + 2) * 4;
 }
 
 int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, bool shared, cudaStream_t st)
@@ -950,7 +950,7 @@ int vtk_attention_args(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer
     a.scale_log2 = scale;
     a.v_mul = vtk_two_to(heads->v_exponent);
     a.flags = &ctx->rt_counts->error_flags;
-    a.counters = (uint32_t *)in->workspace + 4;
+    a.counters = (uint32_t *)((uint8_t *)in->workspace + VTK_TICKET_BYTES);
     a.part = nullptr;
     a.plan = nullptr;
     a.groups = nullptr;

@@ -371,6 +371,11 @@ inline bool vtk_score_scale(const vtoken_heads *heads, float sm_scale, float &sc
     return sm_scale > -1e30f && sm_scale < 1e30f && scale > -INFINITY && scale < INFINITY;
 }
 
+// host: the beginning of every workspace, zero between calls whichever they are: two tickets of the kernels for many query rows, then
+// the arrivals that attention.cu counts, one for each head of a share (at most 16 a CTA).  What a call writes besides lies behind it.
+constexpr int VTK_TICKET_BYTES = 16, VTK_CTA_SHARES = 16;
+inline int64_t vtk_workspace_zeros(const vtoken_ctx *ctx) { return VTK_TICKET_BYTES + (int64_t)ctx->num_sms * VTK_CTA_SHARES * 4; }
+
 // host: launchers of attention.cu and of attention_prompt.cu
 int vtk_launch_attention_rows(vtoken_ctx *ctx, const vtoken_heads *heads, VtkAttnArgs a, int32_t max_query_len, bool shared, cudaStream_t st);
 int vtk_launch_attention_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkAttnArgs &a, uint32_t *tickets, bool prefix, cudaStream_t st);

@@ -744,7 +744,7 @@ int launch_by_type(vtoken_ctx *ctx, const vtoken_heads *h, const Args &w, cudaSt
 
 int64_t vtk_weights_prompt_workspace(const vtoken_ctx *ctx, const vtoken_heads *heads, int32_t max_query_tokens)
 {
-    return 16 + parts_of(ctx, heads, max_query_tokens) * WP_PAIR * 4;
+    return vtk_workspace_zeros(ctx) + parts_of(ctx, heads, max_query_tokens) * WP_PAIR * 4;
 }
 
 int vtk_launch_weights_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const VtkWeightsArgs &weights, void *workspace, cudaStream_t st)
@@ -752,7 +752,7 @@ int vtk_launch_weights_prompt(vtoken_ctx *ctx, const vtoken_heads *heads, const 
     Args w;
     w.w = weights;
     w.tickets = (uint32_t *)workspace;
-    w.parts = (float *)((uint8_t *)workspace + 16);
+    w.parts = (float *)((uint8_t *)workspace + vtk_workspace_zeros(ctx));     // (attention counts in front of them)
     w.max_parts = parts_of(ctx, heads, weights.at.max_query_tokens);
     w.row_limit = weights.at.row_limit;
     w.grid = ctx->num_sms;

@@ -796,8 +796,10 @@ int64_t vtoken_attention_shared_workspace_bytes(const vtoken_ctx *ctx, const vto
 
 /* vtoken_attention (same arguments, results and masks; in->workspace_bytes >= vtoken_attention_shared_workspace_bytes) for
  * requests whose caches begin with the same entries, as the planners' protected blocks hold them: the rows of a prefix are read
- * once for the query rows of its whole group, and each request goes on over its own entries from there.  Requests of more than
- * 32 query rows (tokens times heads of a key head) read the prefix for themselves. */
+ * once for the query rows of its whole group, and each request goes on over its own entries from there, with weights of as many
+ * bits as in the kernel for few rows of vtoken_attention.  Where in->max_query_len times the heads of a key head is more than 32,
+ * requests of more than 32 query rows (tokens times heads of a key head) read the prefix for themselves, in the prompt kernel and
+ * with its weights; with a smaller hint they share it like the others. */
 int vtoken_attention_shared(vtoken_ctx *ctx, const vtoken_heads *heads, int32_t layer, const vtoken_attention_in *in,
                             const vtoken_shared_in *shared, void *cuda_stream);
 

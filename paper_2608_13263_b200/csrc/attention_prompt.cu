@@ -11,7 +11,8 @@
 // row tiles share it again.  Roles, 16 warps:
 //   0 .. 3, 4 .. 7   softmax of row tile 0 and 1, one thread a row: scores from tensor memory, running maximum (moved
 //                    only when a score passes it by 2^8), exponentials, P as 16 bits back into the scores' columns (rounded once, as
-//                    a second product for the rest would double the tensor work: error against 64 bits 0.0021 for 0.0016, bf16)
+//                    a second product for the rest would double the tensor work: error against 64 bits 0.0021 for 0.0016, bf16; behind
+//                    shared prefixes, whose rows are not bound by it, twice)
 //   8 .. 11          producers: rows of Q, K and V gathered by slot into 128-byte-swizzled tiles, 16 bytes a thread by
 //                    cp.async, or 4-bit rows expanded to half precision in registers on the way
 //   12               one thread issues every tcgen05.mma: S = Q K^T (both operands from shared memory, K-major),
@@ -278,6 +279,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
 {
     using Mma = typename std::conditional<FP4, VtkFp16, Act>::type;
     constexpr int PANEL = AP_TILE * 128, PIECES = D / 8;
+    // Rows behind a prefix get the weights that the kernel for few rows would have given them, the sum of two 16-bit numbers (over 4-bit
+    // rows with bf16 queries: one in half precision).  Scores are in registers when P is written, so the second number lies where the
+    // other half of the scores was; the product over V is issued once more for it.  (One number: an error of up to 2^-8 of every bf16 weight,
+    // as large as the output's own rounding.  Two cost nothing behind 8192 tokens in bf16, 110 us a call either way, and 8 of 157 us
+    // behind 32 prefixes in fp16, where softmax warps are what is waited for.)
+    constexpr bool SPLIT_P = PREFIX && !(FP4 && Act::kind == VTOKEN_KV_BF16);
+    constexpr int P_LOW = AP_TILE / 2;                       // columns from the first number to the second
     extern __shared__ uint8_t raw[];
     Shared<D> &sh = *reinterpret_cast<Shared<D> *>(raw + ((1024 - (vtk_smem_u32(raw) & 1023)) & 1023));
     vtk_release_successor();
@@ -442,7 +450,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                     const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        uint32_t p[16];
+                        uint32_t p[16], low[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             float2 y = fma2(make_float2(__uint_as_float(s[q][2 * i]), __uint_as_float(s[q][2 * i + 1])), c2, mc2);
@@ -450,8 +458,13 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                             y.y = vtk_exp2(y.y);
                             sum[i & 1] = add2(sum[i & 1], y);
                             p[i] = Mma::pack(y.x, y.y);
+                            if (SPLIT_P) {
+                                const float2 r = Mma::unpack(p[i]);
+                                low[i] = Mma::pack(y.x - r.x, y.y - r.y);
+                            }
                         }
                         tc_st16(t_s + 16 * q, p);
+                        if (SPLIT_P) tc_st16(t_s + P_LOW + 16 * q, low);
                         if (q & 1) {                                             // half of P: the product over it can start
                             tc_wait_st();
                             tc_before_sync();
@@ -747,6 +760,7 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
                 for (int i = 0; i < AP_TILE / 32; ++i) {
                     const int k = half * (AP_TILE / 32) + i;
                     tc_mma_ts(one, tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + 8 * k, vd + (k * 16 * 128 >> 4), idesc_o, !first || k > 0);
+                    if (SPLIT_P) tc_mma_ts(one, tmem + 2 * AP_TILE + x * D, tmem + x * AP_TILE + P_LOW + 8 * k, vd + (k * 16 * 128 >> 4), idesc_o, 1);
                 }
             };
             bool ok = wait(&sh.q_full, q_count & 1) && wait_tile(k0);

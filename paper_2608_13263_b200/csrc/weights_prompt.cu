@@ -555,9 +555,9 @@ __global__ void __launch_bounds__(WP_NT, 1) weights_prompt_kernel(const __grid_c
             const int count = it.count;
             int word = -1;
             uint32_t left = 0;
-            auto next_tile = [&]() {
-                while (left == 0) left = it.sees[++word];
-                const int64_t t0 = (int64_t)(it.tile0 + 32 * word + __ffs(left) - 1) * w.tokens;
+            auto next_tile = [&]() {                         // (`count` bits are set; the search ends whatever is found there)
+                while (left == 0 && word + 1 < WP_WORDS) left = it.sees[++word];
+                const int64_t t0 = (int64_t)(it.tile0 + (left == 0 ? 0 : 32 * word + __ffs(left) - 1)) * w.tokens;
                 left &= left - 1;
                 return t0;
             };

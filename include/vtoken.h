@@ -779,7 +779,8 @@ typedef struct {                   /* all pointers DEVICE */
  * max(0, p_i - q_i) at the first rejected draft (from p_i if that has no mass), from the last row when none was rejected: the
  * first token whose cumulated mass exceeds sample_random times all of it.  Products and sums in 64 bits.  A probability that is
  * not a positive finite number counts as 0, and so does that of a draft outside [0, vocab); a row without mass gives the token -1.
- * Victims beyond max_victims are dropped (VTOKEN_FLAG_CAPACITY). */
+ * Victims beyond max_victims are dropped (VTOKEN_FLAG_CAPACITY).  How many SMs work on a request follows from max_requests of the context:
+ * a few requests are verified fastest in a context for few (the call does not look at the pools). */
 int vtoken_verify_drafts(vtoken_ctx *ctx, const vtoken_verify_in *in, void *cuda_stream);
 
 /* ---- Attention behind shared prefixes --------------------------------------------------------------- */

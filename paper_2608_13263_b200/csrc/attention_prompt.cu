@@ -282,8 +282,8 @@ __global__ void __launch_bounds__(AP_NT, 1) attention_prompt_kernel(const __grid
     // Rows behind a prefix get the weights that the kernel for few rows would have given them, the sum of two 16-bit numbers (over 4-bit
     // rows with bf16 queries: one in half precision).  Scores are in registers when P is written, so the second number lies where the
     // other half of the scores was; the product over V is issued once more for it.  (One number: an error of up to 2^-8 of every bf16 weight,
-    // as large as the output's own rounding.  Two cost nothing behind 8192 tokens in bf16, 110 us a call either way, and 8 of 157 us
-    // behind 32 prefixes in fp16, where softmax warps are what is waited for.)
+    // as large as the output's own rounding.  Two cost 2 of 112 us a call behind 8192 tokens in bf16 and 10 of 160 behind 32
+    // prefixes in fp16, where softmax warps are what is waited for.)
     constexpr bool SPLIT_P = PREFIX && !(FP4 && Act::kind == VTOKEN_KV_BF16);
     constexpr int P_LOW = AP_TILE / 2;                       // columns from the first number to the second
     extern __shared__ uint8_t raw[];

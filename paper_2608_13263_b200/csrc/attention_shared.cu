@@ -7,7 +7,7 @@
 // part of the tokens leaves is all that the other part needs, so nothing is rounded in between and there is nothing to join behind.
 // Requests of many rows are left to the prompt kernel, which is bound by the products and not by what it reads.
 //
-// 64 requests behind 8192 tokens, 32 heads over 8: 110 us, of which own tokens (160 MB) take 50, the prefix 35 (10 until its first scores,
+// 64 requests behind 8192 tokens, 32 heads over 8: 113 us, of which own tokens (160 MB) take 50, the prefix 38 (10 until its first scores,
 // 2.6 for each 256 rows and 128 tokens), planning and joining 15; without sharing the prefix would be 2.1 GB to read.
 #include "attention.cuh"
 

@@ -4,7 +4,7 @@
 // warps take consecutive runs of the row and sum them in 64 bits, the CTAs exchange their sums, and the run that holds the drawn mass is
 // cut up among its CTA's warps once more before one of them walks over what is left.  The drafts before it need two numbers each.  One more cluster tests the drafts of all
 // requests and lists the rejected ones, so that a step is one launch.  200 requests, vocabulary 128 256: 44 us, 4.7 TB/s; one request of
-// 32 000: 8 us, a chain of dependent loads.
+// 32 000: 8 us, a chain of dependent loads.  (The forms that read 16 bytes at a time spill 224 bytes a thread at three CTAs an SM.)
 #include "cluster.cuh"
 #include "heads.cuh"
 
@@ -360,7 +360,8 @@ template <typename P>
 int launch(vtoken_ctx *ctx, const VerifyArgs &a, bool vec, cudaStream_t st)
 {
     // CTAs of a request: two for each SM in all, a CTA not below 2048 elements.  (Many requests: a cluster whose CTAs do not start
-    // together waits for the last, 200 requests of 128 256 take 91 us with eight CTAs each and 44 with two.)
+    // together waits for the last, 200 requests of 128 256 take 91 us with eight CTAs each and 44 with two.)  The number of requests is on the
+    // device, so the context's capacity stands for it: one request of 128 256 takes 11.5 us in a context for up to 64, 33 in one for 512.
     int size = 1;
     while (size < 8 && a.vocab > size * VD_NT * 8 && (int64_t)a.max_requests * size < 2 * ctx->num_sms) size *= 2;
     const int64_t most = (int64_t)ctx->num_sms * 8 / size;

@@ -8,8 +8,10 @@
 // product is taken as S^T = K Q^T, mma.m16n8k16 with the 16 tokens as rows and 8 query rows as columns: no row of the instruction is
 // empty, a lane's accumulators belong to two tokens whose ids it holds, and the sum over query rows is one over four lanes.  (As
 // S = Q K^T, with half of the instruction empty, twelve shuffles a tile and K one tile ahead in registers, 512 requests took 428 us,
-// 256 over 4-bit rows 472.)  The order of the contracted dimension is free, so 8 dimensions of a token, 16 bytes, are the fragments
-// of two instructions, see attention.cu.  The heads' sums of a token meet in shared memory, in the order of the heads.
+// 256 over 4-bit rows 472.)  Up to 8 RH query rows of a head stay in registers; more are fetched again for every tile, which is right
+// but slow (256 requests, 64 heads over 8, one to four query tokens: 184, 212, 663, 781 us; over 4-bit rows 139, 204, 857, 966).  The
+// order of the contracted dimension is free, so 8 dimensions of a token, 16 bytes, are the fragments of two instructions, see
+// attention.cu.  The heads' sums of a token meet in shared memory, in the order of the heads.
 #include "weights.cuh"
 
 namespace {
